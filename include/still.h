@@ -305,6 +305,105 @@ still_status still_attend_scratch(const still_attend_config *cfg, const void *q,
                                   const void *C_k, const void *C_v, const float *beta, const void *K,
                                   const void *V, void *out, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Paged cache of many sequences: compact entries and the fresh tokens behind
+ * them (Appendix B, logical vs physical cache length), for a serving loop.
+ *
+ * One layer's pages hold `page_size` entries of every KV head each.  A
+ * sequence's entry j lives in slot j % page_size of page
+ * table[s * table_stride + j / page_size].  lens[s] is its number of entries;
+ * a length below 0 counts as 0, one above max_pages * page_size as that.  A
+ * table entry outside [0, n_pages) is an absent page: nothing is written to
+ * it, its entries read as zeros and no query sees them.  Both arrays are read
+ * on the device, so calls can be captured into a graph while they change.
+ * Table and lengths must be the same for the whole of a call.  Positions and
+ * rotation as in still_attend.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t n_kv_heads;   /* H, 1 .. 65535                                          */
+  int32_t head_dim;     /* d in {64, 128, 256}                                    */
+  int32_t page_size;    /* entries per page: a power of two, 16 .. 4096           */
+  int32_t n_pages;      /* pages in the pool, >= 1                                */
+  int32_t mode;         /* still_mode: element type of k, v and of the rows given */
+  void *k, *v;          /* [n_pages][H][page_size][d] (device, 16-byte aligned)   */
+  float *beta;          /* [n_pages][H][page_size]: the entries' bias; NULL: none */
+} still_paged_cache;
+
+typedef struct {
+  int32_t n_seqs;       /* 1 .. 65535                                             */
+  int32_t max_pages;    /* table entries per sequence that count, >= 1;
+                           max_pages * page_size <= 2^30                          */
+  int32_t table_stride; /* table entries between sequences, >= max_pages          */
+  const int32_t *table; /* [n_seqs][table_stride] (device)                        */
+  const int32_t *lens;  /* [n_seqs] (device)                                      */
+} still_paged_seqs;
+
+/* Rows to append.  Token i's row of KV head h starts token_stride * i +
+ * head_stride * h elements behind the pointer and is contiguous; strides are
+ * multiples of 16 bytes (so slices of a fused projection's rows and the
+ * compactor's [H][t][d] outputs are taken as they are). */
+typedef struct {
+  int32_t n_tokens;                      /* >= 0                                               */
+  const void *k, *v;
+  int64_t k_token_stride, k_head_stride; /* elements                                           */
+  int64_t v_token_stride, v_head_stride;
+  const float *beta;                     /* their bias (NULL: 0); needs the cache's beta       */
+  int64_t beta_token_stride, beta_head_stride;
+  const int32_t *offsets;                /* [n_seqs + 1] (device), not decreasing: sequence s has
+                                            tokens offsets[s] .. offsets[s + 1] - 1; tokens outside
+                                            all of them are skipped.  NULL: n_tokens / n_seqs each */
+  const double *positions;               /* [n_tokens] logical positions (required iff rope_theta > 0) */
+  double rope_theta;                     /* > 0: keys are rotated at their positions; 0: stored as given */
+} still_paged_tokens;
+
+/* Append tokens to their sequences, whose lengths count them already: the last
+ * of sequence s's tokens becomes entry lens[s] - 1, the others the entries
+ * before it.  A token whose entry would lie outside [0, max_pages * page_size)
+ * is skipped.  Where the cache keeps bias, the entries' bias is written too.
+ * Nothing else in the pages changes.  The entries that one call writes must be
+ * distinct.  Errors and asynchrony as the compaction calls. */
+still_status still_paged_append(const still_paged_cache *cache, const still_paged_seqs *seqs,
+                                const still_paged_tokens *tokens, void *stream);
+
+/* Entries [start, start + n) of sequence `seq` as dense rows K, V [H][n][d] and
+ * beta [H][n] (NULL: not written; needs the cache's beta): what the compaction
+ * calls read.  Entries past the sequence's length read as zeros.
+ * 0 <= start, 0 <= n, start + n <= max_pages * page_size. */
+still_status still_paged_gather(const still_paged_cache *cache, const still_paged_seqs *seqs, int32_t seq,
+                                int32_t start, int32_t n, void *K, void *V, float *beta, void *stream);
+
+/* Attention of the n_queries newest tokens of every sequence over its entries:
+ *   out = sum_j exp(s_j) v_j / sum_j exp(s_j),   s_j = scale q . k_j + beta_j
+ * over the entries j < lens[s] of present pages (cache->beta NULL: beta = 0).
+ * With causal = 1, query i sits at entry lens[s] - n_queries + i and sees
+ * entries up to that one.  A query that sees nothing gets zeros (a padded batch
+ * row has length 0).  A NaN or an infinity in an entry that some query of the
+ * call sees may reach the other queries of its sequence and KV head; one that
+ * no query sees reaches none. */
+typedef struct {
+  int32_t group;        /* query heads per KV head, >= 1                                    */
+  int32_t n_queries;    /* queries per sequence and query head; group * n_queries <= 32     */
+  int32_t causal;       /* 0 or 1                                                           */
+  float scale;          /* logit scale; 0 -> 1/sqrt(d)                                      */
+  double rope_theta;    /* > 0: rotate q at q_positions; 0: q used as given                 */
+  int64_t q_stride;     /* elements between tokens of q, a multiple of 16 bytes;
+                           0 -> H * group * d                                               */
+} still_paged_attend_config;
+
+/* Bytes of device workspace that serve still_paged_attend at this group,
+ * n_queries, head count and head_dim, whatever the sequences and their lengths
+ * (0: invalid configuration).  Never above STILL_PAGED_WORKSPACE_BYTES. */
+enum { STILL_PAGED_WORKSPACE_BYTES = 72 << 20 };
+size_t still_paged_attend_workspace_size(const still_paged_cache *cache, const still_paged_attend_config *cfg);
+
+/*   q            [n_seqs * n_queries] tokens, sequence by sequence, of [H*group][d]
+ *   q_positions  [n_seqs * n_queries] float64 (required iff rope_theta > 0)
+ *   out          [n_seqs * n_queries][H*group][d]
+ * (query head h * group + g uses KV head h; device pointers, 16-byte aligned). */
+still_status still_paged_attend(const still_paged_cache *cache, const still_paged_seqs *seqs,
+                                const still_paged_attend_config *cfg, const void *q, const double *q_positions,
+                                void *out, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Human-readable name of a status code (static string). */
 const char *still_status_string(int32_t status);
 
@@ -325,8 +424,9 @@ enum {
   STILL_K_QPROJ = 2,        /* cross-attention query projection               */
   STILL_K_REFINE = 3,       /* exact-logit refinement of the top keys         */
   STILL_K_LATENT = 4,       /* latent-side GEMMs (V/O proj, self-attn, FFN, heads) */
-  STILL_K_OTHER = 5,        /* norms, softmax, merge, tables, conversions, beta */
-  STILL_K_ATTEND = 6,       /* still_attend: consumer attention and its merge  */
+  STILL_K_OTHER = 5,        /* norms, softmax, merge, tables, conversions, beta,
+                               paged append and gather                         */
+  STILL_K_ATTEND = 6,       /* consumer attention (dense and paged), its merge   */
   STILL_K_STAGE = 7,        /* RoPE-fix staging of X, X^T: the KV-cache stream */
   STILL_K_COUNT = 8
 };

@@ -65,6 +65,31 @@ class still_attend_config(ctypes.Structure):
                 ("rope_theta", ctypes.c_double)]
 
 
+class still_paged_cache(ctypes.Structure):
+    _fields_ = [("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("mode", ctypes.c_int32), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("beta", ctypes.c_void_p)]
+
+
+class still_paged_seqs(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("table_stride", ctypes.c_int32),
+                ("table", ctypes.c_void_p), ("lens", ctypes.c_void_p)]
+
+
+class still_paged_tokens(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_int32), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_token_stride", ctypes.c_int64), ("k_head_stride", ctypes.c_int64),
+                ("v_token_stride", ctypes.c_int64), ("v_head_stride", ctypes.c_int64),
+                ("beta", ctypes.c_void_p), ("beta_token_stride", ctypes.c_int64),
+                ("beta_head_stride", ctypes.c_int64), ("offsets", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("rope_theta", ctypes.c_double)]
+
+
+class still_paged_attend_config(ctypes.Structure):
+    _fields_ = [("group", ctypes.c_int32), ("n_queries", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("rope_theta", ctypes.c_double), ("q_stride", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -113,6 +138,16 @@ def lib():
         L.still_compact_layer_backward.restype = ctypes.c_int32
         L.still_attend_scratch.argtypes = [ctypes.POINTER(still_attend_config), *[ctypes.c_void_p] * 9]
         L.still_attend_scratch.restype = ctypes.c_int32
+        cache, seqs = ctypes.POINTER(still_paged_cache), ctypes.POINTER(still_paged_seqs)
+        L.still_paged_append.argtypes = [cache, seqs, ctypes.POINTER(still_paged_tokens), ctypes.c_void_p]
+        L.still_paged_append.restype = ctypes.c_int32
+        L.still_paged_gather.argtypes = [cache, seqs, *[ctypes.c_int32] * 3, *[ctypes.c_void_p] * 4]
+        L.still_paged_gather.restype = ctypes.c_int32
+        L.still_paged_attend_workspace_size.argtypes = [cache, ctypes.POINTER(still_paged_attend_config)]
+        L.still_paged_attend_workspace_size.restype = ctypes.c_size_t
+        L.still_paged_attend.argtypes = [cache, seqs, ctypes.POINTER(still_paged_attend_config),
+                                         *[ctypes.c_void_p] * 4, ctypes.c_size_t, ctypes.c_void_p]
+        L.still_paged_attend.restype = ctypes.c_int32
         L.still_status_string.argtypes = [ctypes.c_int32]
         L.still_status_string.restype = ctypes.c_char_p
         L.still_last_error.argtypes = []
@@ -220,6 +255,32 @@ def still_attend_scratch(cfg: still_attend_config, q, q_positions, C_k, C_v, bet
 
 
 STILL_ATTEND_SCRATCH_BYTES = 68 << 20
+
+
+def still_paged_append(cache: still_paged_cache, seqs: still_paged_seqs, tokens: still_paged_tokens, stream) -> int:
+    """Raw entry point; returns the status code."""
+    return lib().still_paged_append(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(tokens), _ptr(stream))
+
+
+def still_paged_gather(cache: still_paged_cache, seqs: still_paged_seqs, seq: int, start: int, n: int, K, V, beta,
+                       stream) -> int:
+    """Raw entry point (pointers or tensors); returns the status code."""
+    return lib().still_paged_gather(ctypes.byref(cache), ctypes.byref(seqs), seq, start, n, _ptr(K), _ptr(V),
+                                    _ptr(beta), _ptr(stream))
+
+
+def still_paged_attend_workspace_size(cache: still_paged_cache, cfg: still_paged_attend_config) -> int:
+    return int(lib().still_paged_attend_workspace_size(ctypes.byref(cache), ctypes.byref(cfg)))
+
+
+def still_paged_attend(cache: still_paged_cache, seqs: still_paged_seqs, cfg: still_paged_attend_config, q,
+                       q_positions, out, workspace, workspace_bytes: int, stream) -> int:
+    """Raw entry point (pointers or tensors); returns the status code."""
+    return lib().still_paged_attend(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(cfg), _ptr(q),
+                                    _ptr(q_positions), _ptr(out), _ptr(workspace), workspace_bytes, _ptr(stream))
+
+
+STILL_PAGED_WORKSPACE_BYTES = 72 << 20
 
 
 def still_status_string(status: int) -> str:
@@ -449,3 +510,227 @@ def attend(q, C_k, C_v, beta, K, V, group: int = 1, causal: bool = False, scale:
     stream = torch.cuda.current_stream(q.device).cuda_stream
     _check(still_attend(acfg, q, q_positions, C_k, C_v, beta, K, V, out, workspace, workspace.numel(), stream))
     return out
+
+
+# ----------------------------------------------------------------------------
+# Paged cache
+# ----------------------------------------------------------------------------
+
+def _refuse(status: int, detail: str):
+    raise StillError(status, detail)
+
+
+def _want(x, name: str, dtype, shape, dev) -> None:
+    """x is a contiguous tensor of this type and shape on dev."""
+    if x.dtype != dtype:
+        _refuse(-3, f"{name} is {x.dtype}, not {dtype}")
+    if tuple(x.shape) != shape:
+        _refuse(-2, f"{name} has shape {tuple(x.shape)}, not {shape}")
+    if not x.is_contiguous():
+        _refuse(-1, f"{name} is not contiguous")
+    if x.device != dev:
+        _refuse(-1, f"{name} is on {x.device}, not {dev}")
+
+
+def _want_rows(x, name: str, pages, shape) -> None:
+    """x is a tensor of the pages' type with this shape and whole rows, on their device."""
+    if x.dtype != pages.dtype:
+        _refuse(-3, f"{name} is {x.dtype}, the pages {pages.dtype}")
+    if tuple(x.shape) != shape:
+        _refuse(-2, f"{name} has shape {tuple(x.shape)}, not {shape}")
+    if x.stride(2) != 1:
+        _refuse(-1, f"{name}'s rows are not contiguous")
+    if x.device != pages.device:
+        _refuse(-1, f"{name} is on {x.device}, not {pages.device}")
+
+
+def _paged(k_pages, v_pages, beta_pages, table, lens):
+    """The C views of a paged cache and its sequences, checked."""
+    torch = _torch()
+    if k_pages.dim() != 4:
+        _refuse(-2, f"k_pages has {k_pages.dim()} dimensions, not [n_pages, H, page_size, d]")
+    dt, dev = k_pages.dtype, k_pages.device
+    if dt != torch.bfloat16 and dt != torch.float32:
+        _refuse(-3, f"pages of {dt}: bfloat16 and float32 are supported")
+    shape = tuple(k_pages.shape)
+    n_pages, H, P, d = shape
+    _want(k_pages, "k_pages", dt, shape, dev)
+    _want(v_pages, "v_pages", dt, shape, dev)
+    if beta_pages is not None:
+        _want(beta_pages, "beta_pages", torch.float32, shape[:3], dev)
+    if table.dim() != 2 or table.dtype != torch.int32 or (table.stride(1) != 1 and table.shape[1] > 1):
+        _refuse(-2, "table is no int32 tensor [n_seqs, pages] with contiguous rows")
+    if table.device != dev:
+        _refuse(-1, f"table is on {table.device}, not {dev}")
+    n, width = table.shape
+    _want(lens, "lens", torch.int32, (n,), dev)
+    if dev.type != "cuda":
+        _refuse(-1, f"the pages are on {dev}: a GPU is needed")
+    return (still_paged_cache(H, d, P, n_pages, configs.MODE_FP32 if dt == torch.float32 else configs.MODE_BF16,
+                              k_pages.data_ptr(), v_pages.data_ptr(), _ptr(beta_pages)),
+            still_paged_seqs(n, width, table.stride(0) if n > 1 else width, table.data_ptr(), lens.data_ptr()))
+
+
+def _on(dev, call, *args):
+    """call(*args, current stream of dev) with dev current."""
+    torch = _torch()
+    if torch.cuda.current_device() == dev.index:
+        return call(*args, torch.cuda.current_stream(dev).cuda_stream)
+    with torch.cuda.device(dev):
+        return call(*args, torch.cuda.current_stream(dev).cuda_stream)
+
+
+def paged_append(k, v, k_pages, v_pages, table, lens, offsets=None, positions=None, rope_theta: float = 0.0,
+                 beta=None, beta_pages=None) -> None:
+    """Append rows k, v [n_tokens, H, d] to the pages [n_pages, H, P, d] of
+    their sequences on the current stream (still_paged_append).  table
+    [n_seqs, pages] and lens [n_seqs] are int32 device tensors; lens counts the
+    new entries already.  Sequence s's tokens are offsets[s] .. offsets[s + 1] - 1
+    (int32 [n_seqs + 1]); without offsets every sequence has n_tokens / n_seqs.
+    With ``positions`` (float64 [n_tokens] logical positions) and
+    ``rope_theta`` the keys are rotated there first.  k and v may be strided
+    views with contiguous rows (slices of a fused projection, transposed [H, t, d]
+    outputs of the compactor).  A cache that keeps bias passes ``beta_pages``
+    [n_pages, H, P] float32 always, and the entries' ``beta`` [n_tokens, H]
+    float32 where it is not zero."""
+    torch = _torch()
+    cache, seqs = _paged(k_pages, v_pages, beta_pages, table, lens)
+    dev = k_pages.device
+    if k.dim() != 3:
+        _refuse(-2, f"k has {k.dim()} dimensions, not [n_tokens, H, d]")
+    n = int(k.shape[0])
+    shape = (n, cache.n_kv_heads, cache.head_dim)
+    _want_rows(k, "k", k_pages, shape)
+    _want_rows(v, "v", k_pages, shape)
+    if offsets is not None:
+        _want(offsets, "offsets", torch.int32, (seqs.n_seqs + 1,), dev)
+    if positions is not None:
+        _want(positions, "positions", torch.float64, (n,), dev)
+    ts = hs = 0
+    if beta is not None:
+        if beta.dtype != torch.float32 or tuple(beta.shape) != shape[:2] or beta.device != dev:
+            _refuse(-2, "beta is no float32 tensor [n_tokens, H] on the pages' device")
+        ts, hs = beta.stride()
+    tokens = still_paged_tokens(n, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), v.stride(0), v.stride(1),
+                                _ptr(beta), ts, hs, _ptr(offsets), _ptr(positions), float(rope_theta))
+    _check(_on(dev, still_paged_append, cache, seqs, tokens))
+
+
+def paged_gather(k_pages, v_pages, table, lens, seq: int, n: int, start: int = 0, beta_pages=None, out=None):
+    """Entries [start, start + n) of sequence ``seq`` as dense (K, V) [H, n, d],
+    with ``beta_pages`` (K, V, beta [H, n]), through still_paged_gather on the
+    current stream; into ``out`` (such a tuple) where given."""
+    torch = _torch()
+    cache, seqs = _paged(k_pages, v_pages, beta_pages, table, lens)
+    dev = k_pages.device
+    shape = (cache.n_kv_heads, int(n), cache.head_dim)
+    if out is None:
+        if n < 0:
+            _refuse(-2, f"{n} entries asked for")
+        out = (torch.empty(shape, dtype=k_pages.dtype, device=dev), torch.empty(shape, dtype=k_pages.dtype, device=dev))
+        if beta_pages is not None:
+            out += (torch.empty(shape[:2], dtype=torch.float32, device=dev),)
+    elif len(out) != (2 if beta_pages is None else 3):
+        _refuse(-2, "out holds K, V and, with beta_pages, beta")
+    else:
+        _want(out[0], "out[0]", k_pages.dtype, shape, dev)
+        _want(out[1], "out[1]", k_pages.dtype, shape, dev)
+        if beta_pages is not None:
+            _want(out[2], "out[2]", torch.float32, shape[:2], dev)
+    _check(_on(dev, still_paged_gather, cache, seqs, int(seq), int(start), int(n), out[0], out[1],
+               None if beta_pages is None else out[2]))
+    return out
+
+
+def paged_attend(q, k_pages, v_pages, table, lens, causal: bool = False, scale: float = 0.0, beta_pages=None,
+                 q_positions=None, rope_theta: float = 0.0, workspace=None, out=None):
+    """Attention of the newest tokens q [n_seqs * n_queries, H * group, d]
+    (sequence by sequence) over their sequences' pages through
+    still_paged_attend on the current stream; returns out, contiguous, like q.
+    q may be a strided view with contiguous tokens.  With ``q_positions``
+    (float64, one per token) and ``rope_theta`` the kernel rotates q first.
+    ``out`` and ``workspace`` (STILL_PAGED_WORKSPACE_BYTES serve every call)
+    may be given, so that the call allocates nothing (graph capture)."""
+    torch = _torch()
+    cache, seqs = _paged(k_pages, v_pages, beta_pages, table, lens)
+    dev = k_pages.device
+    if q.dim() != 3:
+        _refuse(-2, f"q has {q.dim()} dimensions, not [n_seqs * n_queries, H * group, d]")
+    tokens, Hq, d = q.shape
+    H, n = cache.n_kv_heads, seqs.n_seqs
+    if d != cache.head_dim or Hq < H or Hq % H or tokens < n or tokens % n:
+        _refuse(-2, f"q {tuple(q.shape)} does not fit {n} sequences and pages {tuple(k_pages.shape)}")
+    _want_rows(q, "q", k_pages, (tokens, Hq, d))
+    if q.stride(1) != d:
+        _refuse(-1, "q's tokens are not contiguous")
+    if q_positions is not None:
+        _want(q_positions, "q_positions", torch.float64, (tokens,), dev)
+    cfg = still_paged_attend_config(Hq // H, tokens // n, int(causal), float(scale), float(rope_theta),
+                                    q.stride(0) if tokens > 1 else 0)
+    if out is None:
+        out = torch.empty(tokens, Hq, d, dtype=q.dtype, device=dev)
+    else:
+        _want(out, "out", q.dtype, (tokens, Hq, d), dev)
+    if workspace is not None and workspace.device != dev:
+        _refuse(-1, f"workspace is on {workspace.device}, not {dev}")
+    if workspace is None or workspace.numel() < STILL_PAGED_WORKSPACE_BYTES:
+        need = still_paged_attend_workspace_size(cache, cfg)
+        if workspace is None or workspace.numel() < need:
+            workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+    _check(_on(dev, still_paged_attend, cache, seqs, cfg, q, q_positions, out, workspace, workspace.numel()))
+    return out
+
+
+def compact_paged(cfg: configs.CompactorConfig, weights: List[Dict[str, object]], k_pages: List, v_pages: List,
+                  table, lens, seq: int, n: int, positions, rope_theta: float, t: int, start: int = 0,
+                  end: Optional[int] = None, w_beta: Optional[List] = None, beta_pages: Optional[List] = None,
+                  beta_max: float = 0.0, mass_alpha: float = 0.0, log_x: float = 0.0, rerotate: bool = True):
+    """Compact entries [start, end) (default: all) of sequence ``seq``, which
+    holds n entries, to t inside its pages, layer by layer (lists of L layers'
+    weights and pages, one table): they are read out, compacted
+    (still_compact_layer, or still_compact_model_beta with ``w_beta``) and
+    written back behind the preserved prefix, and the entries behind them move
+    up with their bias.  ``positions`` [n] are the entries' float64 logical
+    positions.  Sets lens[seq] on the current stream and returns the new
+    positions [n - (end - start) + t]; pages behind the new length are free.
+    A cache that keeps bias passes ``beta_pages``; new entries without
+    ``w_beta`` get bias 0."""
+    torch = _torch()
+    end = n if end is None else end
+    if not (0 <= start < end <= n):
+        _refuse(-1, f"subrange [{start}, {end}) outside [0, {n})")
+    L = len(k_pages)
+    if len(v_pages) != L or len(weights) != L or any(x is not None and len(x) != L for x in (w_beta, beta_pages)):
+        _refuse(-2, "lists of different numbers of layers")
+    if w_beta is not None and beta_pages is None:
+        _refuse(-1, "w_beta given to a cache without beta")
+    length = n - (end - start) + t
+    if not 0 <= seq < table.shape[0]:
+        _refuse(-2, f"sequence {seq} outside [0, {table.shape[0]})")
+    if length > table.shape[1] * k_pages[0].shape[2]:
+        _refuse(-2, f"{length} entries do not fit the sequence's {table.shape[1]} pages")
+    _want(positions, "positions", torch.float64, (n,), k_pages[0].device)
+    dev, mode = k_pages[0].device, (configs.MODE_FP32 if k_pages[0].dtype == torch.float32 else configs.MODE_BF16)
+    row = table[seq:seq + 1]
+    to = [torch.full((1,), x, dtype=torch.int32, device=dev) for x in (start + t, length)]
+    inside = positions[start:end].contiguous()
+    ws = torch.empty(max(still_workspace_size(make_config(cfg, mode), end - start, t, 1), 1), dtype=torch.uint8,
+                     device=dev)                                     # shared by the layers (one stream)
+    for i in range(L):
+        bp = None if beta_pages is None else beta_pages[i]
+        K, V = paged_gather(k_pages[i], v_pages[i], table, lens, seq, end - start, start)
+        rest = paged_gather(k_pages[i], v_pages[i], table, lens, seq, n - end, end, beta_pages=bp)
+        beta = None
+        if w_beta is None:
+            Ck, Cv, pq = compact_layer(cfg, weights[i], K, V, inside, rope_theta, t, rerotate=rerotate, mode=mode,
+                                       workspace=ws)
+        else:
+            (Ck,), (Cv,), pq, (beta,) = compact_model_beta(cfg, [weights[i]], [K], [V], inside, rope_theta, t,
+                                                           [w_beta[i]], beta_max, mass_alpha, log_x, rerotate, mode, ws)
+            beta = beta.t()
+        paged_append(Ck.transpose(0, 1), Cv.transpose(0, 1), k_pages[i], v_pages[i], row, to[0], beta=beta,
+                     beta_pages=bp)
+        paged_append(rest[0].transpose(0, 1), rest[1].transpose(0, 1), k_pages[i], v_pages[i], row, to[1],
+                     beta=None if bp is None else rest[2].t(), beta_pages=bp)
+    lens[seq:seq + 1].fill_(length)
+    return torch.cat([positions[:start], pq, positions[end:]])

@@ -1,8 +1,8 @@
 """Build libstill.so (HIP, gfx950) in-tree with hipcc.
 
-The library is five translation units compiled in parallel (the C ABI and
+The library is six translation units compiled in parallel (the C ABI and
 the consumer attention; the fp16 attention kernels; the per-layer launch sequence for bf16 I/O; the same
-for the fp32 validation mode; the backward pass) and linked into one shared
+for the fp32 validation mode; the backward pass; the paged cache) and linked into one shared
 object."""
 from __future__ import annotations
 
@@ -16,10 +16,10 @@ ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libstill.so")
 CSRC = os.path.join(PKG, "csrc")
 SOURCES = [os.path.join(CSRC, f) for f in ("still.hip", "xattn.hip", "layer_bf16.hip", "layer_fp32.hip",
-                                            "backward.hip")]
+                                            "backward.hip", "paged.hip")]
 HEADERS = [os.path.join(CSRC, f) for f in ("common.hpp", "gemm.hpp", "attn.hpp", "misc.hpp", "kproj.hpp",
                                            "consumer.hpp", "refine.hpp", "refine64.hpp", "host.hpp",
-                                           "layer.hpp", "bwd.hpp")] + [os.path.join(ROOT, "include", "still.h")]
+                                           "layer.hpp", "bwd.hpp", "paged.hpp")] + [os.path.join(ROOT, "include", "still.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -1,0 +1,228 @@
+// paged.hip - C ABI (include/still.h) of the paged cache: argument validation
+// and launches of the kernels in paged.hpp.
+#include "host.hpp"
+#include "paged.hpp"
+
+namespace still {
+
+static still_status check_cache(const still_paged_cache* c) {
+  if (!c) return fail(STILL_E_INVAL, "paged cache is NULL");
+  if (c->mode != STILL_MODE_BF16 && c->mode != STILL_MODE_FP32) return fail(STILL_E_DTYPE, "unknown mode %d", c->mode);
+  if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256)
+    return fail(STILL_E_UNSUPPORTED, "paged head_dim %d not in {64, 128, 256}", c->head_dim);
+  if (c->n_kv_heads < 1 || c->n_pages < 1) return fail(STILL_E_SHAPE, "paged n_kv_heads and n_pages must be >= 1");
+  if (c->n_kv_heads > 65535) return fail(STILL_E_UNSUPPORTED, "n_kv_heads above 65535");
+  if (c->page_size < 16 || c->page_size > 4096 || (c->page_size & (c->page_size - 1)))
+    return fail(STILL_E_UNSUPPORTED, "page_size %d is no power of two from 16 to 4096", c->page_size);
+  return STILL_OK;
+}
+
+static still_status check_pages(const still_paged_cache* c) {
+  still_status s;
+  if ((s = check_ptr(c->k, "cache k", true)) != STILL_OK || (s = check_ptr(c->v, "cache v", true)) != STILL_OK) return s;
+  if ((uintptr_t)c->beta & 3u) return fail(STILL_E_INVAL, "cache beta is not 4-byte aligned");
+  return STILL_OK;
+}
+
+static still_status check_seqs(const still_paged_cache* c, const still_paged_seqs* q) {
+  if (!q) return fail(STILL_E_INVAL, "paged sequences are NULL");
+  if (q->n_seqs < 1 || q->max_pages < 1) return fail(STILL_E_SHAPE, "n_seqs and max_pages must be >= 1");
+  if (q->n_seqs > 65535) return fail(STILL_E_UNSUPPORTED, "n_seqs above 65535");
+  if ((long)q->max_pages * c->page_size > (1L << 30))
+    return fail(STILL_E_UNSUPPORTED, "max_pages * page_size above 2^30");
+  if (q->table_stride < q->max_pages) return fail(STILL_E_SHAPE, "table_stride %d below max_pages %d", q->table_stride,
+                                                  q->max_pages);
+  if (!q->table || !q->lens || ((uintptr_t)q->table & 3u) || ((uintptr_t)q->lens & 3u))
+    return fail(STILL_E_INVAL, "table or lens is NULL or not 4-byte aligned");
+  return STILL_OK;
+}
+
+static PagedArgs paged_args(const still_paged_cache* c, const still_paged_seqs* q) {
+  PagedArgs a;
+  a.k = (char*)c->k;
+  a.v = (char*)c->v;
+  a.beta = c->beta;
+  a.table = q->table;
+  a.lens = q->lens;
+  a.H = c->n_kv_heads;
+  a.lp = __builtin_ctz((unsigned)c->page_size);
+  a.n_pages = c->n_pages;
+  a.n_seqs = q->n_seqs;
+  a.max_pages = q->max_pages;
+  a.tstride = q->table_stride;
+  return a;
+}
+
+static still_status check_theta(double theta, const double* positions) {
+  if (!(theta >= 0.0) || !std::isfinite(theta)) return fail(STILL_E_INVAL, "rope_theta must be finite and >= 0");
+  if (theta > 0.0 && (!positions || ((uintptr_t)positions & 7u)))
+    return fail(STILL_E_INVAL, "rope_theta > 0 needs 8-byte aligned positions");
+  return STILL_OK;
+}
+
+// f(IT(), head_dim constant) for the cache's element type and head width
+template <class F>
+static void paged_dispatch(const still_paged_cache* c, F f) {
+  auto width = [&](auto it) {
+    switch (c->head_dim) {
+      case 64: f(it, std::integral_constant<int, 64>()); break;
+      case 128: f(it, std::integral_constant<int, 128>()); break;
+      default: f(it, std::integral_constant<int, 256>()); break;
+    }
+  };
+  if (c->mode == STILL_MODE_FP32) width(float());
+  else width(bf16());
+}
+
+static still_status check_attend(const still_paged_cache* c, const still_paged_attend_config* f) {
+  still_status s = check_cache(c);
+  if (s != STILL_OK) return s;
+  if (!f) return fail(STILL_E_INVAL, "paged attend config is NULL");
+  if (f->group < 1 || f->n_queries < 1) return fail(STILL_E_SHAPE, "group and n_queries must be >= 1");
+  if ((long)f->group * f->n_queries > ATTEND_MAX_ROWS)
+    return fail(STILL_E_UNSUPPORTED, "group * n_queries = %ld exceeds %d", (long)f->group * f->n_queries,
+                ATTEND_MAX_ROWS);
+  if (f->causal != 0 && f->causal != 1) return fail(STILL_E_INVAL, "causal must be 0 or 1");
+  if (!std::isfinite(f->scale) || f->scale < 0.f) return fail(STILL_E_INVAL, "scale must be finite and >= 0");
+  if (!(f->rope_theta >= 0.0) || !std::isfinite(f->rope_theta)) return fail(STILL_E_INVAL, "rope_theta must be >= 0");
+  return STILL_OK;
+}
+
+}  // namespace still
+
+using namespace still;
+
+extern "C" {
+
+still_status still_paged_append(const still_paged_cache* cache, const still_paged_seqs* seqs,
+                                const still_paged_tokens* t, void* stream) {
+  still_status s;
+  if ((s = check_cache(cache)) != STILL_OK || (s = check_seqs(cache, seqs)) != STILL_OK) return s;
+  if (!t) return fail(STILL_E_INVAL, "tokens are NULL");
+  if (t->n_tokens < 0) return fail(STILL_E_SHAPE, "n_tokens must be >= 0");
+  if (!t->offsets && t->n_tokens % seqs->n_seqs)
+    return fail(STILL_E_SHAPE, "%d tokens do not divide over %d sequences and no offsets are given", t->n_tokens,
+                seqs->n_seqs);
+  if ((uintptr_t)t->offsets & 3u) return fail(STILL_E_INVAL, "offsets are not 4-byte aligned");
+  const long esize = cache->mode == STILL_MODE_FP32 ? 4 : 2;
+  for (int64_t x : {t->k_token_stride, t->k_head_stride, t->v_token_stride, t->v_head_stride})
+    if (x * esize % 16) return fail(STILL_E_SHAPE, "row strides must be multiples of 16 bytes");
+  if (t->beta && !cache->beta) return fail(STILL_E_INVAL, "beta given to a cache without beta");
+  if ((uintptr_t)t->beta & 3u) return fail(STILL_E_INVAL, "beta is not 4-byte aligned");
+  if ((s = check_pages(cache)) != STILL_OK) return s;
+  if (t->n_tokens == 0) return STILL_OK;
+  if ((s = check_theta(t->rope_theta, t->positions)) != STILL_OK) return s;
+  if ((s = check_ptr(t->k, "k", true)) != STILL_OK || (s = check_ptr(t->v, "v", true)) != STILL_OK) return s;
+  PagedAppendArgs a;
+  a.c = paged_args(cache, seqs);
+  a.k = (const char*)t->k;
+  a.v = (const char*)t->v;
+  a.k_ts = t->k_token_stride * esize;
+  a.k_hs = t->k_head_stride * esize;
+  a.v_ts = t->v_token_stride * esize;
+  a.v_hs = t->v_head_stride * esize;
+  a.nbeta = t->beta;
+  a.b_ts = t->beta_token_stride;
+  a.b_hs = t->beta_head_stride;
+  a.offsets = t->offsets;
+  a.pos = t->rope_theta > 0.0 ? t->positions : nullptr;
+  a.log2_theta = t->rope_theta > 0.0 ? std::log2(t->rope_theta) : 0.0;
+  a.n_tokens = t->n_tokens;
+  a.per_seq = t->n_tokens / seqs->n_seqs;
+  hipStream_t st = (hipStream_t)stream;
+  (void)hipGetLastError();
+  TIMED(STILL_K_OTHER);
+  paged_dispatch(cache, [&](auto it, auto d) {
+    using IT = decltype(it);
+    const unsigned blocks = ((unsigned)t->n_tokens + PAGED_APPEND_TPB - 1) / PAGED_APPEND_TPB;
+    hipLaunchKernelGGL((paged_append_kernel<IT, decltype(d)::value, PAGED_APPEND_TPB>), dim3(blocks), dim3(256), 0, st,
+                       a);
+  });
+  HIP_TRY(hipGetLastError());
+  return STILL_OK;
+}
+
+still_status still_paged_gather(const still_paged_cache* cache, const still_paged_seqs* seqs, int32_t seq,
+                                int32_t start, int32_t n, void* K, void* V, float* beta, void* stream) {
+  still_status s;
+  if ((s = check_cache(cache)) != STILL_OK || (s = check_seqs(cache, seqs)) != STILL_OK) return s;
+  if (seq < 0 || seq >= seqs->n_seqs) return fail(STILL_E_SHAPE, "sequence %d outside [0, %d)", seq, seqs->n_seqs);
+  if (start < 0 || n < 0 || (long)start + n > (long)seqs->max_pages * cache->page_size)
+    return fail(STILL_E_SHAPE, "entries [%d, %ld) outside [0, %ld)", start, (long)start + n,
+                (long)seqs->max_pages * cache->page_size);
+  if (beta && !cache->beta) return fail(STILL_E_INVAL, "beta asked of a cache without beta");
+  if ((uintptr_t)beta & 3u) return fail(STILL_E_INVAL, "beta is not 4-byte aligned");
+  if ((s = check_pages(cache)) != STILL_OK) return s;
+  if (n == 0) return STILL_OK;
+  if ((s = check_ptr(K, "K", true)) != STILL_OK || (s = check_ptr(V, "V", true)) != STILL_OK) return s;
+  PagedGatherArgs a;
+  a.c = paged_args(cache, seqs);
+  a.K = (char*)K;
+  a.V = (char*)V;
+  a.beta = beta;
+  a.seq = seq;
+  a.start = start;
+  a.n = n;
+  hipStream_t st = (hipStream_t)stream;
+  (void)hipGetLastError();
+  TIMED(STILL_K_OTHER);
+  paged_dispatch(cache, [&](auto it, auto d) {
+    using IT = decltype(it);
+    const unsigned blocks = ((unsigned)n + PAGED_GATHER_ROWS - 1) / PAGED_GATHER_ROWS;
+    hipLaunchKernelGGL((paged_gather_kernel<IT, decltype(d)::value>), dim3(blocks, a.c.H), dim3(256), 0, st, a);
+  });
+  HIP_TRY(hipGetLastError());
+  return STILL_OK;
+}
+
+size_t still_paged_attend_workspace_size(const still_paged_cache* cache, const still_paged_attend_config* cfg) {
+  const std::string keep = g_last_error;
+  if (check_attend(cache, cfg) != STILL_OK) {
+    g_last_error = keep;
+    return 0;
+  }
+  return 256;
+}
+
+still_status still_paged_attend(const still_paged_cache* cache, const still_paged_seqs* seqs,
+                                const still_paged_attend_config* cfg, const void* q, const double* q_positions,
+                                void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  still_status s = check_attend(cache, cfg);
+  if (s != STILL_OK || (s = check_seqs(cache, seqs)) != STILL_OK) return s;
+  const long esize = cache->mode == STILL_MODE_FP32 ? 4 : 2;
+  const long q_row = (long)cache->n_kv_heads * cfg->group * cache->head_dim;
+  if (cfg->q_stride * esize % 16) return fail(STILL_E_SHAPE, "q_stride must be a multiple of 16 bytes");
+  if ((s = check_pages(cache)) != STILL_OK || (s = check_theta(cfg->rope_theta, q_positions)) != STILL_OK ||
+      (s = check_ptr(q, "q", true)) != STILL_OK || (s = check_ptr(out, "out", true)) != STILL_OK)
+    return s;
+  if (!workspace) return fail(STILL_E_WORKSPACE, "workspace is NULL");
+  const size_t need = still_paged_attend_workspace_size(cache, cfg);
+  if (workspace_bytes < need)
+    return fail(STILL_E_WORKSPACE, "workspace of %zu bytes, need %zu", workspace_bytes, need);
+  PagedAttendArgs a;
+  a.c = paged_args(cache, seqs);
+  a.q = (const char*)q;
+  a.q_ts = (cfg->q_stride ? cfg->q_stride : q_row) * esize;
+  a.out = (char*)out;
+  a.qpos = cfg->rope_theta > 0.0 ? q_positions : nullptr;
+  a.log2_theta = cfg->rope_theta > 0.0 ? std::log2(cfg->rope_theta) : 0.0;
+  a.group = cfg->group;
+  a.nq = cfg->n_queries;
+  a.causal = cfg->causal;
+  a.scale = cfg->scale != 0.f ? cfg->scale : 1.f / std::sqrt((float)cache->head_dim);
+  hipStream_t st = (hipStream_t)stream;
+  (void)hipGetLastError();
+  TIMED(STILL_K_ATTEND);
+  const int R = cfg->group * cfg->n_queries;
+  paged_dispatch(cache, [&](auto it, auto d) {
+    using IT = decltype(it);
+    constexpr int D = decltype(d)::value;
+    const dim3 grid(a.c.H, a.c.n_seqs), block(64 * PAGED_WAVES);
+    if (R <= 8) hipLaunchKernelGGL((paged_attend_kernel<IT, D, 8>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((paged_attend_kernel<IT, D, 32>), grid, block, 0, st, a);
+  });
+  HIP_TRY(hipGetLastError());
+  return STILL_OK;
+}
+
+}  // extern "C"
