@@ -326,7 +326,8 @@ typedef struct {
   int32_t n_pages;      /* pages in the pool, >= 1                                */
   int32_t mode;         /* still_mode: element type of k, v and of the rows given */
   void *k, *v;          /* [n_pages][H][page_size][d] (device, 16-byte aligned)   */
-  float *beta;          /* [n_pages][H][page_size]: the entries' bias; NULL: none */
+  float *beta;          /* [n_pages][H][page_size]: the entries' bias (16-byte
+                           aligned); NULL: none                                   */
 } still_paged_cache;
 
 typedef struct {

@@ -20,8 +20,7 @@ static still_status check_cache(const still_paged_cache* c) {
 static still_status check_pages(const still_paged_cache* c) {
   still_status s;
   if ((s = check_ptr(c->k, "cache k", true)) != STILL_OK || (s = check_ptr(c->v, "cache v", true)) != STILL_OK) return s;
-  if ((uintptr_t)c->beta & 3u) return fail(STILL_E_INVAL, "cache beta is not 4-byte aligned");
-  return STILL_OK;
+  return check_ptr(c->beta, "cache beta", false);
 }
 
 static still_status check_seqs(const still_paged_cache* c, const still_paged_seqs* q) {
@@ -86,6 +85,26 @@ static still_status check_attend(const still_paged_cache* c, const still_paged_a
   if (!std::isfinite(f->scale) || f->scale < 0.f) return fail(STILL_E_INVAL, "scale must be finite and >= 0");
   if (!(f->rope_theta >= 0.0) || !std::isfinite(f->rope_theta)) return fail(STILL_E_INVAL, "rope_theta must be >= 0");
   return STILL_OK;
+}
+
+// Workgroups per KV head: as many as are resident at once (one of 4 waves per
+// CU and per wave that a SIMD holds).
+constexpr int PAGED_BLOCKS = 512;
+
+struct PagedPlan {
+  int G;
+  size_t opart, mpart, lpart, total;   // offsets behind the plan, bytes
+};
+
+static PagedPlan paged_plan(const still_paged_cache* c, const still_paged_attend_config* f) {
+  PagedPlan p;
+  p.G = std::max(1, PAGED_BLOCKS / c->n_kv_heads);
+  const size_t slots = p.G == 1 ? 0 : (size_t)c->n_kv_heads * p.G * 2 * f->group * f->n_queries;   // one part: no joins
+  p.opart = (size_t)rup(p.G * (long)sizeof(int2), 256);
+  p.mpart = p.opart + slots * c->head_dim * sizeof(float);
+  p.lpart = p.mpart + (size_t)rup((long)(slots * sizeof(float)), 256);
+  p.total = p.lpart + (size_t)rup((long)(slots * sizeof(float)), 256) + 256;   // + alignment slack
+  return p;
 }
 
 }  // namespace still
@@ -181,7 +200,7 @@ size_t still_paged_attend_workspace_size(const still_paged_cache* cache, const s
     g_last_error = keep;
     return 0;
   }
-  return 256;
+  return paged_plan(cache, cfg).total;
 }
 
 still_status still_paged_attend(const still_paged_cache* cache, const still_paged_seqs* seqs,
@@ -196,9 +215,10 @@ still_status still_paged_attend(const still_paged_cache* cache, const still_page
       (s = check_ptr(q, "q", true)) != STILL_OK || (s = check_ptr(out, "out", true)) != STILL_OK)
     return s;
   if (!workspace) return fail(STILL_E_WORKSPACE, "workspace is NULL");
-  const size_t need = still_paged_attend_workspace_size(cache, cfg);
-  if (workspace_bytes < need)
-    return fail(STILL_E_WORKSPACE, "workspace of %zu bytes, need %zu", workspace_bytes, need);
+  const PagedPlan p = paged_plan(cache, cfg);
+  if (workspace_bytes < p.total)
+    return fail(STILL_E_WORKSPACE, "workspace of %zu bytes, need %zu", workspace_bytes, p.total);
+  char* ws = (char*)(((uintptr_t)workspace + 255) & ~(uintptr_t)255);
   PagedAttendArgs a;
   a.c = paged_args(cache, seqs);
   a.q = (const char*)q;
@@ -210,6 +230,11 @@ still_status still_paged_attend(const still_paged_cache* cache, const still_page
   a.nq = cfg->n_queries;
   a.causal = cfg->causal;
   a.scale = cfg->scale != 0.f ? cfg->scale : 1.f / std::sqrt((float)cache->head_dim);
+  a.G = p.G;
+  a.plan = (int2*)ws;
+  a.opart = (float*)(ws + p.opart);
+  a.mpart = (float*)(ws + p.mpart);
+  a.lpart = (float*)(ws + p.lpart);
   hipStream_t st = (hipStream_t)stream;
   (void)hipGetLastError();
   TIMED(STILL_K_ATTEND);
@@ -217,9 +242,12 @@ still_status still_paged_attend(const still_paged_cache* cache, const still_page
   paged_dispatch(cache, [&](auto it, auto d) {
     using IT = decltype(it);
     constexpr int D = decltype(d)::value;
-    const dim3 grid(a.c.H, a.c.n_seqs), block(64 * PAGED_WAVES);
-    if (R <= 8) hipLaunchKernelGGL((paged_attend_kernel<IT, D, 8>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((paged_attend_kernel<IT, D, 32>), grid, block, 0, st, a);
+    const dim3 grid(a.c.H, a.G), block(64 * PAGED_WAVES);
+    const size_t lds = paged_lds_bytes<IT, D>(R);
+    if (R <= 16) hipLaunchKernelGGL((paged_attend_kernel<IT, D, 1>), grid, block, lds, st, a);
+    else hipLaunchKernelGGL((paged_attend_kernel<IT, D, 2>), grid, block, lds, st, a);
+    if (a.G > 1)
+      hipLaunchKernelGGL((paged_merge_kernel<IT, D>), dim3(std::min(R, 8), a.c.H, a.G), dim3(256), 0, st, a);
   });
   HIP_TRY(hipGetLastError());
   return STILL_OK;

@@ -7,6 +7,8 @@
 // Page numbers and lengths are read on the device and may hold anything: every
 // address below is formed from a page number checked against n_pages.
 #pragma once
+#include <algorithm>
+
 #include "common.hpp"
 #include "consumer.hpp"
 
@@ -173,9 +175,30 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(PagedGatherArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Attention: a workgroup of 4 waves per (KV head, sequence).  Wave w takes
-// entries w, w + 4, ...; a lane holds D / 64 features of every query row's
-// running sum.  The waves' sums are joined in LDS.
+// Attention.  The entries of all sequences, cut into chunks of CH, form one line
+// per KV head; G workgroups per head take equal contiguous parts of it, so that
+// ragged lengths load the chip evenly and the host needs to know none of them.
+// A part may hold the end of one sequence, several whole ones and the start of
+// another.  A sequence that lies in one part is finished there; the others
+// leave partial sums (at most two per workgroup: the sequence it continues and
+// the one it starts), joined by paged_merge_kernel.
+//
+// Within a part, wave w of 4 takes chunks w, w + 4, ... of a sequence.
+//   S^T[entry][row]: entries are the matrix rows, query rows the columns, so a
+//   lane owns query row l = lane % 16 and its running maximum and sum stay in
+//   the lane.  Lane group lg = lane / 16 of entry l reads 16-byte pieces
+//   4 i + lg of its key: the pairing of contraction indices is free, so pieces
+//   feed the product as loaded, against the same pieces of the query row.
+//   O^T[feature][row]: register j of tile kt of S^T holds entry 16 kt + 4 lg + j.
+//   Lane l reads features [l D / 16, ..) of its lane group's entries, so value
+//   rows are read whole too, and output tile e holds features e, D / 16 + e, ...
+//   bf16: the lane's 8 entries are the 8 contraction indices of one
+//   v_mfma_f32_16x16x32_bf16; the 16-bit transposition is v_perm in the lane.
+//   Weights (and rotated queries) go in as two bf16 parts, hi + lo, 16 bits of
+//   mantissa: one part alone would round each by 2^-9.  fp32: one
+//   v_mfma_f32_16x16x4_f32 per entry.
+// Keys of the next chunk are loaded once the logits have used this one's, values
+// once P.V has: 32 bytes d of each wave are in flight throughout.
 // ---------------------------------------------------------------------------
 struct PagedAttendArgs {
   PagedArgs c;
@@ -186,99 +209,463 @@ struct PagedAttendArgs {
   double log2_theta;
   int group, nq, causal;
   float scale;
+  int G;               // workgroups per KV head
+  int2* plan;          // [G]: (sequence that starts in workgroup g and goes on, its last workgroup), or (-1, 0)
+  float* opart;        // [H][G][2][R][D]
+  float* mpart;        // [H][G][2][R]
+  float* lpart;
 };
 
 constexpr int PAGED_WAVES = 4;
+constexpr float LOG2E = 1.4426950408889634f;
 
-template <class IT, int D, int RB>
-__global__ __launch_bounds__(64 * PAGED_WAVES) void paged_attend_kernel(PagedAttendArgs a) {
-  constexpr int FPL = D / 64;
-  __shared__ float qs[RB][D];
-  __shared__ float acc[RB][D];
-  __shared__ float wm[PAGED_WAVES][RB], wl[PAGED_WAVES][RB];
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+template <class IT, int D>
+struct PagedTile {
+  static constexpr bool B16 = sizeof(IT) == 2;
+  static constexpr int NKT = B16 ? 2 : 1;               // 16-entry tiles per chunk
+  static constexpr int CH = 16 * NKT;
+  static constexpr int ROWB = D * (int)sizeof(IT);
+  static constexpr int NP = ROWB / 64;                  // 16-byte pieces of a key per lane
+  static constexpr int FPT = D / 16, VB = FPT * (int)sizeof(IT);
+  static constexpr int QROW = ROWB + 16;                // query rows in LDS (padded: 16 rows at one piece)
+  static constexpr int OROW = D + 4;
+};
+
+// entries per chunk, for the host
+inline int paged_chunk(bool fp32) { return fp32 ? PagedTile<float, 64>::CH : PagedTile<bf16, 64>::CH; }
+
+// dynamic LDS: the query rows (bf16: two parts), later the waves' sums [4][R][OROW]
+template <class IT, int D>
+inline size_t paged_lds_bytes(int R) {
+  using TL = PagedTile<IT, D>;
+  const size_t q = (size_t)(R <= 16 ? 16 : 32) * TL::QROW * (TL::B16 ? 2 : 1);
+  return std::max(q, (size_t)PAGED_WAVES * R * TL::OROW * sizeof(float));
+}
+
+// fast base-2 exponential (results below 2^-126 are zero)
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long uniform(long x) {
+  return (long)(((unsigned long)(unsigned)uniform((int)(x >> 32)) << 32) | (unsigned)uniform((int)x));
+}
+
+// This workgroup's part [c0, c1) of the T chunks: the sequence s that holds c0
+// and that sequence's first chunk.  The lengths are scanned by the block.
+struct PagedPart {
+  long T, c0, c1, at;   // at: first chunk of sequence s
+  int s, active;        // active: workgroups per head that have a part
+};
+
+template <int CH>
+__device__ __forceinline__ PagedPart paged_part(const PagedArgs& a, int g, int G) {
+  __shared__ long wsum[PAGED_WAVES];
+  __shared__ long found_at;
+  __shared__ int found;
+  constexpr int NT = 64 * PAGED_WAVES;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int h = blockIdx.x, s = blockIdx.y, R = a.group * a.nq, Hq = a.c.H * a.group;
-  const int len = paged_len(a.c, s);
-  // row g * nq + i: query i of head h * group + g
-  for (int e = tid; e < R * D; e += 64 * PAGED_WAVES) {
-    const int r = e / D, x = e % D, g = r / a.nq, i = r % a.nq;
-    const IT* q = (const IT*)(a.q + ((long)s * a.nq + i) * a.q_ts) + (long)(h * a.group + g) * D;
-    float f = to_f32(q[x]);
-    if (a.qpos) {
-      const int j = x % (D / 2);
-      const float2 c = rope_cs(a.qpos[(long)s * a.nq + i], exp2(a.log2_theta * (-2.0 * j / D)));
-      f = x < D / 2 ? f * c.x - to_f32(q[x + D / 2]) * c.y : f * c.x + to_f32(q[x - D / 2]) * c.y;
+  auto chunks = [&](int s) -> long { return s < a.n_seqs ? (paged_len(a, s) + CH - 1) / CH : 0; };
+  long mine = 0;
+  for (int s = tid; s < a.n_seqs; s += NT) mine += chunks(s);
+  long sum = mine;
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+  if (lane == 0) wsum[w] = sum;
+  __syncthreads();
+  PagedPart p;
+  p.T = 0;
+#pragma unroll
+  for (int i = 0; i < PAGED_WAVES; ++i) p.T += wsum[i];
+  p.T = uniform(p.T);
+  // a workgroup takes four chunks (one per wave) before another one starts
+  p.active = (int)min((long)G, (p.T + PAGED_WAVES - 1) / PAGED_WAVES);
+  p.c0 = p.c1 = p.at = 0;
+  p.s = 0;
+  if (g >= p.active) return p;
+  p.c0 = g * p.T / p.active;
+  p.c1 = (g + 1) * p.T / p.active;
+  long before = 0;   // chunks of the sequences before this round's
+  for (int base = 0; base < a.n_seqs; base += NT) {
+    __syncthreads();   // wsum of the round before has been read
+    const long n = base == 0 && a.n_seqs <= NT ? mine : chunks(base + tid);
+    long incl = n;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const long x = __shfl_up(incl, off);
+      if (lane >= off) incl += x;
     }
-    qs[r][x] = f;
-    acc[r][x] = 0.f;
+    if (lane == 63) wsum[w] = incl;
+    __syncthreads();
+    long first = before + incl - n, total = 0;
+#pragma unroll
+    for (int i = 0; i < PAGED_WAVES; ++i) {
+      if (i < w) first += wsum[i];
+      total += wsum[i];
+    }
+    if (first <= p.c0 && p.c0 < first + n) {   // one thread of one round
+      found = base + tid;
+      found_at = first;
+    }
+    before += total;
+    if (before > p.c0) break;
   }
   __syncthreads();
-  float m[RB], l[RB], o[RB][FPL];
+  p.s = uniform(found);
+  p.at = uniform(found_at);
+  return p;
+}
+
+template <class IT, int D, int NR>
+__global__ __launch_bounds__(64 * PAGED_WAVES, D * NR <= 128 ? 2 : 1) void paged_attend_kernel(PagedAttendArgs a) {
+  using TL = PagedTile<IT, D>;
+  constexpr int NKT = TL::NKT, CH = TL::CH, NP = TL::NP, FPT = TL::FPT, VB = TL::VB, ROWB = TL::ROWB;
+  constexpr int QROW = TL::QROW, OROW = TL::OROW, NT = 64 * PAGED_WAVES, HD = D / 2;
+  extern __shared__ float4 paged_smem[];
+  char* qs = (char*)paged_smem;                  // [16 NR][QROW], bf16: the same again for the low parts
+  char* ql = qs + 16 * NR * QROW;
+  float* osum = (float*)paged_smem;              // [4][R][OROW]
+  __shared__ float wm[PAGED_WAVES][16 * NR], wl[PAGED_WAVES][16 * NR];
+  const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
+  const int l = lane & 15, lg = lane >> 4;
+  const int h = blockIdx.x, g = blockIdx.y, R = a.group * a.nq, Hq = a.c.H * a.group;
+  const bool rot = a.qpos != nullptr;
+  // rows of sequences without entries
+  for (int s = g; s < a.c.n_seqs; s += a.G)
+    if (a.c.lens[s] <= 0)
+      for (int e = tid; e < R * (ROWB / 16); e += NT) {
+        const int r = e / (ROWB / 16), x = e % (ROWB / 16);
+        const u32x4 z = {0, 0, 0, 0};
+        ((u32x4*)(a.out + (((long)s * a.nq + r % a.nq) * Hq + h * a.group + r / a.nq) * ROWB))[x] = z;
+      }
+  const PagedPart part = paged_part<CH>(a.c, g, a.G);
+  int2 goes_on = make_int2(-1, 0);
+  long at = part.at, left = part.c1 - part.c0;
+  int f0 = (int)(part.c0 - part.at);
+  const int koff = l * ROWB + lg * 16, voff = 4 * lg * ROWB + l * VB;
+  for (int s = part.s; left > 0 && s < a.c.n_seqs; ++s, f0 = 0) {
+    const int len = uniform(paged_len(a.c, s)), ns = (len + CH - 1) / CH;
+    const int f1 = (int)min((long)ns, f0 + left);
+    left -= f1 - f0;
+    at += ns;
+    if (f0 >= f1) continue;
+    // ---- chunks: where their 16-entry tiles lie, how many entries of each count
+    struct Chunk {
+      long row[NKT];
+      int nv[NKT];
+    };
+    auto lookup = [&](int c) {
+      Chunk k;
 #pragma unroll
-  for (int r = 0; r < RB; ++r) {
-    m[r] = -INFINITY;
-    l[r] = 0.f;
+      for (int kt = 0; kt < NKT; ++kt) {
+        const long j = (long)c * CH + 16 * kt;
+        const int p = uniform(j < len ? paged_page(a.c, s, j) : -1);
+        k.nv[kt] = p < 0 ? 0 : min(16, (int)(len - j));
+        k.row[kt] = (((long)max(p, 0) * a.c.H + h) << a.c.lp) + (p < 0 ? 0 : j & ((1 << a.c.lp) - 1));
+      }
+      return k;
+    };
+    u32x4 kp[NKT][NP];
+    float4 bias[NKT];
+    uint32_t vr[NKT * 4][VB / 4];
+    auto load_k = [&](const Chunk& k) {
 #pragma unroll
-    for (int u = 0; u < FPL; ++u) o[r][u] = 0.f;
-  }
-  for (int j = w; j < len; j += PAGED_WAVES) {
-    const int page = paged_page(a.c, s, j);
-    if (page < 0) continue;
-    const long at = paged_row(a.c, page, h, j);
-    float kf[FPL], vf[FPL];
+      for (int kt = 0; kt < NKT; ++kt) {
+        const char* base = a.c.k + k.row[kt] * ROWB;
 #pragma unroll
-    for (int u = 0; u < FPL; ++u) {
-      kf[u] = to_f32(((const IT*)a.c.k)[at * D + u * 64 + lane]);
-      vf[u] = to_f32(((const IT*)a.c.v)[at * D + u * 64 + lane]);
-    }
-    const float bias = a.c.beta ? a.c.beta[at] : 0.f;
+        for (int i = 0; i < NP; ++i) kp[kt][i] = *(const u32x4*)(base + koff + 64 * i);
+        bias[kt] = a.c.beta ? *(const float4*)(a.c.beta + k.row[kt] + 4 * lg) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+    };
+    auto load_v = [&](const Chunk& k) {
 #pragma unroll
-    for (int r = 0; r < RB; ++r) {
-      if (r >= R) continue;
-      float d = 0.f;
+      for (int kt = 0; kt < NKT; ++kt) {
+        const char* base = a.c.v + k.row[kt] * ROWB;
 #pragma unroll
-      for (int u = 0; u < FPL; ++u) d += qs[r][u * 64 + lane] * kf[u];
-      d = group_sum<64>(d);
-      const int last = a.causal ? len - a.nq + r % a.nq : len - 1;
-      if (j > last) continue;
-      const float x = d * a.scale + bias, mn = fmaxf(m[r], x);
-      const float ref = mn == -INFINITY ? 0.f : mn;
-      const float al = expf(m[r] - ref), p = expf(x - ref);
-      m[r] = mn;
-      l[r] = l[r] * al + p;
-#pragma unroll
-      for (int u = 0; u < FPL; ++u) o[r][u] = o[r][u] * al + p * vf[u];
-    }
-  }
-#pragma unroll
-  for (int r = 0; r < RB; ++r)
-    if (lane == 0) {
-      wm[w][r] = m[r];
-      wl[w][r] = l[r];
-    }
-  __syncthreads();
-  for (int x = 0; x < PAGED_WAVES; ++x) {
-    if (w == x) {
-#pragma unroll
-      for (int r = 0; r < RB; ++r) {
-        float M = wm[0][r];
-#pragma unroll
-        for (int y = 1; y < PAGED_WAVES; ++y) M = fmaxf(M, wm[y][r]);
-        const float sc = expf(m[r] - (M == -INFINITY ? 0.f : M));
-#pragma unroll
-        for (int u = 0; u < FPL; ++u)
-          if (r < R) acc[r][u * 64 + lane] += o[r][u] * sc;
+        for (int j = 0; j < 4; ++j) load_words<VB>(base + voff + j * ROWB, vr[kt * 4 + j]);
+      }
+    };
+    Chunk cur = lookup(min(f0 + w, f1 - 1));
+    load_k(cur);
+    load_v(cur);
+    // ---- query rows into LDS: row g * nq + i is query i of head h * group + g
+    for (int e = tid; e < 16 * NR * HD; e += NT) {
+      const int r = e / HD, j = e % HD;
+      float x0 = 0.f, x1 = 0.f;
+      if (r < R) {
+        const long t = (long)s * a.nq + r % a.nq;
+        const IT* q = (const IT*)(a.q + t * a.q_ts) + (long)(h * a.group + r / a.nq) * D;
+        x0 = to_f32(q[j]);
+        x1 = to_f32(q[j + HD]);
+        if (rot) {
+          const float2 cs = rope_cs(a.qpos[t], exp2(a.log2_theta * (-2.0 * j / D)));
+          const float y0 = x0 * cs.x - x1 * cs.y;
+          x1 = x1 * cs.x + x0 * cs.y;
+          x0 = y0;
+        }
+      }
+      if constexpr (TL::B16) {
+        const __bf16 h0 = (__bf16)x0, h1 = (__bf16)x1;
+        ((__bf16*)(qs + r * QROW))[j] = h0;
+        ((__bf16*)(qs + r * QROW))[j + HD] = h1;
+        if (rot) {
+          ((__bf16*)(ql + r * QROW))[j] = (__bf16)(x0 - (float)h0);
+          ((__bf16*)(ql + r * QROW))[j + HD] = (__bf16)(x1 - (float)h1);
+        }
+      } else {
+        ((float*)(qs + r * QROW))[j] = x0;
+        ((float*)(qs + r * QROW))[j + HD] = x1;
       }
     }
     __syncthreads();
+    f32x4 o[NR][FPT];
+    float m[NR], ls[NR];
+    int lim[NR];   // last entry that this lane's row sees
+#pragma unroll
+    for (int rt = 0; rt < NR; ++rt) {
+      m[rt] = -INFINITY;
+      ls[rt] = 0.f;
+      lim[rt] = a.causal ? len - a.nq + (16 * rt + l) % a.nq : len - 1;
+#pragma unroll
+      for (int e = 0; e < FPT; ++e) o[rt][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int open = a.causal ? len - a.nq : len - 1;   // entries up to this one are seen by every row
+    for (int c = f0 + w; c < f1; c += PAGED_WAVES) {
+      const bool more = c + PAGED_WAVES < f1;
+      Chunk nxt;
+      if (more) nxt = lookup(c + PAGED_WAVES);
+      // ---- logits
+      f32x4 x[NR][NKT];
+#pragma unroll
+      for (int rt = 0; rt < NR; ++rt)
+#pragma unroll
+        for (int kt = 0; kt < NKT; ++kt) x[rt][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) {
+          const int qoff = (16 * rt + l) * QROW + 64 * i + 16 * lg;
+          const u32x4 qv = *(const u32x4*)(qs + qoff);
+#pragma unroll
+          for (int kt = 0; kt < NKT; ++kt) {
+            if constexpr (TL::B16) {
+              x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kp[kt][i]),
+                                                                  __builtin_bit_cast(bf16x8, qv), x[rt][kt], 0, 0, 0);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kp[kt][i][e]), __uint_as_float(qv[e]),
+                                                                 x[rt][kt], 0, 0, 0);
+            }
+          }
+          if (TL::B16 && rot) {
+            const u32x4 qw = *(const u32x4*)(ql + qoff);
+#pragma unroll
+            for (int kt = 0; kt < NKT; ++kt)
+              x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kp[kt][i]),
+                                                                  __builtin_bit_cast(bf16x8, qw), x[rt][kt], 0, 0, 0);
+          }
+        }
+      float4 bc[NKT];
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt) bc[kt] = bias[kt];
+      if (more) load_k(nxt);
+      // ---- online softmax of this lane's rows over its entries
+      bool full = c * CH + CH - 1 <= open;
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt) full = full && cur.nv[kt] == 16;
+      if (!full) {   // values that no row sees may be anything: zeros in their place
+#pragma unroll
+        for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < VB / 4; ++e) vr[kt * 4 + j][e] = 4 * lg + j < cur.nv[kt] ? vr[kt * 4 + j][e] : 0u;
+      }
+#pragma unroll
+      for (int rt = 0; rt < NR; ++rt) {
+        float cm = -INFINITY;
+#pragma unroll
+        for (int kt = 0; kt < NKT; ++kt) {
+          const float bv[4] = {bc[kt].x, bc[kt].y, bc[kt].z, bc[kt].w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[rt][kt][j] = fmaf(x[rt][kt][j], a.scale, bv[j]);
+          if (!full) {
+            const int seen = min(cur.nv[kt], lim[rt] - (c * CH + 16 * kt) + 1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[rt][kt][j] = 4 * lg + j < seen ? x[rt][kt][j] : -INFINITY;
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) cm = fmaxf(cm, x[rt][kt][j]);
+        }
+        cm = fmaxf(cm, __shfl_xor(cm, 16));
+        cm = fmaxf(cm, __shfl_xor(cm, 32));
+        const float mn = fmaxf(m[rt], cm), ref = mn == -INFINITY ? 0.f : mn;
+        const float al = exp_of(m[rt] - ref);
+        m[rt] = mn;
+        float cs = 0.f;
+#pragma unroll
+        for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            x[rt][kt][j] = exp_of(x[rt][kt][j] - ref);
+            cs += x[rt][kt][j];
+          }
+        ls[rt] = ls[rt] * al + cs;   // (this lane's entries; its lane groups are added at the end)
+#pragma unroll
+        for (int e = 0; e < FPT; ++e) o[rt][e] *= al;
+      }
+      // ---- P.V
+      if constexpr (TL::B16) {
+        bf16x8 ph[NR], pl[NR];
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float p = x[rt][k >> 2][k & 3];
+            ph[rt][k] = (__bf16)p;
+            pl[rt][k] = (__bf16)(p - (float)ph[rt][k]);
+          }
+#pragma unroll
+        for (int e = 0; e < FPT; ++e) {
+          u32x4 t;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            t[k] = __builtin_amdgcn_perm(vr[2 * k + 1][e >> 1], vr[2 * k][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
+          const bf16x8 vt = __builtin_bit_cast(bf16x8, t);
+#pragma unroll
+          for (int rt = 0; rt < NR; ++rt) {
+            o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, ph[rt], o[rt][e], 0, 0, 0);
+            o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pl[rt], o[rt][e], 0, 0, 0);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int e = 0; e < FPT; ++e)
+#pragma unroll
+            for (int rt = 0; rt < NR; ++rt)
+              o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[j][e]), x[rt][0][j], o[rt][e], 0, 0, 0);
+      }
+      if (more) {
+        load_v(nxt);
+        cur = nxt;
+      }
+    }
+    // ---- the waves' sums into LDS, then added
+#pragma unroll
+    for (int rt = 0; rt < NR; ++rt) {
+      ls[rt] += __shfl_xor(ls[rt], 16);
+      ls[rt] += __shfl_xor(ls[rt], 32);
+    }
+    __syncthreads();   // every wave has read the query rows
+#pragma unroll
+    for (int rt = 0; rt < NR; ++rt) {
+      const int r = 16 * rt + l;
+      if (lg == 0) {
+        wm[w][r] = m[rt];
+        wl[w][r] = ls[rt];
+      }
+      if (r < R) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float* dst = osum + (w * R + r) * OROW + (4 * lg + j) * FPT;
+#pragma unroll
+          for (int e = 0; e < FPT; e += 4)
+            *(float4*)(dst + e) = make_float4(o[rt][e][j], o[rt][e + 1][j], o[rt][e + 2][j], o[rt][e + 3][j]);
+        }
+      }
+    }
+    __syncthreads();
+    const bool whole = f0 == 0 && f1 == ns;
+    const long slot = ((long)h * a.G + g) * 2 + (f0 == 0 ? 1 : 0);
+    for (int e = tid; e < R * (D / 4); e += NT) {
+      const int r = e / (D / 4), x = e % (D / 4) * 4;
+      float M = wm[0][r];
+#pragma unroll
+      for (int i = 1; i < PAGED_WAVES; ++i) M = fmaxf(M, wm[i][r]);
+      const float ref = M == -INFINITY ? 0.f : M;
+      float L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < PAGED_WAVES; ++i) {
+        const float sc = exp_of(wm[i][r] - ref);
+        const float4 y = *(const float4*)(osum + (i * R + r) * OROW + x);
+        L += sc * wl[i][r];
+        acc[0] += sc * y.x;
+        acc[1] += sc * y.y;
+        acc[2] += sc * y.z;
+        acc[3] += sc * y.w;
+      }
+      if (whole) {
+        const float inv = L == 0.f ? 0.f : 1.f / L;   // a row that sees nothing; a NaN stays one
+        IT* dst = (IT*)a.out + (((long)s * a.nq + r % a.nq) * Hq + h * a.group + r / a.nq) * D + x;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) dst[u] = from_f32<IT>(acc[u] * inv);
+      } else {
+        *(float4*)(a.opart + (slot * R + r) * D + x) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+        if (x == 0) {
+          a.mpart[slot * R + r] = M;
+          a.lpart[slot * R + r] = L;
+        }
+      }
+    }
+    if (f0 == 0 && f1 < ns) goes_on = make_int2(s, (int)((at * part.active - 1) / part.T));
+    __syncthreads();   // the sums have been read before the next sequence's query rows
   }
-  for (int e = tid; e < R * D; e += 64 * PAGED_WAVES) {
-    const int r = e / D, x = e % D, g = r / a.nq, i = r % a.nq;
-    float M = -INFINITY, L = 0.f;
-    for (int y = 0; y < PAGED_WAVES; ++y) M = fmaxf(M, wm[y][r]);
-    for (int y = 0; y < PAGED_WAVES; ++y) L += expf(wm[y][r] - (M == -INFINITY ? 0.f : M)) * wl[y][r];
-    const float f = L == 0.f ? 0.f : acc[r][x] / L;   // (a NaN stays one)
-    ((IT*)a.out)[(((long)s * a.nq + i) * Hq + h * a.group + g) * D + x] = from_f32<IT>(f);
+  if (h == 0 && tid == 0) a.plan[g] = goes_on;
+}
+
+// Joins the partial sums of the sequences that lie in several parts: block
+// (x, h, g) those of the sequence that starts in workgroup g, rows x, x + gridDim.x, ...
+template <class IT, int D>
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttendArgs a) {
+  constexpr int LPR = D / 4, NG = 256 / LPR;   // lanes per row, groups of parts
+  __shared__ float4 acc[NG][LPR];
+  __shared__ float sum[NG];
+  const int h = blockIdx.y, g = blockIdx.z, R = a.group * a.nq, Hq = a.c.H * a.group;
+  const int2 p = a.plan[g];
+  if (p.x < 0) return;
+  const int x = threadIdx.x % LPR, k = threadIdx.x / LPR, n = p.y - g + 1;
+  // part 0: the start, slot 1 of workgroup g; part i: slot 0 of workgroup g + i
+  auto slot = [&](int i) { return ((long)h * a.G + g + i) * 2 + (i == 0 ? 1 : 0); };
+  for (int r = blockIdx.x; r < R; r += gridDim.x) {
+    float M = -INFINITY;
+    for (int i = 0; i < n; ++i) M = fmaxf(M, a.mpart[slot(i) * R + r]);
+    const float ref = M == -INFINITY ? 0.f : M;
+    float L = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i = k; i < n; i += NG) {
+      const long at = slot(i) * R + r;
+      const float sc = exp_of(a.mpart[at] - ref);
+      const float4 v = *(const float4*)(a.opart + at * D + 4 * x);
+      L += sc * a.lpart[at];
+      y[0] += sc * v.x;
+      y[1] += sc * v.y;
+      y[2] += sc * v.z;
+      y[3] += sc * v.w;
+    }
+    acc[k][x] = make_float4(y[0], y[1], y[2], y[3]);
+    if (x == 0) sum[k] = L;
+    __syncthreads();
+    if (k == 0) {
+      float S = 0.f, z[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        const float4 v = acc[i][x];
+        S += sum[i];
+        z[0] += v.x;
+        z[1] += v.y;
+        z[2] += v.z;
+        z[3] += v.w;
+      }
+      const float inv = S == 0.f ? 0.f : 1.f / S;
+      IT* dst = (IT*)a.out + (((long)p.x * a.nq + r % a.nq) * Hq + h * a.group + r / a.nq) * D + 4 * x;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) dst[u] = from_f32<IT>(z[u] * inv);
+    }
+    __syncthreads();
   }
 }
 
