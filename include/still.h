@@ -333,7 +333,7 @@ typedef struct {
 typedef struct {
   int32_t n_seqs;       /* 1 .. 65535                                             */
   int32_t max_pages;    /* table entries per sequence that count, >= 1;
-                           max_pages * page_size <= 2^30                          */
+                           max_pages * page_size <= 2^30, times n_seqs <= 2^34    */
   int32_t table_stride; /* table entries between sequences, >= max_pages          */
   const int32_t *table; /* [n_seqs][table_stride] (device)                        */
   const int32_t *lens;  /* [n_seqs] (device)                                      */

@@ -29,6 +29,8 @@ static still_status check_seqs(const still_paged_cache* c, const still_paged_seq
   if (q->n_seqs > 65535) return fail(STILL_E_UNSUPPORTED, "n_seqs above 65535");
   if ((long)q->max_pages * c->page_size > (1L << 30))
     return fail(STILL_E_UNSUPPORTED, "max_pages * page_size above 2^30");
+  if ((long)q->n_seqs * q->max_pages * c->page_size > (1L << 34))
+    return fail(STILL_E_UNSUPPORTED, "n_seqs * max_pages * page_size above 2^34");
   if (q->table_stride < q->max_pages) return fail(STILL_E_SHAPE, "table_stride %d below max_pages %d", q->table_stride,
                                                   q->max_pages);
   if (!q->table || !q->lens || ((uintptr_t)q->table & 3u) || ((uintptr_t)q->lens & 3u))
@@ -87,10 +89,6 @@ static still_status check_attend(const still_paged_cache* c, const still_paged_a
   return STILL_OK;
 }
 
-// Workgroups per KV head: as many as are resident at once (one of 4 waves per
-// CU and per wave that a SIMD holds).
-constexpr int PAGED_BLOCKS = 512;
-
 struct PagedPlan {
   int G;
   size_t opart, mpart, lpart, total;   // offsets behind the plan, bytes
@@ -98,9 +96,10 @@ struct PagedPlan {
 
 static PagedPlan paged_plan(const still_paged_cache* c, const still_paged_attend_config* f) {
   PagedPlan p;
-  p.G = std::max(1, PAGED_BLOCKS / c->n_kv_heads);
+  // workgroups per KV head: as many as are resident at once
+  p.G = std::max(1, 256 * paged_resident(c->head_dim, f->group * f->n_queries <= 16 ? 1 : 2) / c->n_kv_heads);
   const size_t slots = p.G == 1 ? 0 : (size_t)c->n_kv_heads * p.G * 2 * f->group * f->n_queries;   // one part: no joins
-  p.opart = (size_t)rup(p.G * (long)sizeof(int2), 256);
+  p.opart = (size_t)rup(p.G * (long)sizeof(int4), 256);
   p.mpart = p.opart + slots * c->head_dim * sizeof(float);
   p.lpart = p.mpart + (size_t)rup((long)(slots * sizeof(float)), 256);
   p.total = p.lpart + (size_t)rup((long)(slots * sizeof(float)), 256) + 256;   // + alignment slack
@@ -231,7 +230,8 @@ still_status still_paged_attend(const still_paged_cache* cache, const still_page
   a.causal = cfg->causal;
   a.scale = cfg->scale != 0.f ? cfg->scale : 1.f / std::sqrt((float)cache->head_dim);
   a.G = p.G;
-  a.plan = (int2*)ws;
+  a.by_seq = seqs->n_seqs <= p.G;
+  a.plan = (int4*)ws;
   a.opart = (float*)(ws + p.opart);
   a.mpart = (float*)(ws + p.mpart);
   a.lpart = (float*)(ws + p.lpart);
@@ -247,7 +247,7 @@ still_status still_paged_attend(const still_paged_cache* cache, const still_page
     if (R <= 16) hipLaunchKernelGGL((paged_attend_kernel<IT, D, 1>), grid, block, lds, st, a);
     else hipLaunchKernelGGL((paged_attend_kernel<IT, D, 2>), grid, block, lds, st, a);
     if (a.G > 1)
-      hipLaunchKernelGGL((paged_merge_kernel<IT, D>), dim3(std::min(R, 8), a.c.H, a.G), dim3(256), 0, st, a);
+      hipLaunchKernelGGL((paged_merge_kernel<IT, D>), dim3(R, a.c.H, std::min(a.c.n_seqs, a.G)), dim3(256), 0, st, a);
   });
   HIP_TRY(hipGetLastError());
   return STILL_OK;

@@ -176,14 +176,17 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(PagedGatherArgs a) {
 
 // ---------------------------------------------------------------------------
 // Attention.  The entries of all sequences, cut into chunks of CH, form one line
-// per KV head; G workgroups per head take equal contiguous parts of it, so that
-// ragged lengths load the chip evenly and the host needs to know none of them.
-// A part may hold the end of one sequence, several whole ones and the start of
-// another.  A sequence that lies in one part is finished there; the others
-// leave partial sums (at most two per workgroup: the sequence it continues and
-// the one it starts), joined by paged_merge_kernel.
+// per KV head (a sequence counts PAGED_PAD chunks more, for what its rows cost
+// beside its entries); G workgroups per head take equal contiguous parts of it,
+// so that ragged lengths load the chip evenly and the host needs to know none
+// of them.  A part may hold the end of one sequence, several whole ones and the
+// start of another.  A sequence that lies in one part is finished there; the
+// others leave partial sums (at most two per workgroup: the sequence it
+// continues and the one it starts), joined by paged_merge_kernel.
 //
-// Within a part, wave w of 4 takes chunks w, w + 4, ... of a sequence.
+// Within a part, wave w of 4 takes chunks w, w + 4, ... of the part's, whichever
+// sequence they belong to, so that its loads run on from one sequence into the
+// next; the waves' sums are added where a sequence ends.
 //   S^T[entry][row]: entries are the matrix rows, query rows the columns, so a
 //   lane owns query row l = lane % 16 and its running maximum and sum stay in
 //   the lane.  Lane group lg = lane / 16 of entry l reads 16-byte pieces
@@ -198,7 +201,11 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(PagedGatherArgs a) {
 //   mantissa: one part alone would round each by 2^-9.  fp32: one
 //   v_mfma_f32_16x16x4_f32 per entry.
 // Keys of the next chunk are loaded once the logits have used this one's, values
-// once P.V has: 32 bytes d of each wave are in flight throughout.
+// once P.V has; page numbers are read two chunks ahead, before the keys of the
+// next one, so that they are there with them (loads return in order).  A tile is
+// read through a buffer descriptor of its valid rows: the others read as zeros
+// and cost nothing, so the loop has no branch and every load's wait counts only
+// the loads behind it.
 // ---------------------------------------------------------------------------
 struct PagedAttendArgs {
   PagedArgs c;
@@ -210,13 +217,16 @@ struct PagedAttendArgs {
   int group, nq, causal;
   float scale;
   int G;               // workgroups per KV head
-  int2* plan;          // [G]: (sequence that starts in workgroup g and goes on, its last workgroup), or (-1, 0)
+  int by_seq;          // plan entries are per sequence (n_seqs <= G), else per workgroup
+  int4* plan;          // (sequence in several parts or -1, its first and its last workgroup, 0)
   float* opart;        // [H][G][2][R][D]
   float* mpart;        // [H][G][2][R]
   float* lpart;
 };
 
 constexpr int PAGED_WAVES = 4;
+constexpr int PAGED_ROUND = 64 * PAGED_WAVES;   // sequences whose lengths a block holds at a time
+constexpr int PAGED_PAD = 2;
 constexpr float LOG2E = 1.4426950408889634f;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -232,440 +242,540 @@ struct PagedTile {
   static constexpr int FPT = D / 16, VB = FPT * (int)sizeof(IT);
   static constexpr int QROW = ROWB + 16;                // query rows in LDS (padded: 16 rows at one piece)
   static constexpr int OROW = D + 4;
+  static constexpr int QBYTES = 16 * QROW * (B16 ? 2 : 1);   // per 16 rows; bf16: two parts
 };
 
-// entries per chunk, for the host
-inline int paged_chunk(bool fp32) { return fp32 ? PagedTile<float, 64>::CH : PagedTile<bf16, 64>::CH; }
+// the waves' sums take the query rows' place in LDS where both do not fit 160 KB
+constexpr bool paged_alias(int D, int NR) { return D * NR > 256; }
 
-// dynamic LDS: the query rows (bf16: two parts), later the waves' sums [4][R][OROW]
+// workgroups resident on a CU (waves per SIMD): 16 rows of up to 128 features leave
+// 256 registers to two
+constexpr int paged_resident(int D, int NR) { return D * NR <= 128 ? 2 : 1; }
+
+// dynamic LDS: the query rows, the waves' sums [4][R][OROW]
 template <class IT, int D>
 inline size_t paged_lds_bytes(int R) {
   using TL = PagedTile<IT, D>;
-  const size_t q = (size_t)(R <= 16 ? 16 : 32) * TL::QROW * (TL::B16 ? 2 : 1);
-  return std::max(q, (size_t)PAGED_WAVES * R * TL::OROW * sizeof(float));
+  const int nr = R <= 16 ? 1 : 2;
+  const size_t q = (size_t)nr * TL::QBYTES, o = (size_t)PAGED_WAVES * R * TL::OROW * sizeof(float);
+  return paged_alias(D, nr) ? std::max(q, o) : q + o;
 }
 
 // fast base-2 exponential (results below 2^-126 are zero)
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ long uniform(long x) {
-  return (long)(((unsigned long)(unsigned)uniform((int)(x >> 32)) << 32) | (unsigned)uniform((int)x));
+
+// maximum over lanes l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ float groups_max(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// This workgroup's part [c0, c1) of the T chunks: the sequence s that holds c0
-// and that sequence's first chunk.  The lengths are scanned by the block.
-struct PagedPart {
-  long T, c0, c1, at;   // at: first chunk of sequence s
-  int s, active;        // active: workgroups per head that have a part
-};
-
-template <int CH>
-__device__ __forceinline__ PagedPart paged_part(const PagedArgs& a, int g, int G) {
-  __shared__ long wsum[PAGED_WAVES];
-  __shared__ long found_at;
-  __shared__ int found;
-  constexpr int NT = 64 * PAGED_WAVES;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  auto chunks = [&](int s) -> long { return s < a.n_seqs ? (paged_len(a, s) + CH - 1) / CH : 0; };
-  long mine = 0;
-  for (int s = tid; s < a.n_seqs; s += NT) mine += chunks(s);
-  long sum = mine;
+// B bytes (4, 8 or a multiple of 16) at byte off of a buffer into words
+template <int B>
+__device__ __forceinline__ void buffer_words(__amdgpu_buffer_rsrc_t r, int off, uint32_t (&w)[B / 4]) {
+  if constexpr (B == 4) {
+    w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0);
+  } else if constexpr (B == 8) {
+    const u32x2 u = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
+    w[0] = u.x;
+    w[1] = u.y;
+  } else {
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
-  if (lane == 0) wsum[w] = sum;
-  __syncthreads();
-  PagedPart p;
-  p.T = 0;
+    for (int i = 0; i < B / 16; ++i) {
+      const u32x4 u = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off + 16 * i, 0, 0));
 #pragma unroll
-  for (int i = 0; i < PAGED_WAVES; ++i) p.T += wsum[i];
-  p.T = uniform(p.T);
-  // a workgroup takes four chunks (one per wave) before another one starts
-  p.active = (int)min((long)G, (p.T + PAGED_WAVES - 1) / PAGED_WAVES);
-  p.c0 = p.c1 = p.at = 0;
-  p.s = 0;
-  if (g >= p.active) return p;
-  p.c0 = g * p.T / p.active;
-  p.c1 = (g + 1) * p.T / p.active;
-  long before = 0;   // chunks of the sequences before this round's
-  for (int base = 0; base < a.n_seqs; base += NT) {
-    __syncthreads();   // wsum of the round before has been read
-    const long n = base == 0 && a.n_seqs <= NT ? mine : chunks(base + tid);
-    long incl = n;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const long x = __shfl_up(incl, off);
-      if (lane >= off) incl += x;
+      for (int e = 0; e < 4; ++e) w[4 * i + e] = u[e];
     }
-    if (lane == 63) wsum[w] = incl;
-    __syncthreads();
-    long first = before + incl - n, total = 0;
-#pragma unroll
-    for (int i = 0; i < PAGED_WAVES; ++i) {
-      if (i < w) first += wsum[i];
-      total += wsum[i];
-    }
-    if (first <= p.c0 && p.c0 < first + n) {   // one thread of one round
-      found = base + tid;
-      found_at = first;
-    }
-    before += total;
-    if (before > p.c0) break;
   }
-  __syncthreads();
-  p.s = uniform(found);
-  p.at = uniform(found_at);
-  return p;
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t paged_rows(const void* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000);
 }
 
 template <class IT, int D, int NR>
-__global__ __launch_bounds__(64 * PAGED_WAVES, D * NR <= 128 ? 2 : 1) void paged_attend_kernel(PagedAttendArgs a) {
+__global__ __launch_bounds__(64 * PAGED_WAVES, paged_resident(D, NR)) void paged_attend_kernel(PagedAttendArgs a) {
   using TL = PagedTile<IT, D>;
   constexpr int NKT = TL::NKT, CH = TL::CH, NP = TL::NP, FPT = TL::FPT, VB = TL::VB, ROWB = TL::ROWB;
-  constexpr int QROW = TL::QROW, OROW = TL::OROW, NT = 64 * PAGED_WAVES, HD = D / 2;
+  constexpr int QROW = TL::QROW, OROW = TL::OROW, NT = 64 * PAGED_WAVES, HD = D / 2, NW = PAGED_WAVES;
+  constexpr bool ALIAS = paged_alias(D, NR);
   extern __shared__ float4 paged_smem[];
   char* qs = (char*)paged_smem;                  // [16 NR][QROW], bf16: the same again for the low parts
   char* ql = qs + 16 * NR * QROW;
-  float* osum = (float*)paged_smem;              // [4][R][OROW]
-  __shared__ float wm[PAGED_WAVES][16 * NR], wl[PAGED_WAVES][16 * NR];
+  float* osum = (float*)(qs + (ALIAS ? 0 : NR * TL::QBYTES));   // [4][R][OROW]
+  __shared__ float wm[NW][16 * NR], wl[NW][16 * NR];
+  __shared__ int wsum[NW], wcnt[NW], cut[2];
+  // a round's sequences: first chunk, length, non-empty ones before
+  __shared__ int first[PAGED_ROUND + 1], slen[PAGED_ROUND], before[PAGED_ROUND];
   const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
   const int l = lane & 15, lg = lane >> 4;
   const int h = blockIdx.x, g = blockIdx.y, R = a.group * a.nq, Hq = a.c.H * a.group;
+  const int n_seqs = a.c.n_seqs, pad = n_seqs > 1 ? PAGED_PAD : 0;
   const bool rot = a.qpos != nullptr;
-  // rows of sequences without entries
-  for (int s = g; s < a.c.n_seqs; s += a.G)
-    if (a.c.lens[s] <= 0)
-      for (int e = tid; e < R * (ROWB / 16); e += NT) {
-        const int r = e / (ROWB / 16), x = e % (ROWB / 16);
-        const u32x4 z = {0, 0, 0, 0};
-        ((u32x4*)(a.out + (((long)s * a.nq + r % a.nq) * Hq + h * a.group + r / a.nq) * ROWB))[x] = z;
-      }
-  const PagedPart part = paged_part<CH>(a.c, g, a.G);
-  int2 goes_on = make_int2(-1, 0);
-  long at = part.at, left = part.c1 - part.c0;
-  int f0 = (int)(part.c0 - part.at);
   const int koff = l * ROWB + lg * 16, voff = 4 * lg * ROWB + l * VB;
-  for (int s = part.s; left > 0 && s < a.c.n_seqs; ++s, f0 = 0) {
-    const int len = uniform(paged_len(a.c, s)), ns = (len + CH - 1) / CH;
-    const int f1 = (int)min((long)ns, f0 + left);
-    left -= f1 - f0;
-    at += ns;
-    if (f0 >= f1) continue;
-    // ---- chunks: where their 16-entry tiles lie, how many entries of each count
+  auto out_row = [&](int s, int r) { return (((long)s * a.nq + r % a.nq) * Hq + h * a.group + r / a.nq) * D; };
+
+  // ---- this workgroup's part of the line
+  int T = 0, TV = 0, active = 0, v0 = 0, v1 = 0;   // chunks, chunks with pads, workgroups with a part, the part's cuts
+  auto cuts = [&](int chunks, int seqs) {
+    T = chunks;
+    TV = chunks + pad * seqs;
+    active = min(a.G, (chunks + NW - 1) / NW);   // a workgroup takes a chunk per wave before another one starts
+    if (g < active) {
+      v0 = (int)((long)g * TV / active);
+      v1 = (int)((long)(g + 1) * TV / active);
+    }
+  };
+  auto length = [&](int s) { return s < n_seqs ? paged_len(a.c, s) : 0; };
+  auto totals = [&](int chunks, int seqs) {   // of the block; leaves the waves' in wsum, wcnt
+    if (lane == 63) {
+      wsum[w] = chunks;
+      wcnt[w] = seqs;
+    }
+    __syncthreads();
+    int2 t = make_int2(0, 0);
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      t.x += wsum[i];
+      t.y += wcnt[i];
+    }
+    return make_int2(uniform(t.x), uniform(t.y));
+  };
+  if (n_seqs > PAGED_ROUND) {
+    int n = 0, m = 0;
+    for (int s = tid; s < n_seqs; s += NT) {
+      const int c = (length(s) + CH - 1) / CH;
+      n += c;
+      m += c > 0;
+    }
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      n += __shfl_xor(n, off);
+      m += __shfl_xor(m, off);
+    }
+    const int2 t = totals(n, m);
+    cuts(t.x, t.y);
+    __syncthreads();
+  }
+  int goes_on[3] = {-1, 0, 0};
+  int line = 0, seqs = 0;   // chunks and non-empty sequences before this round
+  for (int base = 0; base < n_seqs; base += PAGED_ROUND) {
+    const int cnt = min(PAGED_ROUND, n_seqs - base);
+    int lo, hi;
+    {
+      const int len = length(base + tid), n = (len + CH - 1) / CH;
+      int incl = n;
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        const int x = __shfl_up(incl, off);
+        if (lane >= off) incl += x;
+      }
+      const unsigned long some = __ballot(n > 0);
+      const int2 t = totals(incl, __popcll(some));
+      if (n_seqs <= PAGED_ROUND) cuts(t.x, t.y);
+      int f = line + incl - n, b = seqs + __popcll(some & ((1UL << lane) - 1));
+#pragma unroll
+      for (int i = 0; i < NW; ++i)
+        if (i < w) {
+          f += wsum[i];
+          b += wcnt[i];
+        }
+      first[tid] = f;
+      slen[tid] = len;
+      before[tid] = b;
+      if (tid == 0) first[PAGED_ROUND] = line + t.x;
+      const int v = f + pad * b, p = n > 0 ? pad : 0;   // its place on the line with pads
+      if (n > 0 && v <= v0 && v0 < v + p + n) cut[0] = f + max(0, v0 - v - p);
+      if (n > 0 && v <= v1 && v1 < v + p + n) cut[1] = f + max(0, v1 - v - p);
+      __syncthreads();
+      const int vs = line + pad * seqs, ve = vs + t.x + pad * t.y;
+      lo = v0 <= vs ? line : v0 >= ve ? line + t.x : uniform(cut[0]);
+      hi = v1 <= vs ? line : v1 >= ve ? line + t.x : uniform(cut[1]);
+      line += t.x;
+      seqs += t.y;
+    }
+    // rows of sequences without entries
+    for (int k = g; k < cnt; k += a.G)
+      if (uniform(slen[k]) == 0) {
+        for (int e = tid; e < R * (ROWB / 16); e += NT) {
+          const u32x4 z = {0, 0, 0, 0};
+          ((u32x4*)(a.out + out_row(base + k, e / (ROWB / 16)) * (long)sizeof(IT)))[e % (ROWB / 16)] = z;
+        }
+        if (h == 0 && tid == 0 && a.by_seq) a.plan[base + k] = make_int4(-1, 0, 0, 0);
+      }
+    // ---- the stream of this wave's chunks.  Lane k holds the first chunks and
+    // lengths of sequences k, 64 + k, ... of the round.
+    int lfirst[NW], llen[NW];
+#pragma unroll
+    for (int k = 0; k < NW; ++k) {
+      lfirst[k] = first[64 * k + lane];
+      llen[k] = slen[64 * k + lane];
+    }
     struct Chunk {
-      long row[NKT];
-      int nv[NKT];
+      int i, c, len;    // sequence of the round (none: PAGED_ROUND), chunk in it, its length
+      int p[NKT];       // page numbers of its tiles, as read
     };
-    auto lookup = [&](int c) {
+    auto lookup = [&](int u) {   // chunk u of the line: the last sequence that starts at or before it
       Chunk k;
+      int li = -1, f = 0;
+#pragma unroll
+      for (int x = 0; x < NW; ++x) li += __popcll(__ballot(lfirst[x] <= u));
+      li = min(max(li, 0), cnt - 1);
+#pragma unroll
+      for (int x = 0; x < NW; ++x) {
+        const bool here = li >> 6 == x;
+        const int ff = __builtin_amdgcn_readlane(lfirst[x], li & 63), ll = __builtin_amdgcn_readlane(llen[x], li & 63);
+        f = here ? ff : f;
+        k.len = here || x == 0 ? ll : k.len;
+      }
+      const bool there = u < hi;
+      k.i = there ? li : PAGED_ROUND;
+      k.len = there ? k.len : 0;
+      k.c = u - f;
 #pragma unroll
       for (int kt = 0; kt < NKT; ++kt) {
-        const long j = (long)c * CH + 16 * kt;
-        const int p = uniform(j < len ? paged_page(a.c, s, j) : -1);
-        k.nv[kt] = p < 0 ? 0 : min(16, (int)(len - j));
-        k.row[kt] = (((long)max(p, 0) * a.c.H + h) << a.c.lp) + (p < 0 ? 0 : j & ((1 << a.c.lp) - 1));
+        const int j = max(min(k.c * CH + 16 * kt, k.len - 1), 0);
+        k.p[kt] = a.c.table[(base + li) * a.c.tstride + (j >> a.c.lp)];
       }
       return k;
     };
+    struct Tiles {
+      int i, c;
+      int nv[NKT];      // valid entries of each tile
+      long row[NKT];    // rows of the pages in front of the tile
+    };
+    auto resolve = [&](const Chunk& k) {
+      Tiles t;
+      t.i = k.i;
+      t.c = k.c;
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt) {
+        const int j = k.c * CH + 16 * kt, p = uniform(k.p[kt]);
+        const bool ok = j < k.len && (unsigned)p < (unsigned)a.c.n_pages;
+        t.nv[kt] = ok ? min(16, k.len - j) : 0;
+        t.row[kt] = (((long)(ok ? p : 0) * a.c.H + h) << a.c.lp) + (ok ? j & ((1 << a.c.lp) - 1) : 0);
+      }
+      return t;
+    };
     u32x4 kp[NKT][NP];
-    float4 bias[NKT];
+    f32x4 bias[NKT];
     uint32_t vr[NKT * 4][VB / 4];
-    auto load_k = [&](const Chunk& k) {
+    auto load_k = [&](const Tiles& k) {
 #pragma unroll
       for (int kt = 0; kt < NKT; ++kt) {
-        const char* base = a.c.k + k.row[kt] * ROWB;
+        const auto r = paged_rows(a.c.k + k.row[kt] * ROWB, k.nv[kt] * ROWB);
 #pragma unroll
-        for (int i = 0; i < NP; ++i) kp[kt][i] = *(const u32x4*)(base + koff + 64 * i);
-        bias[kt] = a.c.beta ? *(const float4*)(a.c.beta + k.row[kt] + 4 * lg) : make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i = 0; i < NP; ++i)
+          kp[kt][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, koff + 64 * i, 0, 0));
+        bias[kt] = __builtin_bit_cast(
+            f32x4, __builtin_amdgcn_raw_buffer_load_b128(paged_rows(a.c.beta + k.row[kt], a.c.beta ? k.nv[kt] * 4 : 0),
+                                                         16 * lg, 0, 0));
       }
     };
-    auto load_v = [&](const Chunk& k) {
+    auto load_v = [&](const Tiles& k) {
 #pragma unroll
       for (int kt = 0; kt < NKT; ++kt) {
-        const char* base = a.c.v + k.row[kt] * ROWB;
+        const auto r = paged_rows(a.c.v + k.row[kt] * ROWB, k.nv[kt] * ROWB);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) load_words<VB>(base + voff + j * ROWB, vr[kt * 4 + j]);
+        for (int j = 0; j < 4; ++j) buffer_words<VB>(r, voff + j * ROWB, vr[kt * 4 + j]);
       }
     };
-    Chunk cur = lookup(min(f0 + w, f1 - 1));
-    load_k(cur);
-    load_v(cur);
-    // ---- query rows into LDS: row g * nq + i is query i of head h * group + g
-    for (int e = tid; e < 16 * NR * HD; e += NT) {
-      const int r = e / HD, j = e % HD;
-      float x0 = 0.f, x1 = 0.f;
-      if (r < R) {
-        const long t = (long)s * a.nq + r % a.nq;
-        const IT* q = (const IT*)(a.q + t * a.q_ts) + (long)(h * a.group + r / a.nq) * D;
-        x0 = to_f32(q[j]);
-        x1 = to_f32(q[j + HD]);
-        if (rot) {
-          const float2 cs = rope_cs(a.qpos[t], exp2(a.log2_theta * (-2.0 * j / D)));
-          const float y0 = x0 * cs.x - x1 * cs.y;
-          x1 = x1 * cs.x + x0 * cs.y;
-          x0 = y0;
-        }
-      }
-      if constexpr (TL::B16) {
-        const __bf16 h0 = (__bf16)x0, h1 = (__bf16)x1;
-        ((__bf16*)(qs + r * QROW))[j] = h0;
-        ((__bf16*)(qs + r * QROW))[j + HD] = h1;
-        if (rot) {
-          ((__bf16*)(ql + r * QROW))[j] = (__bf16)(x0 - (float)h0);
-          ((__bf16*)(ql + r * QROW))[j + HD] = (__bf16)(x1 - (float)h1);
-        }
-      } else {
-        ((float*)(qs + r * QROW))[j] = x0;
-        ((float*)(qs + r * QROW))[j + HD] = x1;
-      }
-    }
-    __syncthreads();
-    f32x4 o[NR][FPT];
-    float m[NR], ls[NR];
-    int lim[NR];   // last entry that this lane's row sees
-#pragma unroll
-    for (int rt = 0; rt < NR; ++rt) {
-      m[rt] = -INFINITY;
-      ls[rt] = 0.f;
-      lim[rt] = a.causal ? len - a.nq + (16 * rt + l) % a.nq : len - 1;
-#pragma unroll
-      for (int e = 0; e < FPT; ++e) o[rt][e] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    const int open = a.causal ? len - a.nq : len - 1;   // entries up to this one are seen by every row
-    for (int c = f0 + w; c < f1; c += PAGED_WAVES) {
-      const bool more = c + PAGED_WAVES < f1;
-      Chunk nxt;
-      if (more) nxt = lookup(c + PAGED_WAVES);
-      // ---- logits
-      f32x4 x[NR][NKT];
-#pragma unroll
-      for (int rt = 0; rt < NR; ++rt)
-#pragma unroll
-        for (int kt = 0; kt < NKT; ++kt) x[rt][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < NP; ++i)
-#pragma unroll
-        for (int rt = 0; rt < NR; ++rt) {
-          const int qoff = (16 * rt + l) * QROW + 64 * i + 16 * lg;
-          const u32x4 qv = *(const u32x4*)(qs + qoff);
-#pragma unroll
-          for (int kt = 0; kt < NKT; ++kt) {
-            if constexpr (TL::B16) {
-              x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kp[kt][i]),
-                                                                  __builtin_bit_cast(bf16x8, qv), x[rt][kt], 0, 0, 0);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kp[kt][i][e]), __uint_as_float(qv[e]),
-                                                                 x[rt][kt], 0, 0, 0);
+    if (lo < hi) {
+      int u = lo + w;
+      Tiles cur = resolve(lookup(u));
+      Chunk nxt = lookup(u + NW);
+      load_k(cur);
+      __builtin_amdgcn_sched_barrier(0);   // (loads stay in this order: their waits count the ones behind)
+      load_v(cur);
+      __builtin_amdgcn_sched_barrier(0);
+      for (int i = 0, at = lo; at < hi; ++i) {
+        const int s0 = uniform(first[i]), s1 = uniform(first[i + 1]);
+        if (s1 <= at) continue;   // before the part, or empty
+        const int s = base + i, end = min(s1, hi), len = uniform(slen[i]);
+        // ---- query rows into LDS: row g * nq + i is query i of head h * group + g
+        for (int e = tid; e < 16 * NR * HD; e += NT) {
+          const int r = e / HD, j = e % HD;
+          float x0 = 0.f, x1 = 0.f;
+          if (r < R) {
+            const long t = (long)s * a.nq + r % a.nq;
+            const IT* q = (const IT*)(a.q + t * a.q_ts) + (long)(h * a.group + r / a.nq) * D;
+            x0 = to_f32(q[j]);
+            x1 = to_f32(q[j + HD]);
+            if (rot) {
+              const float2 cs = rope_cs(a.qpos[t], exp2(a.log2_theta * (-2.0 * j / D)));
+              const float y0 = x0 * cs.x - x1 * cs.y;
+              x1 = x1 * cs.x + x0 * cs.y;
+              x0 = y0;
             }
           }
-          if (TL::B16 && rot) {
-            const u32x4 qw = *(const u32x4*)(ql + qoff);
-#pragma unroll
-            for (int kt = 0; kt < NKT; ++kt)
-              x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kp[kt][i]),
-                                                                  __builtin_bit_cast(bf16x8, qw), x[rt][kt], 0, 0, 0);
+          if constexpr (TL::B16) {
+            const __bf16 h0 = (__bf16)x0, h1 = (__bf16)x1;
+            ((__bf16*)(qs + r * QROW))[j] = h0;
+            ((__bf16*)(qs + r * QROW))[j + HD] = h1;
+            ((__bf16*)(ql + r * QROW))[j] = (__bf16)(rot ? x0 - (float)h0 : 0.f);   // (as given: exact)
+            ((__bf16*)(ql + r * QROW))[j + HD] = (__bf16)(rot ? x1 - (float)h1 : 0.f);
+          } else {
+            ((float*)(qs + r * QROW))[j] = x0;
+            ((float*)(qs + r * QROW))[j + HD] = x1;
           }
         }
-      float4 bc[NKT];
+        __syncthreads();
+        f32x4 o[NR][FPT];
+        float m[NR], ls[NR];
+        int lim[NR];   // last entry that this lane's row sees
 #pragma unroll
-      for (int kt = 0; kt < NKT; ++kt) bc[kt] = bias[kt];
-      if (more) load_k(nxt);
-      // ---- online softmax of this lane's rows over its entries
-      bool full = c * CH + CH - 1 <= open;
+        for (int rt = 0; rt < NR; ++rt) {
+          m[rt] = -INFINITY;
+          ls[rt] = 0.f;
+          lim[rt] = a.causal ? len - a.nq + (16 * rt + l) % a.nq : len - 1;
 #pragma unroll
-      for (int kt = 0; kt < NKT; ++kt) full = full && cur.nv[kt] == 16;
-      if (!full) {   // values that no row sees may be anything: zeros in their place
-#pragma unroll
-        for (int kt = 0; kt < NKT; ++kt)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int e = 0; e < VB / 4; ++e) vr[kt * 4 + j][e] = 4 * lg + j < cur.nv[kt] ? vr[kt * 4 + j][e] : 0u;
-      }
-#pragma unroll
-      for (int rt = 0; rt < NR; ++rt) {
-        float cm = -INFINITY;
-#pragma unroll
-        for (int kt = 0; kt < NKT; ++kt) {
-          const float bv[4] = {bc[kt].x, bc[kt].y, bc[kt].z, bc[kt].w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[rt][kt][j] = fmaf(x[rt][kt][j], a.scale, bv[j]);
-          if (!full) {
-            const int seen = min(cur.nv[kt], lim[rt] - (c * CH + 16 * kt) + 1);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[rt][kt][j] = 4 * lg + j < seen ? x[rt][kt][j] : -INFINITY;
-          }
-#pragma unroll
-          for (int j = 0; j < 4; ++j) cm = fmaxf(cm, x[rt][kt][j]);
+          for (int e = 0; e < FPT; ++e) o[rt][e] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        cm = fmaxf(cm, __shfl_xor(cm, 16));
-        cm = fmaxf(cm, __shfl_xor(cm, 32));
-        const float mn = fmaxf(m[rt], cm), ref = mn == -INFINITY ? 0.f : mn;
-        const float al = exp_of(m[rt] - ref);
-        m[rt] = mn;
-        float cs = 0.f;
+        while (cur.i == i) {
+          u += NW;
+          const Chunk third = lookup(u + NW);
+          __builtin_amdgcn_sched_barrier(0);
+          // ---- logits
+          f32x4 x[NR][NKT];
 #pragma unroll
-        for (int kt = 0; kt < NKT; ++kt)
+          for (int rt = 0; rt < NR; ++rt)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            x[rt][kt][j] = exp_of(x[rt][kt][j] - ref);
-            cs += x[rt][kt][j];
-          }
-        ls[rt] = ls[rt] * al + cs;   // (this lane's entries; its lane groups are added at the end)
+            for (int kt = 0; kt < NKT; ++kt) x[rt][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < FPT; ++e) o[rt][e] *= al;
-      }
-      // ---- P.V
-      if constexpr (TL::B16) {
-        bf16x8 ph[NR], pl[NR];
+          for (int p = 0; p < NP; ++p)
 #pragma unroll
-        for (int rt = 0; rt < NR; ++rt)
+            for (int rt = 0; rt < NR; ++rt) {
+              const int qoff = (16 * rt + l) * QROW + 64 * p + 16 * lg;
+              const u32x4 qv = *(const u32x4*)(qs + qoff);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const float p = x[rt][k >> 2][k & 3];
-            ph[rt][k] = (__bf16)p;
-            pl[rt][k] = (__bf16)(p - (float)ph[rt][k]);
-          }
+              for (int kt = 0; kt < NKT; ++kt) {
+                if constexpr (TL::B16) {
+                  x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                      __builtin_bit_cast(bf16x8, kp[kt][p]), __builtin_bit_cast(bf16x8, qv), x[rt][kt], 0, 0, 0);
+                } else {
 #pragma unroll
-        for (int e = 0; e < FPT; ++e) {
-          u32x4 t;
+                  for (int e = 0; e < 4; ++e)
+                    x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kp[kt][p][e]),
+                                                                     __uint_as_float(qv[e]), x[rt][kt], 0, 0, 0);
+                }
+              }
+              if constexpr (TL::B16) {
+                const u32x4 qw = *(const u32x4*)(ql + qoff);
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            t[k] = __builtin_amdgcn_perm(vr[2 * k + 1][e >> 1], vr[2 * k][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
-          const bf16x8 vt = __builtin_bit_cast(bf16x8, t);
+                for (int kt = 0; kt < NKT; ++kt)
+                  x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                      __builtin_bit_cast(bf16x8, kp[kt][p]), __builtin_bit_cast(bf16x8, qw), x[rt][kt], 0, 0, 0);
+              }
+            }
+          f32x4 bc[NKT];
+#pragma unroll
+          for (int kt = 0; kt < NKT; ++kt) bc[kt] = bias[kt];
+          const Tiles next = resolve(nxt);
+          load_k(next);
+          __builtin_amdgcn_sched_barrier(0);
+          // ---- online softmax of this lane's rows over its entries
 #pragma unroll
           for (int rt = 0; rt < NR; ++rt) {
-            o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, ph[rt], o[rt][e], 0, 0, 0);
-            o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pl[rt], o[rt][e], 0, 0, 0);
+            float cm = -INFINITY;
+#pragma unroll
+            for (int kt = 0; kt < NKT; ++kt) {
+              const int seen = min(cur.nv[kt], lim[rt] - (cur.c * CH + 16 * kt) + 1) - 4 * lg;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                x[rt][kt][j] = j < seen ? fmaf(x[rt][kt][j], a.scale, bc[kt][j]) : -INFINITY;
+                cm = fmaxf(cm, x[rt][kt][j]);
+              }
+            }
+            const float mn = fmaxf(m[rt], groups_max(cm)), ref = mn == -INFINITY ? 0.f : mn;
+            const float al = exp_of(m[rt] - ref);
+            m[rt] = mn;
+            float cs = 0.f;
+#pragma unroll
+            for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                x[rt][kt][j] = exp_of(x[rt][kt][j] - ref);
+                cs += x[rt][kt][j];
+              }
+            ls[rt] = ls[rt] * al + cs;   // (this lane's entries; its lane groups are added at the end)
+#pragma unroll
+            for (int e = 0; e < FPT; ++e) o[rt][e] *= al;
           }
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int e = 0; e < FPT; ++e)
+          // ---- P.V
+          if constexpr (TL::B16) {
+            bf16x8 ph[NR], pl[NR];
 #pragma unroll
             for (int rt = 0; rt < NR; ++rt)
-              o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[j][e]), x[rt][0][j], o[rt][e], 0, 0, 0);
-      }
-      if (more) {
-        load_v(nxt);
-        cur = nxt;
-      }
-    }
-    // ---- the waves' sums into LDS, then added
 #pragma unroll
-    for (int rt = 0; rt < NR; ++rt) {
-      ls[rt] += __shfl_xor(ls[rt], 16);
-      ls[rt] += __shfl_xor(ls[rt], 32);
-    }
-    __syncthreads();   // every wave has read the query rows
+              for (int k = 0; k < 8; ++k) {
+                const float p = x[rt][k >> 2][k & 3];
+                ph[rt][k] = (__bf16)p;
+                pl[rt][k] = (__bf16)(p - (float)ph[rt][k]);
+              }
 #pragma unroll
-    for (int rt = 0; rt < NR; ++rt) {
-      const int r = 16 * rt + l;
-      if (lg == 0) {
-        wm[w][r] = m[rt];
-        wl[w][r] = ls[rt];
-      }
-      if (r < R) {
+            for (int e = 0; e < FPT; e += 2) {   // an even and an odd feature of one word
+              u32x4 t0, t1;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float* dst = osum + (w * R + r) * OROW + (4 * lg + j) * FPT;
+              for (int k = 0; k < 4; ++k) {
+                t0[k] = __builtin_amdgcn_perm(vr[2 * k + 1][e >> 1], vr[2 * k][e >> 1], 0x05040100u);
+                t1[k] = __builtin_amdgcn_perm(vr[2 * k + 1][e >> 1], vr[2 * k][e >> 1], 0x07060302u);
+              }
+              const bf16x8 w0 = __builtin_bit_cast(bf16x8, t0), w1 = __builtin_bit_cast(bf16x8, t1);
 #pragma unroll
-          for (int e = 0; e < FPT; e += 4)
-            *(float4*)(dst + e) = make_float4(o[rt][e][j], o[rt][e + 1][j], o[rt][e + 2][j], o[rt][e + 3][j]);
+              for (int rt = 0; rt < NR; ++rt) {
+                o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w0, ph[rt], o[rt][e], 0, 0, 0);
+                o[rt][e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w1, ph[rt], o[rt][e + 1], 0, 0, 0);
+                o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w0, pl[rt], o[rt][e], 0, 0, 0);
+                o[rt][e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w1, pl[rt], o[rt][e + 1], 0, 0, 0);
+              }
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+              for (int e = 0; e < FPT; ++e)
+#pragma unroll
+                for (int rt = 0; rt < NR; ++rt)
+                  o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[j][e]), x[rt][0][j], o[rt][e], 0, 0, 0);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          load_v(next);
+          __builtin_amdgcn_sched_barrier(0);
+          cur = next;
+          nxt = third;
         }
-      }
-    }
-    __syncthreads();
-    const bool whole = f0 == 0 && f1 == ns;
-    const long slot = ((long)h * a.G + g) * 2 + (f0 == 0 ? 1 : 0);
-    for (int e = tid; e < R * (D / 4); e += NT) {
-      const int r = e / (D / 4), x = e % (D / 4) * 4;
-      float M = wm[0][r];
+        // ---- the waves' sums into LDS, then added
 #pragma unroll
-      for (int i = 1; i < PAGED_WAVES; ++i) M = fmaxf(M, wm[i][r]);
-      const float ref = M == -INFINITY ? 0.f : M;
-      float L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < PAGED_WAVES; ++i) {
-        const float sc = exp_of(wm[i][r] - ref);
-        const float4 y = *(const float4*)(osum + (i * R + r) * OROW + x);
-        L += sc * wl[i][r];
-        acc[0] += sc * y.x;
-        acc[1] += sc * y.y;
-        acc[2] += sc * y.z;
-        acc[3] += sc * y.w;
-      }
-      if (whole) {
-        const float inv = L == 0.f ? 0.f : 1.f / L;   // a row that sees nothing; a NaN stays one
-        IT* dst = (IT*)a.out + (((long)s * a.nq + r % a.nq) * Hq + h * a.group + r / a.nq) * D + x;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) dst[u] = from_f32<IT>(acc[u] * inv);
-      } else {
-        *(float4*)(a.opart + (slot * R + r) * D + x) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-        if (x == 0) {
-          a.mpart[slot * R + r] = M;
-          a.lpart[slot * R + r] = L;
+        for (int rt = 0; rt < NR; ++rt) {
+          ls[rt] += __shfl_xor(ls[rt], 16);
+          ls[rt] += __shfl_xor(ls[rt], 32);
         }
+        if (ALIAS) __syncthreads();   // every wave has read the query rows
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) {
+          const int r = 16 * rt + l;
+          if (lg == 0) {
+            wm[w][r] = m[rt];
+            wl[w][r] = ls[rt];
+          }
+          if (r < R) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              float* dst = osum + (w * R + r) * OROW + (4 * lg + j) * FPT;
+#pragma unroll
+              for (int e = 0; e < FPT; e += 4)
+                *(float4*)(dst + e) = make_float4(o[rt][e][j], o[rt][e + 1][j], o[rt][e + 2][j], o[rt][e + 3][j]);
+            }
+          }
+        }
+        __syncthreads();   // (also: every wave has read the query rows)
+        const bool starts = at == s0, whole = starts && end == s1;
+        const long slot = ((long)h * a.G + g) * 2 + (starts ? 1 : 0);
+        for (int e = tid; e < R * (D / 4); e += NT) {
+          const int r = e / (D / 4), x = e % (D / 4) * 4;
+          float M = wm[0][r];
+#pragma unroll
+          for (int k = 1; k < NW; ++k) M = fmaxf(M, wm[k][r]);
+          const float ref = M == -INFINITY ? 0.f : M;
+          float L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < NW; ++k) {
+            const float sc = exp_of(wm[k][r] - ref);
+            const float4 y = *(const float4*)(osum + (k * R + r) * OROW + x);
+            L += sc * wl[k][r];
+            acc[0] += sc * y.x;
+            acc[1] += sc * y.y;
+            acc[2] += sc * y.z;
+            acc[3] += sc * y.w;
+          }
+          if (whole) {
+            const float inv = L == 0.f ? 0.f : 1.f / L;   // a row that sees nothing; a NaN stays one
+            IT* dst = (IT*)a.out + out_row(s, r) + x;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) dst[k] = from_f32<IT>(acc[k] * inv);
+          } else {
+            *(float4*)(a.opart + (slot * R + r) * D + x) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+            if (x == 0) {
+              a.mpart[slot * R + r] = M;
+              a.lpart[slot * R + r] = L;
+            }
+          }
+        }
+        if (starts) {
+          const int v = s1 + pad * (uniform(before[i]) + 1);   // the line with pads behind its last chunk
+          const int4 p = whole ? make_int4(-1, 0, 0, 0) : make_int4(s, g, (int)(((long)v * active - 1) / TV), 0);
+          if (a.by_seq) {
+            if (h == 0 && tid == 0) a.plan[s] = p;
+          } else if (!whole) {
+            goes_on[0] = p.x;
+            goes_on[1] = p.y;
+            goes_on[2] = p.z;
+          }
+        }
+        at = end;
+        if (ALIAS) __syncthreads();   // the sums have been read before the next sequence's query rows
       }
     }
-    if (f0 == 0 && f1 < ns) goes_on = make_int2(s, (int)((at * part.active - 1) / part.T));
-    __syncthreads();   // the sums have been read before the next sequence's query rows
+    __syncthreads();   // the round's lengths have been read
   }
-  if (h == 0 && tid == 0) a.plan[g] = goes_on;
+  if (h == 0 && tid == 0 && !a.by_seq) a.plan[g] = make_int4(goes_on[0], goes_on[1], goes_on[2], 0);
 }
 
 // Joins the partial sums of the sequences that lie in several parts: block
-// (x, h, g) those of the sequence that starts in workgroup g, rows x, x + gridDim.x, ...
+// (r, h, k) row r of plan entry k.  Groups of D / 4 lanes take every NG-th part.
 template <class IT, int D>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttendArgs a) {
-  constexpr int LPR = D / 4, NG = 256 / LPR;   // lanes per row, groups of parts
+  constexpr int LPR = D / 4, NG = 256 / LPR;
   __shared__ float4 acc[NG][LPR];
-  __shared__ float sum[NG];
-  const int h = blockIdx.y, g = blockIdx.z, R = a.group * a.nq, Hq = a.c.H * a.group;
-  const int2 p = a.plan[g];
+  __shared__ float sum[NG], top[NG];
+  const int r = blockIdx.x, h = blockIdx.y, R = a.group * a.nq, Hq = a.c.H * a.group;
+  const int4 p = a.plan[blockIdx.z];
   if (p.x < 0) return;
-  const int x = threadIdx.x % LPR, k = threadIdx.x / LPR, n = p.y - g + 1;
-  // part 0: the start, slot 1 of workgroup g; part i: slot 0 of workgroup g + i
-  auto slot = [&](int i) { return ((long)h * a.G + g + i) * 2 + (i == 0 ? 1 : 0); };
-  for (int r = blockIdx.x; r < R; r += gridDim.x) {
-    float M = -INFINITY;
-    for (int i = 0; i < n; ++i) M = fmaxf(M, a.mpart[slot(i) * R + r]);
+  const int x = threadIdx.x % LPR, k = threadIdx.x / LPR, n = p.z - p.y + 1;
+  // part 0: the start, slot 1 of its workgroup; part i: slot 0 of the i-th one behind it
+  auto at = [&](int i) { return (((long)h * a.G + p.y + i) * 2 + (i == 0 ? 1 : 0)) * R + r; };
+  float M = -INFINITY, L = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = k; i < n; i += NG) {
+    const float m = a.mpart[at(i)], l = a.lpart[at(i)];
+    const float4 v = *(const float4*)(a.opart + at(i) * D + 4 * x);
+    const float mn = fmaxf(M, m), ref = mn == -INFINITY ? 0.f : mn;
+    const float so = exp_of(M - ref), sn = exp_of(m - ref);
+    M = mn;
+    L = L * so + l * sn;
+    y[0] = y[0] * so + v.x * sn;
+    y[1] = y[1] * so + v.y * sn;
+    y[2] = y[2] * so + v.z * sn;
+    y[3] = y[3] * so + v.w * sn;
+  }
+  acc[k][x] = make_float4(y[0], y[1], y[2], y[3]);
+  if (x == 0) {
+    sum[k] = L;
+    top[k] = M;
+  }
+  __syncthreads();
+  if (k == 0) {
+    float S = 0.f, z[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NG; ++i) M = fmaxf(M, top[i]);
     const float ref = M == -INFINITY ? 0.f : M;
-    float L = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i = k; i < n; i += NG) {
-      const long at = slot(i) * R + r;
-      const float sc = exp_of(a.mpart[at] - ref);
-      const float4 v = *(const float4*)(a.opart + at * D + 4 * x);
-      L += sc * a.lpart[at];
-      y[0] += sc * v.x;
-      y[1] += sc * v.y;
-      y[2] += sc * v.z;
-      y[3] += sc * v.w;
-    }
-    acc[k][x] = make_float4(y[0], y[1], y[2], y[3]);
-    if (x == 0) sum[k] = L;
-    __syncthreads();
-    if (k == 0) {
-      float S = 0.f, z[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < NG; ++i) {
-        const float4 v = acc[i][x];
-        S += sum[i];
-        z[0] += v.x;
-        z[1] += v.y;
-        z[2] += v.z;
-        z[3] += v.w;
-      }
-      const float inv = S == 0.f ? 0.f : 1.f / S;
-      IT* dst = (IT*)a.out + (((long)p.x * a.nq + r % a.nq) * Hq + h * a.group + r / a.nq) * D + 4 * x;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) dst[u] = from_f32<IT>(z[u] * inv);
+    for (int i = 0; i < NG; ++i) {
+      const float4 v = acc[i][x];
+      const float sc = exp_of(top[i] - ref);
+      S += sum[i] * sc;
+      z[0] += v.x * sc;
+      z[1] += v.y * sc;
+      z[2] += v.z * sc;
+      z[3] += v.w * sc;
     }
-    __syncthreads();
+    const float inv = S == 0.f ? 0.f : 1.f / S;
+    IT* dst = (IT*)a.out + (((long)p.x * a.nq + r % a.nq) * Hq + h * a.group + r / a.nq) * D + 4 * x;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) dst[u] = from_f32<IT>(z[u] * inv);
   }
 }
 
