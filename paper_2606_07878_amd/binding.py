@@ -520,64 +520,70 @@ def _refuse(status: int, detail: str):
     raise StillError(status, detail)
 
 
-def _want(x, name: str, dtype, shape, dev) -> None:
-    """x is a contiguous tensor of this type and shape on dev."""
+def _want(x, name: str, dtype, shape, dev: int) -> None:
+    """x is a contiguous tensor of this type and shape on GPU dev (-1: none)."""
+    if x.dtype == dtype and x.shape == shape and x.is_contiguous() and x.get_device() == dev:
+        return
     if x.dtype != dtype:
         _refuse(-3, f"{name} is {x.dtype}, not {dtype}")
-    if tuple(x.shape) != shape:
-        _refuse(-2, f"{name} has shape {tuple(x.shape)}, not {shape}")
-    if not x.is_contiguous():
-        _refuse(-1, f"{name} is not contiguous")
-    if x.device != dev:
-        _refuse(-1, f"{name} is on {x.device}, not {dev}")
+    if x.shape != shape:
+        _refuse(-2, f"{name} has shape {tuple(x.shape)}, not {tuple(shape)}")
+    if x.get_device() != dev:
+        _refuse(-1, f"{name} is on {x.device}, the pages on GPU {dev}")
+    _refuse(-1, f"{name} is not contiguous")
 
 
 def _want_rows(x, name: str, pages, shape) -> None:
-    """x is a tensor of the pages' type with this shape and whole rows, on their device."""
+    """x is a tensor of the pages' type with this shape and whole rows, on their GPU."""
+    if x.dtype == pages.dtype and x.shape == shape and x.stride(2) == 1 and x.get_device() == pages.get_device():
+        return
     if x.dtype != pages.dtype:
         _refuse(-3, f"{name} is {x.dtype}, the pages {pages.dtype}")
-    if tuple(x.shape) != shape:
-        _refuse(-2, f"{name} has shape {tuple(x.shape)}, not {shape}")
-    if x.stride(2) != 1:
-        _refuse(-1, f"{name}'s rows are not contiguous")
-    if x.device != pages.device:
-        _refuse(-1, f"{name} is on {x.device}, not {pages.device}")
+    if x.shape != shape:
+        _refuse(-2, f"{name} has shape {tuple(x.shape)}, not {tuple(shape)}")
+    if x.get_device() != pages.get_device():
+        _refuse(-1, f"{name} is on {x.device}, the pages on {pages.device}")
+    _refuse(-1, f"{name}'s rows are not contiguous")
 
 
-def _paged(k_pages, v_pages, beta_pages, table, lens):
+def _paged(torch, k_pages, v_pages, beta_pages, table, lens):
     """The C views of a paged cache and its sequences, checked."""
-    torch = _torch()
-    if k_pages.dim() != 4:
-        _refuse(-2, f"k_pages has {k_pages.dim()} dimensions, not [n_pages, H, page_size, d]")
-    dt, dev = k_pages.dtype, k_pages.device
+    shape, dt, dev = k_pages.shape, k_pages.dtype, k_pages.get_device()
+    if len(shape) != 4:
+        _refuse(-2, f"k_pages has {len(shape)} dimensions, not [n_pages, H, page_size, d]")
     if dt != torch.bfloat16 and dt != torch.float32:
         _refuse(-3, f"pages of {dt}: bfloat16 and float32 are supported")
-    shape = tuple(k_pages.shape)
-    n_pages, H, P, d = shape
-    _want(k_pages, "k_pages", dt, shape, dev)
+    if not k_pages.is_contiguous():
+        _refuse(-1, "k_pages is not contiguous")
     _want(v_pages, "v_pages", dt, shape, dev)
+    n_pages, H, P, d = shape
+    beta = None
     if beta_pages is not None:
         _want(beta_pages, "beta_pages", torch.float32, shape[:3], dev)
-    if table.dim() != 2 or table.dtype != torch.int32 or (table.stride(1) != 1 and table.shape[1] > 1):
+        beta = beta_pages.data_ptr()
+    size = table.shape
+    if len(size) != 2 or table.dtype != torch.int32 or (table.stride(1) != 1 and size[1] > 1):
         _refuse(-2, "table is no int32 tensor [n_seqs, pages] with contiguous rows")
-    if table.device != dev:
-        _refuse(-1, f"table is on {table.device}, not {dev}")
-    n, width = table.shape
-    _want(lens, "lens", torch.int32, (n,), dev)
-    if dev.type != "cuda":
-        _refuse(-1, f"the pages are on {dev}: a GPU is needed")
+    if table.get_device() != dev:
+        _refuse(-1, f"table is on {table.device}, the pages on {k_pages.device}")
+    n, width = size
+    _want(lens, "lens", torch.int32, size[:1], dev)
+    if dev < 0:
+        _refuse(-1, f"the pages are on {k_pages.device}: a GPU is needed")
     return (still_paged_cache(H, d, P, n_pages, configs.MODE_FP32 if dt == torch.float32 else configs.MODE_BF16,
-                              k_pages.data_ptr(), v_pages.data_ptr(), _ptr(beta_pages)),
+                              k_pages.data_ptr(), v_pages.data_ptr(), beta),
             still_paged_seqs(n, width, table.stride(0) if n > 1 else width, table.data_ptr(), lens.data_ptr()))
 
 
-def _on(dev, call, *args):
-    """call(*args, current stream of dev) with dev current."""
-    torch = _torch()
-    if torch.cuda.current_device() == dev.index:
-        return call(*args, torch.cuda.current_stream(dev).cuda_stream)
-    with torch.cuda.device(dev):
-        return call(*args, torch.cuda.current_stream(dev).cuda_stream)
+def _on(torch, dev: int, call, *args) -> None:
+    """call(*args, current stream of GPU dev) with that GPU current; raises if it fails."""
+    if torch.cuda.current_device() == dev:
+        status = call(*args, torch._C._cuda_getCurrentRawStream(dev))
+    else:
+        with torch.cuda.device(dev):
+            status = call(*args, torch._C._cuda_getCurrentRawStream(dev))
+    if status != STILL_OK:
+        _check(status)
 
 
 def paged_append(k, v, k_pages, v_pages, table, lens, offsets=None, positions=None, rope_theta: float = 0.0,
@@ -594,26 +600,31 @@ def paged_append(k, v, k_pages, v_pages, table, lens, offsets=None, positions=No
     [n_pages, H, P] float32 always, and the entries' ``beta`` [n_tokens, H]
     float32 where it is not zero."""
     torch = _torch()
-    cache, seqs = _paged(k_pages, v_pages, beta_pages, table, lens)
-    dev = k_pages.device
+    cache, seqs = _paged(torch, k_pages, v_pages, beta_pages, table, lens)
+    dev = k_pages.get_device()
     if k.dim() != 3:
         _refuse(-2, f"k has {k.dim()} dimensions, not [n_tokens, H, d]")
-    n = int(k.shape[0])
+    n = k.shape[0]
     shape = (n, cache.n_kv_heads, cache.head_dim)
     _want_rows(k, "k", k_pages, shape)
     _want_rows(v, "v", k_pages, shape)
+    off = pos = b = None
     if offsets is not None:
         _want(offsets, "offsets", torch.int32, (seqs.n_seqs + 1,), dev)
+        off = offsets.data_ptr()
     if positions is not None:
         _want(positions, "positions", torch.float64, (n,), dev)
+        pos = positions.data_ptr()
     ts = hs = 0
     if beta is not None:
-        if beta.dtype != torch.float32 or tuple(beta.shape) != shape[:2] or beta.device != dev:
+        if beta.dtype != torch.float32 or beta.shape != shape[:2] or beta.get_device() != dev:
             _refuse(-2, "beta is no float32 tensor [n_tokens, H] on the pages' device")
         ts, hs = beta.stride()
-    tokens = still_paged_tokens(n, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), v.stride(0), v.stride(1),
-                                _ptr(beta), ts, hs, _ptr(offsets), _ptr(positions), float(rope_theta))
-    _check(_on(dev, still_paged_append, cache, seqs, tokens))
+        b = beta.data_ptr()
+    ks, vs = k.stride(), v.stride()
+    tokens = still_paged_tokens(n, k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1], b, ts, hs, off, pos,
+                                rope_theta)
+    _on(torch, dev, lib().still_paged_append, ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(tokens))
 
 
 def paged_gather(k_pages, v_pages, table, lens, seq: int, n: int, start: int = 0, beta_pages=None, out=None):
@@ -621,15 +632,15 @@ def paged_gather(k_pages, v_pages, table, lens, seq: int, n: int, start: int = 0
     with ``beta_pages`` (K, V, beta [H, n]), through still_paged_gather on the
     current stream; into ``out`` (such a tuple) where given."""
     torch = _torch()
-    cache, seqs = _paged(k_pages, v_pages, beta_pages, table, lens)
-    dev = k_pages.device
-    shape = (cache.n_kv_heads, int(n), cache.head_dim)
+    cache, seqs = _paged(torch, k_pages, v_pages, beta_pages, table, lens)
+    dev, n = k_pages.get_device(), int(n)
+    shape = (cache.n_kv_heads, n, cache.head_dim)
     if out is None:
         if n < 0:
             _refuse(-2, f"{n} entries asked for")
-        out = (torch.empty(shape, dtype=k_pages.dtype, device=dev), torch.empty(shape, dtype=k_pages.dtype, device=dev))
+        out = tuple(torch.empty(shape, dtype=k_pages.dtype, device=k_pages.device) for _ in range(2))
         if beta_pages is not None:
-            out += (torch.empty(shape[:2], dtype=torch.float32, device=dev),)
+            out += (torch.empty(shape[:2], dtype=torch.float32, device=k_pages.device),)
     elif len(out) != (2 if beta_pages is None else 3):
         _refuse(-2, "out holds K, V and, with beta_pages, beta")
     else:
@@ -637,8 +648,8 @@ def paged_gather(k_pages, v_pages, table, lens, seq: int, n: int, start: int = 0
         _want(out[1], "out[1]", k_pages.dtype, shape, dev)
         if beta_pages is not None:
             _want(out[2], "out[2]", torch.float32, shape[:2], dev)
-    _check(_on(dev, still_paged_gather, cache, seqs, int(seq), int(start), int(n), out[0], out[1],
-               None if beta_pages is None else out[2]))
+    _on(torch, dev, lib().still_paged_gather, ctypes.byref(cache), ctypes.byref(seqs), int(seq), int(start), n,
+        out[0].data_ptr(), out[1].data_ptr(), None if beta_pages is None else out[2].data_ptr())
     return out
 
 
@@ -652,32 +663,37 @@ def paged_attend(q, k_pages, v_pages, table, lens, causal: bool = False, scale: 
     ``out`` and ``workspace`` (STILL_PAGED_WORKSPACE_BYTES serve every call)
     may be given, so that the call allocates nothing (graph capture)."""
     torch = _torch()
-    cache, seqs = _paged(k_pages, v_pages, beta_pages, table, lens)
-    dev = k_pages.device
-    if q.dim() != 3:
-        _refuse(-2, f"q has {q.dim()} dimensions, not [n_seqs * n_queries, H * group, d]")
-    tokens, Hq, d = q.shape
+    cache, seqs = _paged(torch, k_pages, v_pages, beta_pages, table, lens)
+    dev, shape = k_pages.get_device(), q.shape
+    if len(shape) != 3:
+        _refuse(-2, f"q has {len(shape)} dimensions, not [n_seqs * n_queries, H * group, d]")
+    tokens, Hq, d = shape
     H, n = cache.n_kv_heads, seqs.n_seqs
     if d != cache.head_dim or Hq < H or Hq % H or tokens < n or tokens % n:
-        _refuse(-2, f"q {tuple(q.shape)} does not fit {n} sequences and pages {tuple(k_pages.shape)}")
-    _want_rows(q, "q", k_pages, (tokens, Hq, d))
-    if q.stride(1) != d:
+        _refuse(-2, f"q {tuple(shape)} does not fit {n} sequences and pages {tuple(k_pages.shape)}")
+    _want_rows(q, "q", k_pages, shape)
+    qs = q.stride()
+    if qs[1] != d:
         _refuse(-1, "q's tokens are not contiguous")
+    pos = None
     if q_positions is not None:
         _want(q_positions, "q_positions", torch.float64, (tokens,), dev)
-    cfg = still_paged_attend_config(Hq // H, tokens // n, int(causal), float(scale), float(rope_theta),
-                                    q.stride(0) if tokens > 1 else 0)
+        pos = q_positions.data_ptr()
+    cfg = still_paged_attend_config(Hq // H, tokens // n, causal, scale, rope_theta, qs[0] if tokens > 1 else 0)
     if out is None:
-        out = torch.empty(tokens, Hq, d, dtype=q.dtype, device=dev)
+        out = torch.empty(shape, dtype=q.dtype, device=q.device)
     else:
-        _want(out, "out", q.dtype, (tokens, Hq, d), dev)
-    if workspace is not None and workspace.device != dev:
-        _refuse(-1, f"workspace is on {workspace.device}, not {dev}")
-    if workspace is None or workspace.numel() < STILL_PAGED_WORKSPACE_BYTES:
+        _want(out, "out", q.dtype, shape, dev)
+    if workspace is not None and workspace.get_device() != dev:
+        _refuse(-1, f"workspace is on {workspace.device}, the pages on {k_pages.device}")
+    room = 0 if workspace is None else workspace.numel()
+    if room < STILL_PAGED_WORKSPACE_BYTES:
         need = still_paged_attend_workspace_size(cache, cfg)
-        if workspace is None or workspace.numel() < need:
-            workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
-    _check(_on(dev, still_paged_attend, cache, seqs, cfg, q, q_positions, out, workspace, workspace.numel()))
+        if room < need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            room = need
+    _on(torch, dev, lib().still_paged_attend, ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(cfg), q.data_ptr(),
+        pos, out.data_ptr(), _ptr(workspace), room)
     return out
 
 
@@ -709,7 +725,7 @@ def compact_paged(cfg: configs.CompactorConfig, weights: List[Dict[str, object]]
         _refuse(-2, f"sequence {seq} outside [0, {table.shape[0]})")
     if length > table.shape[1] * k_pages[0].shape[2]:
         _refuse(-2, f"{length} entries do not fit the sequence's {table.shape[1]} pages")
-    _want(positions, "positions", torch.float64, (n,), k_pages[0].device)
+    _want(positions, "positions", torch.float64, (n,), k_pages[0].get_device())
     dev, mode = k_pages[0].device, (configs.MODE_FP32 if k_pages[0].dtype == torch.float32 else configs.MODE_BF16)
     row = table[seq:seq + 1]
     to = [torch.full((1,), x, dtype=torch.int32, device=dev) for x in (start + t, length)]

@@ -89,6 +89,11 @@ static still_status check_attend(const still_paged_cache* c, const still_paged_a
   return STILL_OK;
 }
 
+// Whether a workgroup takes a whole sequence.
+static bool paged_single(const still_paged_cache* c, const still_paged_seqs* q, int R) {
+  return R <= 16 && (long)q->max_pages * c->page_size <= 1024;
+}
+
 struct PagedPlan {
   int G;
   size_t opart, mpart, lpart, total;   // offsets behind the plan, bytes
@@ -227,6 +232,7 @@ still_status still_paged_attend(const still_paged_cache* cache, const still_page
   a.log2_theta = cfg->rope_theta > 0.0 ? std::log2(cfg->rope_theta) : 0.0;
   a.group = cfg->group;
   a.nq = cfg->n_queries;
+  a.nq_inv = (1 << 16) / cfg->n_queries + 1;
   a.causal = cfg->causal;
   a.scale = cfg->scale != 0.f ? cfg->scale : 1.f / std::sqrt((float)cache->head_dim);
   a.G = p.G;
@@ -242,10 +248,15 @@ still_status still_paged_attend(const still_paged_cache* cache, const still_page
   paged_dispatch(cache, [&](auto it, auto d) {
     using IT = decltype(it);
     constexpr int D = decltype(d)::value;
+    if (paged_single(cache, seqs, R)) {
+      hipLaunchKernelGGL((paged_attend_kernel<IT, D, 1, true>), dim3(a.c.H, a.c.n_seqs), dim3(64 * PAGED_SINGLE_WAVES),
+                         (paged_lds_bytes<IT, D>(R, PAGED_SINGLE_WAVES)), st, a);
+      return;
+    }
     const dim3 grid(a.c.H, a.G), block(64 * PAGED_WAVES);
-    const size_t lds = paged_lds_bytes<IT, D>(R);
-    if (R <= 16) hipLaunchKernelGGL((paged_attend_kernel<IT, D, 1>), grid, block, lds, st, a);
-    else hipLaunchKernelGGL((paged_attend_kernel<IT, D, 2>), grid, block, lds, st, a);
+    const size_t lds = paged_lds_bytes<IT, D>(R, PAGED_WAVES);
+    if (R <= 16) hipLaunchKernelGGL((paged_attend_kernel<IT, D, 1, false>), grid, block, lds, st, a);
+    else hipLaunchKernelGGL((paged_attend_kernel<IT, D, 2, false>), grid, block, lds, st, a);
     if (a.G > 1)
       hipLaunchKernelGGL((paged_merge_kernel<IT, D>), dim3(R, a.c.H, std::min(a.c.n_seqs, a.G)), dim3(256), 0, st, a);
   });

@@ -206,6 +206,8 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(PagedGatherArgs a) {
 // read through a buffer descriptor of its valid rows: the others read as zeros
 // and cost nothing, so the loop has no branch and every load's wait counts only
 // the loads behind it.
+//
+// SINGLE: workgroup (h, s) takes all of sequence s; nothing is joined.
 // ---------------------------------------------------------------------------
 struct PagedAttendArgs {
   PagedArgs c;
@@ -215,6 +217,7 @@ struct PagedAttendArgs {
   const double* qpos;  // NULL: q as given
   double log2_theta;
   int group, nq, causal;
+  int nq_inv;          // 2^16 / nq + 1: r / nq = r nq_inv >> 16 for the rows r < 32
   float scale;
   int G;               // workgroups per KV head
   int by_seq;          // plan entries are per sequence (n_seqs <= G), else per workgroup
@@ -224,8 +227,9 @@ struct PagedAttendArgs {
   float* lpart;
 };
 
-constexpr int PAGED_WAVES = 4;
-constexpr int PAGED_ROUND = 64 * PAGED_WAVES;   // sequences whose lengths a block holds at a time
+constexpr int PAGED_WAVES = 4;           // per workgroup
+constexpr int PAGED_SINGLE_WAVES = 8;    // ... that takes a whole sequence
+constexpr int PAGED_ROUND = 256;         // sequences whose lengths a wave holds at a time, four per lane
 constexpr int PAGED_PAD = 2;
 constexpr float LOG2E = 1.4426950408889634f;
 
@@ -252,12 +256,12 @@ constexpr bool paged_alias(int D, int NR) { return D * NR > 256; }
 // 256 registers to two
 constexpr int paged_resident(int D, int NR) { return D * NR <= 128 ? 2 : 1; }
 
-// dynamic LDS: the query rows, the waves' sums [4][R][OROW]
+// dynamic LDS: the query rows, the waves' sums [waves][R][OROW]
 template <class IT, int D>
-inline size_t paged_lds_bytes(int R) {
+inline size_t paged_lds_bytes(int R, int waves) {
   using TL = PagedTile<IT, D>;
   const int nr = R <= 16 ? 1 : 2;
-  const size_t q = (size_t)nr * TL::QBYTES, o = (size_t)PAGED_WAVES * R * TL::OROW * sizeof(float);
+  const size_t q = (size_t)nr * TL::QBYTES, o = (size_t)waves * R * TL::OROW * sizeof(float);
   return paged_alias(D, nr) ? std::max(q, o) : q + o;
 }
 
@@ -272,6 +276,34 @@ __device__ __forceinline__ float groups_max(float x) {
   x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
   const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// inclusive sum over the wave's lanes up to this one
+__device__ __forceinline__ int lanes_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);   // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // last lane of the row before, into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);  // lane 31 into rows 2 and 3
+  return x;
+}
+
+// Lane k of a wave holds values 4 k .. 4 k + 3 of a list: value i (uniform), and
+// the last one at or below v in a rising list that starts at or below it.
+__device__ __forceinline__ int list_get(const int (&x)[4], int i) {
+  const int l = i >> 2, k = i & 3;
+  const int a = __builtin_amdgcn_readlane(x[0], l), b = __builtin_amdgcn_readlane(x[1], l);
+  const int c = __builtin_amdgcn_readlane(x[2], l), d = __builtin_amdgcn_readlane(x[3], l);
+  const int ab = k & 1 ? b : a, cd = k & 1 ? d : c;
+  return k & 2 ? cd : ab;
+}
+__device__ __forceinline__ int list_find(const int (&x)[4], int v) {
+  const int l = max(__popcll(__ballot(x[0] <= v)) - 1, 0);
+  int i = 4 * l;
+#pragma unroll
+  for (int k = 1; k < 4; ++k) i += __builtin_amdgcn_readlane(x[k], l) <= v;
+  return i;
 }
 
 // B bytes (4, 8 or a multiple of 16) at byte off of a buffer into words
@@ -296,149 +328,129 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t paged_rows(const void* p, int 
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000);
 }
 
-template <class IT, int D, int NR>
-__global__ __launch_bounds__(64 * PAGED_WAVES, paged_resident(D, NR)) void paged_attend_kernel(PagedAttendArgs a) {
+template <class IT, int D, int NR, bool SINGLE>
+__global__ __launch_bounds__(64 * (SINGLE ? PAGED_SINGLE_WAVES : PAGED_WAVES),
+                             SINGLE ? 2 : paged_resident(D, NR)) void paged_attend_kernel(PagedAttendArgs a) {
   using TL = PagedTile<IT, D>;
   constexpr int NKT = TL::NKT, CH = TL::CH, NP = TL::NP, FPT = TL::FPT, VB = TL::VB, ROWB = TL::ROWB;
-  constexpr int QROW = TL::QROW, OROW = TL::OROW, NT = 64 * PAGED_WAVES, HD = D / 2, NW = PAGED_WAVES;
+  constexpr int NW = SINGLE ? PAGED_SINGLE_WAVES : PAGED_WAVES;
+  constexpr int QROW = TL::QROW, OROW = TL::OROW, NT = 64 * NW, HD = D / 2;
   constexpr bool ALIAS = paged_alias(D, NR);
   extern __shared__ float4 paged_smem[];
   char* qs = (char*)paged_smem;                  // [16 NR][QROW], bf16: the same again for the low parts
   char* ql = qs + 16 * NR * QROW;
-  float* osum = (float*)(qs + (ALIAS ? 0 : NR * TL::QBYTES));   // [4][R][OROW]
+  float* osum = (float*)(qs + (ALIAS ? 0 : NR * TL::QBYTES));   // [NW][R][OROW]
   __shared__ float wm[NW][16 * NR], wl[NW][16 * NR];
-  __shared__ int wsum[NW], wcnt[NW], cut[2];
-  // a round's sequences: first chunk, length, non-empty ones before
-  __shared__ int first[PAGED_ROUND + 1], slen[PAGED_ROUND], before[PAGED_ROUND];
   const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
   const int l = lane & 15, lg = lane >> 4;
-  const int h = blockIdx.x, g = blockIdx.y, R = a.group * a.nq, Hq = a.c.H * a.group;
+  const int h = blockIdx.x, g = SINGLE ? 0 : blockIdx.y, R = a.group * a.nq, Hq = a.c.H * a.group;
   const int n_seqs = a.c.n_seqs, pad = n_seqs > 1 ? PAGED_PAD : 0;
   const bool rot = a.qpos != nullptr;
   const int koff = l * ROWB + lg * 16, voff = 4 * lg * ROWB + l * VB;
-  auto out_row = [&](int s, int r) { return (((long)s * a.nq + r % a.nq) * Hq + h * a.group + r / a.nq) * D; };
+  auto head_of = [&](int r) { return r * a.nq_inv >> 16; };   // of the group; the query is r - nq * that
+  auto out_row = [&](int s, int r) {
+    const int hr = head_of(r);
+    return (((long)s * a.nq + r - hr * a.nq) * Hq + h * a.group + hr) * D;
+  };
 
   // ---- this workgroup's part of the line
-  int T = 0, TV = 0, active = 0, v0 = 0, v1 = 0;   // chunks, chunks with pads, workgroups with a part, the part's cuts
-  auto cuts = [&](int chunks, int seqs) {
-    T = chunks;
-    TV = chunks + pad * seqs;
-    active = min(a.G, (chunks + NW - 1) / NW);   // a workgroup takes a chunk per wave before another one starts
+  const int cap = (int)paged_cap(a.c);
+  int lens[4];    // of the round's sequences, four per lane
+  auto load_lens = [&](int base) {
+    const auto x = __builtin_bit_cast(
+        u32x4, __builtin_amdgcn_raw_buffer_load_b128(paged_rows(a.c.lens + base, 4 * min(PAGED_ROUND, n_seqs - base)),
+                                                     16 * lane, 0, 0));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) lens[k] = min(max((int)x[k], 0), cap);
+  };
+  auto chunks = [&](int len) { return (len + CH - 1) / CH; };
+  int TV = 0, active = 0, v0 = 0, v1 = 0;   // chunks with pads, workgroups with a part, this part's cuts
+  auto cuts = [&](int T, int some) {        // of the sums over all sequences
+    TV = T + pad * some;
+    active = min(a.G, (T + NW - 1) / NW);   // a workgroup takes a chunk per wave before another one starts
     if (g < active) {
       v0 = (int)((long)g * TV / active);
       v1 = (int)((long)(g + 1) * TV / active);
     }
   };
-  auto length = [&](int s) { return s < n_seqs ? paged_len(a.c, s) : 0; };
-  auto totals = [&](int chunks, int seqs) {   // of the block; leaves the waves' in wsum, wcnt
-    if (lane == 63) {
-      wsum[w] = chunks;
-      wcnt[w] = seqs;
-    }
-    __syncthreads();
-    int2 t = make_int2(0, 0);
+  if (!SINGLE && n_seqs > PAGED_ROUND) {
+    int n = 0, some = 0;
+    for (int base = 0; base < n_seqs; base += PAGED_ROUND) {
+      load_lens(base);
 #pragma unroll
-    for (int i = 0; i < NW; ++i) {
-      t.x += wsum[i];
-      t.y += wcnt[i];
-    }
-    return make_int2(uniform(t.x), uniform(t.y));
-  };
-  if (n_seqs > PAGED_ROUND) {
-    int n = 0, m = 0;
-    for (int s = tid; s < n_seqs; s += NT) {
-      const int c = (length(s) + CH - 1) / CH;
-      n += c;
-      m += c > 0;
-    }
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      n += __shfl_xor(n, off);
-      m += __shfl_xor(m, off);
-    }
-    const int2 t = totals(n, m);
-    cuts(t.x, t.y);
-    __syncthreads();
-  }
-  int goes_on[3] = {-1, 0, 0};
-  int line = 0, seqs = 0;   // chunks and non-empty sequences before this round
-  for (int base = 0; base < n_seqs; base += PAGED_ROUND) {
-    const int cnt = min(PAGED_ROUND, n_seqs - base);
-    int lo, hi;
-    {
-      const int len = length(base + tid), n = (len + CH - 1) / CH;
-      int incl = n;
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        const int x = __shfl_up(incl, off);
-        if (lane >= off) incl += x;
+      for (int k = 0; k < 4; ++k) {
+        n += chunks(lens[k]);
+        some += lens[k] > 0;
       }
-      const unsigned long some = __ballot(n > 0);
-      const int2 t = totals(incl, __popcll(some));
-      if (n_seqs <= PAGED_ROUND) cuts(t.x, t.y);
-      int f = line + incl - n, b = seqs + __popcll(some & ((1UL << lane) - 1));
-#pragma unroll
-      for (int i = 0; i < NW; ++i)
-        if (i < w) {
-          f += wsum[i];
-          b += wcnt[i];
-        }
-      first[tid] = f;
-      slen[tid] = len;
-      before[tid] = b;
-      if (tid == 0) first[PAGED_ROUND] = line + t.x;
-      const int v = f + pad * b, p = n > 0 ? pad : 0;   // its place on the line with pads
-      if (n > 0 && v <= v0 && v0 < v + p + n) cut[0] = f + max(0, v0 - v - p);
-      if (n > 0 && v <= v1 && v1 < v + p + n) cut[1] = f + max(0, v1 - v - p);
-      __syncthreads();
-      const int vs = line + pad * seqs, ve = vs + t.x + pad * t.y;
-      lo = v0 <= vs ? line : v0 >= ve ? line + t.x : uniform(cut[0]);
-      hi = v1 <= vs ? line : v1 >= ve ? line + t.x : uniform(cut[1]);
-      line += t.x;
-      seqs += t.y;
     }
+    cuts(__builtin_amdgcn_readlane(lanes_scan(n), 63), __builtin_amdgcn_readlane(lanes_scan(some), 63));
+  }
+  int4 goes_on = make_int4(-1, 0, 0, 0);
+  int line = 0, padded = 0;   // chunks in front of the round, without and with pads
+  for (int base = SINGLE ? blockIdx.y : 0; base < n_seqs; base += PAGED_ROUND) {
+    const int cnt = SINGLE ? 1 : min(PAGED_ROUND, n_seqs - base);
+    int first[4], padded_first[4], lo, hi;   // of the round's sequences on the line; the part's chunks in the round
+    if constexpr (SINGLE) {
+      lens[0] = uniform(min(max(a.c.lens[base], 0), cap));
+      lo = 0;
+      hi = chunks(lens[0]);
+    } else {
+      load_lens(base);
+      int n = 0, some = 0, before = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        n += chunks(lens[k]);
+        const unsigned long full = __ballot(lens[k] > 0);
+        some += __popcll(full);
+        before += __popcll(full & ((1UL << lane) - 1));
+      }
+      const int incl = lanes_scan(n), total = __builtin_amdgcn_readlane(incl, 63);
+      if (n_seqs <= PAGED_ROUND) cuts(total, some);
+      int f = line + incl - n, v = padded + incl - n + pad * before;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        first[k] = f;
+        padded_first[k] = v;
+        f += chunks(lens[k]);
+        v += chunks(lens[k]) + (lens[k] > 0 ? pad : 0);
+      }
+      const int line_end = line + total, padded_end = padded + total + pad * some;
+      auto cut = [&](int v) {   // the first chunk at or behind place v of the line with pads
+        const int i = list_find(padded_first, v);
+        const int c = list_get(first, i) + max(0, v - list_get(padded_first, i) - pad);
+        return v <= padded ? line : v >= padded_end ? line_end : c;
+      };
+      lo = cut(v0);
+      hi = cut(v1);
+      line = line_end;
+      padded = padded_end;
+    }
+    auto len_of = [&](int i) { return SINGLE ? lens[0] : list_get(lens, i); };
     // rows of sequences without entries
-    for (int k = g; k < cnt; k += a.G)
-      if (uniform(slen[k]) == 0) {
+    for (int k = SINGLE ? 0 : g; k < cnt; k += SINGLE ? 1 : a.G)
+      if (len_of(k) == 0) {
         for (int e = tid; e < R * (ROWB / 16); e += NT) {
           const u32x4 z = {0, 0, 0, 0};
           ((u32x4*)(a.out + out_row(base + k, e / (ROWB / 16)) * (long)sizeof(IT)))[e % (ROWB / 16)] = z;
         }
-        if (h == 0 && tid == 0 && a.by_seq) a.plan[base + k] = make_int4(-1, 0, 0, 0);
+        if (!SINGLE && h == 0 && tid == 0 && a.by_seq) a.plan[base + k] = make_int4(-1, 0, 0, 0);
       }
-    // ---- the stream of this wave's chunks.  Lane k holds the first chunks and
-    // lengths of sequences k, 64 + k, ... of the round.
-    int lfirst[NW], llen[NW];
-#pragma unroll
-    for (int k = 0; k < NW; ++k) {
-      lfirst[k] = first[64 * k + lane];
-      llen[k] = slen[64 * k + lane];
-    }
+    // ---- the stream of this wave's chunks
     struct Chunk {
       int i, c, len;    // sequence of the round (none: PAGED_ROUND), chunk in it, its length
       int p[NKT];       // page numbers of its tiles, as read
     };
     auto lookup = [&](int u) {   // chunk u of the line: the last sequence that starts at or before it
       Chunk k;
-      int li = -1, f = 0;
-#pragma unroll
-      for (int x = 0; x < NW; ++x) li += __popcll(__ballot(lfirst[x] <= u));
-      li = min(max(li, 0), cnt - 1);
-#pragma unroll
-      for (int x = 0; x < NW; ++x) {
-        const bool here = li >> 6 == x;
-        const int ff = __builtin_amdgcn_readlane(lfirst[x], li & 63), ll = __builtin_amdgcn_readlane(llen[x], li & 63);
-        f = here ? ff : f;
-        k.len = here || x == 0 ? ll : k.len;
-      }
+      const int i = SINGLE ? 0 : min(list_find(first, u), cnt - 1);
       const bool there = u < hi;
-      k.i = there ? li : PAGED_ROUND;
-      k.len = there ? k.len : 0;
-      k.c = u - f;
+      k.i = there ? i : PAGED_ROUND;
+      k.len = there ? len_of(i) : 0;
+      k.c = SINGLE ? u : u - list_get(first, i);
 #pragma unroll
       for (int kt = 0; kt < NKT; ++kt) {
         const int j = max(min(k.c * CH + 16 * kt, k.len - 1), 0);
-        k.p[kt] = a.c.table[(base + li) * a.c.tstride + (j >> a.c.lp)];
+        k.p[kt] = a.c.table[(base + i) * a.c.tstride + (j >> a.c.lp)];
       }
       return k;
     };
@@ -491,17 +503,18 @@ __global__ __launch_bounds__(64 * PAGED_WAVES, paged_resident(D, NR)) void paged
       __builtin_amdgcn_sched_barrier(0);   // (loads stay in this order: their waits count the ones behind)
       load_v(cur);
       __builtin_amdgcn_sched_barrier(0);
-      for (int i = 0, at = lo; at < hi; ++i) {
-        const int s0 = uniform(first[i]), s1 = uniform(first[i + 1]);
-        if (s1 <= at) continue;   // before the part, or empty
-        const int s = base + i, end = min(s1, hi), len = uniform(slen[i]);
+      for (int i = SINGLE ? 0 : list_find(first, lo), at = lo; at < hi; ++i) {
+        const int len = len_of(i), s0 = SINGLE ? 0 : list_get(first, i), s1 = s0 + chunks(len);
+        if (len == 0) continue;
+        const int s = base + i, end = min(s1, hi);
         // ---- query rows into LDS: row g * nq + i is query i of head h * group + g
         for (int e = tid; e < 16 * NR * HD; e += NT) {
           const int r = e / HD, j = e % HD;
           float x0 = 0.f, x1 = 0.f;
           if (r < R) {
-            const long t = (long)s * a.nq + r % a.nq;
-            const IT* q = (const IT*)(a.q + t * a.q_ts) + (long)(h * a.group + r / a.nq) * D;
+            const int hr = head_of(r);
+            const long t = (long)s * a.nq + r - hr * a.nq;
+            const IT* q = (const IT*)(a.q + t * a.q_ts) + (long)(h * a.group + hr) * D;
             x0 = to_f32(q[j]);
             x1 = to_f32(q[j + HD]);
             if (rot) {
@@ -530,7 +543,7 @@ __global__ __launch_bounds__(64 * PAGED_WAVES, paged_resident(D, NR)) void paged
         for (int rt = 0; rt < NR; ++rt) {
           m[rt] = -INFINITY;
           ls[rt] = 0.f;
-          lim[rt] = a.causal ? len - a.nq + (16 * rt + l) % a.nq : len - 1;
+          lim[rt] = a.causal ? len - a.nq + 16 * rt + l - head_of(16 * rt + l) * a.nq : len - 1;
 #pragma unroll
           for (int e = 0; e < FPT; ++e) o[rt][e] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
@@ -672,7 +685,7 @@ __global__ __launch_bounds__(64 * PAGED_WAVES, paged_resident(D, NR)) void paged
           }
         }
         __syncthreads();   // (also: every wave has read the query rows)
-        const bool starts = at == s0, whole = starts && end == s1;
+        const bool starts = at == s0, whole = SINGLE || (starts && end == s1);
         const long slot = ((long)h * a.G + g) * 2 + (starts ? 1 : 0);
         for (int e = tid; e < R * (D / 4); e += NT) {
           const int r = e / (D / 4), x = e % (D / 4) * 4;
@@ -704,24 +717,23 @@ __global__ __launch_bounds__(64 * PAGED_WAVES, paged_resident(D, NR)) void paged
             }
           }
         }
-        if (starts) {
-          const int v = s1 + pad * (uniform(before[i]) + 1);   // the line with pads behind its last chunk
+        if (!SINGLE && starts) {
+          const int v = list_get(padded_first, i) + pad + s1 - s0;   // behind its last chunk
           const int4 p = whole ? make_int4(-1, 0, 0, 0) : make_int4(s, g, (int)(((long)v * active - 1) / TV), 0);
           if (a.by_seq) {
             if (h == 0 && tid == 0) a.plan[s] = p;
           } else if (!whole) {
-            goes_on[0] = p.x;
-            goes_on[1] = p.y;
-            goes_on[2] = p.z;
+            goes_on = p;
           }
         }
         at = end;
         if (ALIAS) __syncthreads();   // the sums have been read before the next sequence's query rows
       }
     }
-    __syncthreads();   // the round's lengths have been read
+    if (SINGLE) break;
+    __syncthreads();   // the last sequence's sums have been read
   }
-  if (h == 0 && tid == 0 && !a.by_seq) a.plan[g] = make_int4(goes_on[0], goes_on[1], goes_on[2], 0);
+  if (!SINGLE && h == 0 && tid == 0 && !a.by_seq) a.plan[g] = goes_on;
 }
 
 // Joins the partial sums of the sequences that lie in several parts: block
