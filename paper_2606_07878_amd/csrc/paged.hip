@@ -91,7 +91,8 @@ static still_status check_attend(const still_paged_cache* c, const still_paged_a
 
 // Whether a workgroup takes a whole sequence.
 static bool paged_single(const still_paged_cache* c, const still_paged_seqs* q, int R) {
-  return R <= 16 && (long)q->max_pages * c->page_size <= 1024;
+  return R <= 16 && c->head_dim <= 128 && (long)q->max_pages * c->page_size <= 1024 &&
+         (long)q->n_seqs * c->n_kv_heads <= 512;
 }
 
 struct PagedPlan {
@@ -248,13 +249,13 @@ still_status still_paged_attend(const still_paged_cache* cache, const still_page
   paged_dispatch(cache, [&](auto it, auto d) {
     using IT = decltype(it);
     constexpr int D = decltype(d)::value;
-    if (paged_single(cache, seqs, R)) {
-      hipLaunchKernelGGL((paged_attend_kernel<IT, D, 1, true>), dim3(a.c.H, a.c.n_seqs), dim3(64 * PAGED_SINGLE_WAVES),
-                         (paged_lds_bytes<IT, D>(R, PAGED_SINGLE_WAVES)), st, a);
+    if constexpr (D <= 128) if (paged_single(cache, seqs, R)) {
+      hipLaunchKernelGGL((paged_attend_kernel<IT, D, 1, true>), dim3(a.c.H, a.c.n_seqs), dim3(64 * paged_waves(sizeof(IT), D, 1, true)),
+                         (paged_lds_bytes<IT, D>(R, true)), st, a);
       return;
     }
-    const dim3 grid(a.c.H, a.G), block(64 * PAGED_WAVES);
-    const size_t lds = paged_lds_bytes<IT, D>(R, PAGED_WAVES);
+    const dim3 grid(a.c.H, a.G), block(64 * paged_waves(sizeof(IT), D, R <= 16 ? 1 : 2, false));
+    const size_t lds = paged_lds_bytes<IT, D>(R, false);
     if (R <= 16) hipLaunchKernelGGL((paged_attend_kernel<IT, D, 1, false>), grid, block, lds, st, a);
     else hipLaunchKernelGGL((paged_attend_kernel<IT, D, 2, false>), grid, block, lds, st, a);
     if (a.G > 1)

@@ -227,19 +227,28 @@ struct PagedAttendArgs {
   float* lpart;
 };
 
-constexpr int PAGED_WAVES = 4;           // per workgroup
-constexpr int PAGED_SINGLE_WAVES = 8;    // ... that takes a whole sequence
 constexpr int PAGED_ROUND = 256;         // sequences whose lengths a wave holds at a time, four per lane
 constexpr int PAGED_PAD = 2;
+constexpr float PAGED_SLACK = 6.f;       // weights reach e^6 before they are scaled back
 constexpr float LOG2E = 1.4426950408889634f;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-template <class IT, int D>
+// Waves per workgroup, workgroups resident on a CU, and 16-entry tiles per chunk:
+// 128 KB of keys and values in flight per CU.
+constexpr int paged_waves(int esize, int D, int NR, bool SINGLE) {
+  return SINGLE || (NR == 2 && D <= 128 && esize == 4) ? 8 : 4;
+}
+constexpr int paged_resident(int D, int NR) { return NR == 1 && D <= 128 ? 2 : 1; }
+constexpr int paged_tiles(int esize, int D, int NR) {
+  return (NR == 1 && D == 64 ? 64 : 128) * 1024 / (paged_waves(esize, D, NR, false) * paged_resident(D, NR) * 32 * D * esize);
+}
+
+template <class IT, int D, int NR, bool SINGLE>
 struct PagedTile {
   static constexpr bool B16 = sizeof(IT) == 2;
-  static constexpr int NKT = B16 ? 2 : 1;               // 16-entry tiles per chunk
+  static constexpr int NKT = SINGLE ? (B16 ? 2 : 1) : paged_tiles(sizeof(IT), D, NR);   // 16-entry tiles per chunk
   static constexpr int CH = 16 * NKT;
   static constexpr int ROWB = D * (int)sizeof(IT);
   static constexpr int NP = ROWB / 64;                  // 16-byte pieces of a key per lane
@@ -250,18 +259,14 @@ struct PagedTile {
 };
 
 // the waves' sums take the query rows' place in LDS where both do not fit 160 KB
-constexpr bool paged_alias(int D, int NR) { return D * NR > 256; }
-
-// workgroups resident on a CU (waves per SIMD): 16 rows of up to 128 features leave
-// 256 registers to two
-constexpr int paged_resident(int D, int NR) { return D * NR <= 128 ? 2 : 1; }
+constexpr bool paged_alias(int D, int NR) { return D * NR >= 256 && NR == 2; }
 
 // dynamic LDS: the query rows, the waves' sums [waves][R][OROW]
 template <class IT, int D>
-inline size_t paged_lds_bytes(int R, int waves) {
-  using TL = PagedTile<IT, D>;
+inline size_t paged_lds_bytes(int R, bool single) {
+  using TL = PagedTile<IT, D, 1, true>;   // (the row sizes are the same for all)
   const int nr = R <= 16 ? 1 : 2;
-  const size_t q = (size_t)nr * TL::QBYTES, o = (size_t)waves * R * TL::OROW * sizeof(float);
+  const size_t q = (size_t)nr * TL::QBYTES, o = (size_t)paged_waves(sizeof(IT), D, nr, single) * R * TL::OROW * sizeof(float);
   return paged_alias(D, nr) ? std::max(q, o) : q + o;
 }
 
@@ -329,17 +334,18 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t paged_rows(const void* p, int 
 }
 
 template <class IT, int D, int NR, bool SINGLE>
-__global__ __launch_bounds__(64 * (SINGLE ? PAGED_SINGLE_WAVES : PAGED_WAVES),
-                             SINGLE ? 2 : paged_resident(D, NR)) void paged_attend_kernel(PagedAttendArgs a) {
-  using TL = PagedTile<IT, D>;
+__global__ __launch_bounds__(64 * paged_waves(sizeof(IT), D, NR, SINGLE),
+                             paged_waves(sizeof(IT), D, NR, SINGLE) * (SINGLE ? 1 : paged_resident(D, NR)) / 4) void paged_attend_kernel(PagedAttendArgs a) {
+  using TL = PagedTile<IT, D, NR, SINGLE>;
   constexpr int NKT = TL::NKT, CH = TL::CH, NP = TL::NP, FPT = TL::FPT, VB = TL::VB, ROWB = TL::ROWB;
-  constexpr int NW = SINGLE ? PAGED_SINGLE_WAVES : PAGED_WAVES;
+  constexpr int NW = paged_waves(sizeof(IT), D, NR, SINGLE);
   constexpr int QROW = TL::QROW, OROW = TL::OROW, NT = 64 * NW, HD = D / 2;
   constexpr bool ALIAS = paged_alias(D, NR);
   extern __shared__ float4 paged_smem[];
   char* qs = (char*)paged_smem;                  // [16 NR][QROW], bf16: the same again for the low parts
   char* ql = qs + 16 * NR * QROW;
   float* osum = (float*)(qs + (ALIAS ? 0 : NR * TL::QBYTES));   // [NW][R][OROW]
+  float2* cs = (float2*)(qs + NR * TL::QBYTES);                // [nq][D / 2], before the sums: the queries' (cos, sin)
   __shared__ float wm[NW][16 * NR], wl[NW][16 * NR];
   const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
   const int l = lane & 15, lg = lane >> 4;
@@ -351,6 +357,66 @@ __global__ __launch_bounds__(64 * (SINGLE ? PAGED_SINGLE_WAVES : PAGED_WAVES),
   auto out_row = [&](int s, int r) {
     const int hr = head_of(r);
     return (((long)s * a.nq + r - hr * a.nq) * Hq + h * a.group + hr) * D;
+  };
+
+  // ---- a sequence's query rows, row g * nq + i query i of head h * group + g: a
+  // thread's pairs of 16-byte pieces D / 2 apart, the members of the rotated pairs
+  constexpr int HP = ROWB / 32, EPP = 16 / (int)sizeof(IT), QI = (16 * NR * HP + NT - 1) / NT;
+  u32x4 qr[QI][2];
+  static_assert(NT % HD == 0, "a thread's angles belong to one pair");
+  const double inv_freq = rot ? exp2(a.log2_theta * (-2.0 * (tid % HD) / D)) : 0.0;
+  auto load_q = [&](int s) {
+#pragma unroll
+    for (int k = 0; k < QI; ++k) {
+      const int e = k * NT + tid, r = min(e / HP, R - 1), hr = head_of(r);   // (rows past R repeat the last one)
+      const u32x4* q = (const u32x4*)(a.q + ((long)s * a.nq + r - hr * a.nq) * a.q_ts + (h * a.group + hr) * ROWB);
+      qr[k][0] = q[e % HP];
+      qr[k][1] = q[e % HP + HP];
+    }
+  };
+  auto stage_q = [&](int s) {   // rotated, in LDS; ends with a barrier
+    if (rot) {
+      for (int e = tid; e < a.nq * HD; e += NT) cs[e] = rope_cs(a.qpos[(long)s * a.nq + e / HD], inv_freq);
+      __syncthreads();
+    }
+#pragma unroll
+    for (int k = 0; k < QI; ++k) {
+      const int e = k * NT + tid, r = e / HP, j = e % HP * EPP;
+      if (16 * NR * HP % NT && r >= 16 * NR) break;
+      if (rot) {
+        const int i = min(r, R - 1);
+        const float2* c = cs + (i - head_of(i) * a.nq) * HD + j;
+        float x0[EPP], x1[EPP];
+        unpack16<IT>(qr[k][0], x0);
+        unpack16<IT>(qr[k][1], x1);
+#pragma unroll
+        for (int u = 0; u < EPP; ++u) {
+          const float y = x0[u] * c[u].x - x1[u] * c[u].y;
+          x1[u] = x1[u] * c[u].x + x0[u] * c[u].y;
+          x0[u] = y;
+        }
+        if constexpr (TL::B16) {
+          bf16x8 h0, h1, l0, l1;
+#pragma unroll
+          for (int u = 0; u < EPP; ++u) {
+            h0[u] = (__bf16)x0[u];
+            h1[u] = (__bf16)x1[u];
+            l0[u] = (__bf16)(x0[u] - (float)h0[u]);
+            l1[u] = (__bf16)(x1[u] - (float)h1[u]);
+          }
+          qr[k][0] = __builtin_bit_cast(u32x4, h0);
+          qr[k][1] = __builtin_bit_cast(u32x4, h1);
+          *(bf16x8*)(ql + r * QROW + 16 * (e % HP)) = l0;
+          *(bf16x8*)(ql + r * QROW + 16 * (e % HP + HP)) = l1;
+        } else {
+          qr[k][0] = u32x4{__float_as_uint(x0[0]), __float_as_uint(x0[1]), __float_as_uint(x0[2]), __float_as_uint(x0[3])};
+          qr[k][1] = u32x4{__float_as_uint(x1[0]), __float_as_uint(x1[1]), __float_as_uint(x1[2]), __float_as_uint(x1[3])};
+        }
+      }
+      *(u32x4*)(qs + r * QROW + 16 * (e % HP)) = qr[k][0];
+      *(u32x4*)(qs + r * QROW + 16 * (e % HP + HP)) = qr[k][1];
+    }
+    __syncthreads();
   };
 
   // ---- this workgroup's part of the line
@@ -475,67 +541,45 @@ __global__ __launch_bounds__(64 * (SINGLE ? PAGED_SINGLE_WAVES : PAGED_WAVES),
     u32x4 kp[NKT][NP];
     f32x4 bias[NKT];
     uint32_t vr[NKT * 4][VB / 4];
+    // (the offsets are opaque to the compiler, which would keep every sum of one with
+    // a constant in a register of its own instead of in the load)
     auto load_k = [&](const Tiles& k) {
+      int off = koff, boff = 16 * lg;
+      asm volatile("" : "+v"(off), "+v"(boff));
 #pragma unroll
       for (int kt = 0; kt < NKT; ++kt) {
         const auto r = paged_rows(a.c.k + k.row[kt] * ROWB, k.nv[kt] * ROWB);
 #pragma unroll
         for (int i = 0; i < NP; ++i)
-          kp[kt][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, koff + 64 * i, 0, 0));
+          kp[kt][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off + 64 * i, 0, 0));
         bias[kt] = __builtin_bit_cast(
             f32x4, __builtin_amdgcn_raw_buffer_load_b128(paged_rows(a.c.beta + k.row[kt], a.c.beta ? k.nv[kt] * 4 : 0),
-                                                         16 * lg, 0, 0));
+                                                         boff, 0, 0));
       }
     };
     auto load_v = [&](const Tiles& k) {
+      int off = voff;
+      asm volatile("" : "+v"(off));
 #pragma unroll
       for (int kt = 0; kt < NKT; ++kt) {
         const auto r = paged_rows(a.c.v + k.row[kt] * ROWB, k.nv[kt] * ROWB);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) buffer_words<VB>(r, voff + j * ROWB, vr[kt * 4 + j]);
+        for (int j = 0; j < 4; ++j) buffer_words<VB>(r, off + j * ROWB, vr[kt * 4 + j]);
       }
     };
     if (lo < hi) {
-      int u = lo + w;
+      int u = lo + w, i = SINGLE ? 0 : list_find(first, lo), at = lo;
+      load_q(base + i);
       Tiles cur = resolve(lookup(u));
       Chunk nxt = lookup(u + NW);
       load_k(cur);
       __builtin_amdgcn_sched_barrier(0);   // (loads stay in this order: their waits count the ones behind)
       load_v(cur);
       __builtin_amdgcn_sched_barrier(0);
-      for (int i = SINGLE ? 0 : list_find(first, lo), at = lo; at < hi; ++i) {
+      while (true) {   // the part's sequences that have entries
         const int len = len_of(i), s0 = SINGLE ? 0 : list_get(first, i), s1 = s0 + chunks(len);
-        if (len == 0) continue;
         const int s = base + i, end = min(s1, hi);
-        // ---- query rows into LDS: row g * nq + i is query i of head h * group + g
-        for (int e = tid; e < 16 * NR * HD; e += NT) {
-          const int r = e / HD, j = e % HD;
-          float x0 = 0.f, x1 = 0.f;
-          if (r < R) {
-            const int hr = head_of(r);
-            const long t = (long)s * a.nq + r - hr * a.nq;
-            const IT* q = (const IT*)(a.q + t * a.q_ts) + (long)(h * a.group + hr) * D;
-            x0 = to_f32(q[j]);
-            x1 = to_f32(q[j + HD]);
-            if (rot) {
-              const float2 cs = rope_cs(a.qpos[t], exp2(a.log2_theta * (-2.0 * j / D)));
-              const float y0 = x0 * cs.x - x1 * cs.y;
-              x1 = x1 * cs.x + x0 * cs.y;
-              x0 = y0;
-            }
-          }
-          if constexpr (TL::B16) {
-            const __bf16 h0 = (__bf16)x0, h1 = (__bf16)x1;
-            ((__bf16*)(qs + r * QROW))[j] = h0;
-            ((__bf16*)(qs + r * QROW))[j + HD] = h1;
-            ((__bf16*)(ql + r * QROW))[j] = (__bf16)(rot ? x0 - (float)h0 : 0.f);   // (as given: exact)
-            ((__bf16*)(ql + r * QROW))[j + HD] = (__bf16)(rot ? x1 - (float)h1 : 0.f);
-          } else {
-            ((float*)(qs + r * QROW))[j] = x0;
-            ((float*)(qs + r * QROW))[j + HD] = x1;
-          }
-        }
-        __syncthreads();
+        stage_q(s);
         f32x4 o[NR][FPT];
         float m[NR], ls[NR];
         int lim[NR];   // last entry that this lane's row sees
@@ -547,6 +591,7 @@ __global__ __launch_bounds__(64 * (SINGLE ? PAGED_SINGLE_WAVES : PAGED_WAVES),
 #pragma unroll
           for (int e = 0; e < FPT; ++e) o[rt][e] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
+        const int open = a.causal ? len - a.nq : len - 1;   // every row sees the entries up to this one
         while (cur.i == i) {
           u += NW;
           const Chunk third = lookup(u + NW);
@@ -561,8 +606,7 @@ __global__ __launch_bounds__(64 * (SINGLE ? PAGED_SINGLE_WAVES : PAGED_WAVES),
           for (int p = 0; p < NP; ++p)
 #pragma unroll
             for (int rt = 0; rt < NR; ++rt) {
-              const int qoff = (16 * rt + l) * QROW + 64 * p + 16 * lg;
-              const u32x4 qv = *(const u32x4*)(qs + qoff);
+              const u32x4 qv = *(const u32x4*)(qs + (16 * rt + l) * QROW + 64 * p + 16 * lg);
 #pragma unroll
               for (int kt = 0; kt < NKT; ++kt) {
                 if constexpr (TL::B16) {
@@ -575,84 +619,117 @@ __global__ __launch_bounds__(64 * (SINGLE ? PAGED_SINGLE_WAVES : PAGED_WAVES),
                                                                      __uint_as_float(qv[e]), x[rt][kt], 0, 0, 0);
                 }
               }
-              if constexpr (TL::B16) {
-                const u32x4 qw = *(const u32x4*)(ql + qoff);
+            }
+          if (TL::B16 && rot) {
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+              for (int rt = 0; rt < NR; ++rt) {
+                const u32x4 qv = *(const u32x4*)(ql + (16 * rt + l) * QROW + 64 * p + 16 * lg);
 #pragma unroll
                 for (int kt = 0; kt < NKT; ++kt)
                   x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                      __builtin_bit_cast(bf16x8, kp[kt][p]), __builtin_bit_cast(bf16x8, qw), x[rt][kt], 0, 0, 0);
+                      __builtin_bit_cast(bf16x8, kp[kt][p]), __builtin_bit_cast(bf16x8, qv), x[rt][kt], 0, 0, 0);
               }
-            }
+          }
           f32x4 bc[NKT];
 #pragma unroll
           for (int kt = 0; kt < NKT; ++kt) bc[kt] = bias[kt];
           const Tiles next = resolve(nxt);
           load_k(next);
           __builtin_amdgcn_sched_barrier(0);
-          // ---- online softmax of this lane's rows over its entries
+          // ---- online softmax of this lane's rows over its entries.  The sums stay
+          // relative to m, a logit of the row, until one exceeds it by PAGED_SLACK.
+          bool full = cur.c * CH + CH - 1 <= open;
+#pragma unroll
+          for (int kt = 0; kt < NKT; ++kt) full = full && cur.nv[kt] == 16;
+          float cm[NR];
+          bool grows = false;
 #pragma unroll
           for (int rt = 0; rt < NR; ++rt) {
-            float cm = -INFINITY;
 #pragma unroll
-            for (int kt = 0; kt < NKT; ++kt) {
-              const int seen = min(cur.nv[kt], lim[rt] - (cur.c * CH + 16 * kt) + 1) - 4 * lg;
+            for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                x[rt][kt][j] = j < seen ? fmaf(x[rt][kt][j], a.scale, bc[kt][j]) : -INFINITY;
-                cm = fmaxf(cm, x[rt][kt][j]);
+              for (int j = 0; j < 4; ++j) x[rt][kt][j] = fmaf(x[rt][kt][j], a.scale, bc[kt][j]);
+            if (!full) {
+#pragma unroll
+              for (int kt = 0; kt < NKT; ++kt) {
+                const int seen = min(cur.nv[kt], lim[rt] - (cur.c * CH + 16 * kt) + 1) - 4 * lg;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[rt][kt][j] = j < seen ? x[rt][kt][j] : -INFINITY;
               }
             }
-            const float mn = fmaxf(m[rt], groups_max(cm)), ref = mn == -INFINITY ? 0.f : mn;
-            const float al = exp_of(m[rt] - ref);
-            m[rt] = mn;
-            float cs = 0.f;
+            cm[rt] = -INFINITY;
+#pragma unroll
+            for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) cm[rt] = fmaxf(cm[rt], x[rt][kt][j]);
+            cm[rt] = groups_max(cm[rt]);
+            grows = grows || cm[rt] > m[rt] + PAGED_SLACK;
+          }
+          if (__any(grows)) {
+#pragma unroll
+            for (int rt = 0; rt < NR; ++rt) {
+              const float mn = fmaxf(m[rt], cm[rt]);
+              const float al = exp_of(m[rt] - (mn == -INFINITY ? 0.f : mn));
+              m[rt] = mn;
+              ls[rt] *= al;
+#pragma unroll
+              for (int e = 0; e < FPT; ++e) o[rt][e] *= al;
+            }
+          }
+#pragma unroll
+          for (int rt = 0; rt < NR; ++rt) {
+            const float ref = m[rt] == -INFINITY ? 0.f : m[rt];
 #pragma unroll
             for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 x[rt][kt][j] = exp_of(x[rt][kt][j] - ref);
-                cs += x[rt][kt][j];
+                ls[rt] += x[rt][kt][j];   // (this lane's entries; its lane groups are added at the end)
               }
-            ls[rt] = ls[rt] * al + cs;   // (this lane's entries; its lane groups are added at the end)
-#pragma unroll
-            for (int e = 0; e < FPT; ++e) o[rt][e] *= al;
           }
           // ---- P.V
           if constexpr (TL::B16) {
-            bf16x8 ph[NR], pl[NR];
 #pragma unroll
-            for (int rt = 0; rt < NR; ++rt)
+            for (int k2 = 0; k2 < NKT; k2 += 2) {
+              bf16x8 ph[NR], pl[NR];
 #pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const float p = x[rt][k >> 2][k & 3];
-                ph[rt][k] = (__bf16)p;
-                pl[rt][k] = (__bf16)(p - (float)ph[rt][k]);
-              }
+              for (int rt = 0; rt < NR; ++rt)
 #pragma unroll
-            for (int e = 0; e < FPT; e += 2) {   // an even and an odd feature of one word
-              u32x4 t0, t1;
+                for (int k = 0; k < 8; ++k) {
+                  const float p = x[rt][k2 + (k >> 2)][k & 3];
+                  ph[rt][k] = (__bf16)p;
+                  pl[rt][k] = (__bf16)(p - (float)ph[rt][k]);
+                }
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                t0[k] = __builtin_amdgcn_perm(vr[2 * k + 1][e >> 1], vr[2 * k][e >> 1], 0x05040100u);
-                t1[k] = __builtin_amdgcn_perm(vr[2 * k + 1][e >> 1], vr[2 * k][e >> 1], 0x07060302u);
-              }
-              const bf16x8 w0 = __builtin_bit_cast(bf16x8, t0), w1 = __builtin_bit_cast(bf16x8, t1);
+              for (int e = 0; e < FPT; e += 2) {   // an even and an odd feature of one word
+                u32x4 t0, t1;
 #pragma unroll
-              for (int rt = 0; rt < NR; ++rt) {
-                o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w0, ph[rt], o[rt][e], 0, 0, 0);
-                o[rt][e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w1, ph[rt], o[rt][e + 1], 0, 0, 0);
-                o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w0, pl[rt], o[rt][e], 0, 0, 0);
-                o[rt][e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w1, pl[rt], o[rt][e + 1], 0, 0, 0);
+                for (int k = 0; k < 4; ++k) {
+                  const uint32_t a0 = vr[4 * k2 + 2 * k][e >> 1], a1 = vr[4 * k2 + 2 * k + 1][e >> 1];
+                  t0[k] = __builtin_amdgcn_perm(a1, a0, 0x05040100u);
+                  t1[k] = __builtin_amdgcn_perm(a1, a0, 0x07060302u);
+                }
+                const bf16x8 w0 = __builtin_bit_cast(bf16x8, t0), w1 = __builtin_bit_cast(bf16x8, t1);
+#pragma unroll
+                for (int rt = 0; rt < NR; ++rt) {
+                  o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w0, ph[rt], o[rt][e], 0, 0, 0);
+                  o[rt][e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w1, ph[rt], o[rt][e + 1], 0, 0, 0);
+                  o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w0, pl[rt], o[rt][e], 0, 0, 0);
+                  o[rt][e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w1, pl[rt], o[rt][e + 1], 0, 0, 0);
+                }
               }
             }
           } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int k = 0; k < 4 * NKT; ++k)
 #pragma unroll
               for (int e = 0; e < FPT; ++e)
 #pragma unroll
                 for (int rt = 0; rt < NR; ++rt)
-                  o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[j][e]), x[rt][0][j], o[rt][e], 0, 0, 0);
+                  o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[k][e]), x[rt][k >> 2][k & 3],
+                                                                  o[rt][e], 0, 0, 0);
           }
           __builtin_amdgcn_sched_barrier(0);
           load_v(next);
@@ -660,7 +737,10 @@ __global__ __launch_bounds__(64 * (SINGLE ? PAGED_SINGLE_WAVES : PAGED_WAVES),
           cur = next;
           nxt = third;
         }
-        // ---- the waves' sums into LDS, then added
+        // ---- the waves' sums into LDS, then added, the next rows on their way
+        const bool last = SINGLE || end == hi;
+        const int ni = last ? i : list_find(first, end);
+        if (!last) load_q(base + ni);
 #pragma unroll
         for (int rt = 0; rt < NR; ++rt) {
           ls[rt] += __shfl_xor(ls[rt], 16);
@@ -726,8 +806,10 @@ __global__ __launch_bounds__(64 * (SINGLE ? PAGED_SINGLE_WAVES : PAGED_WAVES),
             goes_on = p;
           }
         }
+        if (last) break;
+        i = ni;
         at = end;
-        if (ALIAS) __syncthreads();   // the sums have been read before the next sequence's query rows
+        if (ALIAS || rot) __syncthreads();   // the sums have been read before the next sequence's rows or angles
       }
     }
     if (SINGLE) break;
