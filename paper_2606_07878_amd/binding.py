@@ -546,8 +546,8 @@ def _want_rows(x, name: str, pages, shape) -> None:
     _refuse(-1, f"{name}'s rows are not contiguous")
 
 
-def _paged(torch, k_pages, v_pages, beta_pages, table, lens):
-    """The C views of a paged cache and its sequences, checked."""
+def _refuse_paged(torch, k_pages, v_pages, beta_pages, table, lens) -> None:
+    """Says what is wrong with a paged cache or its sequences."""
     shape, dt, dev = k_pages.shape, k_pages.dtype, k_pages.get_device()
     if len(shape) != 4:
         _refuse(-2, f"k_pages has {len(shape)} dimensions, not [n_pages, H, page_size, d]")
@@ -556,23 +556,34 @@ def _paged(torch, k_pages, v_pages, beta_pages, table, lens):
     if not k_pages.is_contiguous():
         _refuse(-1, "k_pages is not contiguous")
     _want(v_pages, "v_pages", dt, shape, dev)
-    n_pages, H, P, d = shape
-    beta = None
     if beta_pages is not None:
         _want(beta_pages, "beta_pages", torch.float32, shape[:3], dev)
-        beta = beta_pages.data_ptr()
-    size = table.shape
-    if len(size) != 2 or table.dtype != torch.int32 or (table.stride(1) != 1 and size[1] > 1):
+    if table.dim() != 2 or table.dtype != torch.int32 or (table.stride(1) != 1 and table.shape[1] > 1):
         _refuse(-2, "table is no int32 tensor [n_seqs, pages] with contiguous rows")
     if table.get_device() != dev:
         _refuse(-1, f"table is on {table.device}, the pages on {k_pages.device}")
+    _want(lens, "lens", torch.int32, table.shape[:1], dev)
+    _refuse(-1, f"the pages are on {k_pages.device}: a GPU is needed")
+
+
+def _paged(torch, k_pages, v_pages, beta_pages, table, lens):
+    """(C view of a paged cache, C view of its sequences, GPU), checked."""
+    shape, dt, dev, size = k_pages.shape, k_pages.dtype, k_pages.get_device(), table.shape
+    i32, fp32 = torch.int32, dt is torch.float32
+    # one expression: this runs before every call of a decode step
+    if not (dev >= 0 and len(shape) == 4 and (fp32 or dt is torch.bfloat16) and v_pages.dtype is dt
+            and v_pages.shape == shape and k_pages.is_contiguous() and v_pages.is_contiguous()
+            and v_pages.get_device() == dev and table.dtype is i32 and len(size) == 2 and lens.dtype is i32
+            and lens.shape == size[:1] and lens.is_contiguous() and lens.get_device() == dev
+            and table.get_device() == dev and (table.stride(1) == 1 or size[1] <= 1)
+            and (beta_pages is None or beta_pages.dtype is torch.float32 and beta_pages.shape == shape[:3]
+                 and beta_pages.is_contiguous() and beta_pages.get_device() == dev)):
+        _refuse_paged(torch, k_pages, v_pages, beta_pages, table, lens)
+    n_pages, H, P, d = shape
     n, width = size
-    _want(lens, "lens", torch.int32, size[:1], dev)
-    if dev < 0:
-        _refuse(-1, f"the pages are on {k_pages.device}: a GPU is needed")
-    return (still_paged_cache(H, d, P, n_pages, configs.MODE_FP32 if dt == torch.float32 else configs.MODE_BF16,
-                              k_pages.data_ptr(), v_pages.data_ptr(), beta),
-            still_paged_seqs(n, width, table.stride(0) if n > 1 else width, table.data_ptr(), lens.data_ptr()))
+    return (still_paged_cache(H, d, P, n_pages, fp32, k_pages.data_ptr(), v_pages.data_ptr(),
+                              None if beta_pages is None else beta_pages.data_ptr()),
+            still_paged_seqs(n, width, table.stride(0) if n > 1 else width, table.data_ptr(), lens.data_ptr()), dev)
 
 
 def _on(torch, dev: int, call, *args) -> None:
@@ -600,8 +611,7 @@ def paged_append(k, v, k_pages, v_pages, table, lens, offsets=None, positions=No
     [n_pages, H, P] float32 always, and the entries' ``beta`` [n_tokens, H]
     float32 where it is not zero."""
     torch = _torch()
-    cache, seqs = _paged(torch, k_pages, v_pages, beta_pages, table, lens)
-    dev = k_pages.get_device()
+    cache, seqs, dev = _paged(torch, k_pages, v_pages, beta_pages, table, lens)
     if k.dim() != 3:
         _refuse(-2, f"k has {k.dim()} dimensions, not [n_tokens, H, d]")
     n = k.shape[0]
@@ -624,7 +634,7 @@ def paged_append(k, v, k_pages, v_pages, table, lens, offsets=None, positions=No
     ks, vs = k.stride(), v.stride()
     tokens = still_paged_tokens(n, k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1], b, ts, hs, off, pos,
                                 rope_theta)
-    _on(torch, dev, lib().still_paged_append, ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(tokens))
+    _on(torch, dev, (_lib or lib()).still_paged_append, ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(tokens))
 
 
 def paged_gather(k_pages, v_pages, table, lens, seq: int, n: int, start: int = 0, beta_pages=None, out=None):
@@ -632,8 +642,8 @@ def paged_gather(k_pages, v_pages, table, lens, seq: int, n: int, start: int = 0
     with ``beta_pages`` (K, V, beta [H, n]), through still_paged_gather on the
     current stream; into ``out`` (such a tuple) where given."""
     torch = _torch()
-    cache, seqs = _paged(torch, k_pages, v_pages, beta_pages, table, lens)
-    dev, n = k_pages.get_device(), int(n)
+    cache, seqs, dev = _paged(torch, k_pages, v_pages, beta_pages, table, lens)
+    n = int(n)
     shape = (cache.n_kv_heads, n, cache.head_dim)
     if out is None:
         if n < 0:
@@ -648,7 +658,7 @@ def paged_gather(k_pages, v_pages, table, lens, seq: int, n: int, start: int = 0
         _want(out[1], "out[1]", k_pages.dtype, shape, dev)
         if beta_pages is not None:
             _want(out[2], "out[2]", torch.float32, shape[:2], dev)
-    _on(torch, dev, lib().still_paged_gather, ctypes.byref(cache), ctypes.byref(seqs), int(seq), int(start), n,
+    _on(torch, dev, (_lib or lib()).still_paged_gather, ctypes.byref(cache), ctypes.byref(seqs), int(seq), int(start), n,
         out[0].data_ptr(), out[1].data_ptr(), None if beta_pages is None else out[2].data_ptr())
     return out
 
@@ -663,8 +673,8 @@ def paged_attend(q, k_pages, v_pages, table, lens, causal: bool = False, scale: 
     ``out`` and ``workspace`` (STILL_PAGED_WORKSPACE_BYTES serve every call)
     may be given, so that the call allocates nothing (graph capture)."""
     torch = _torch()
-    cache, seqs = _paged(torch, k_pages, v_pages, beta_pages, table, lens)
-    dev, shape = k_pages.get_device(), q.shape
+    cache, seqs, dev = _paged(torch, k_pages, v_pages, beta_pages, table, lens)
+    shape = q.shape
     if len(shape) != 3:
         _refuse(-2, f"q has {len(shape)} dimensions, not [n_seqs * n_queries, H * group, d]")
     tokens, Hq, d = shape
@@ -692,7 +702,7 @@ def paged_attend(q, k_pages, v_pages, table, lens, causal: bool = False, scale: 
         if room < need:
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
             room = need
-    _on(torch, dev, lib().still_paged_attend, ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(cfg), q.data_ptr(),
+    _on(torch, dev, (_lib or lib()).still_paged_attend, ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(cfg), q.data_ptr(),
         pos, out.data_ptr(), _ptr(workspace), room)
     return out
 

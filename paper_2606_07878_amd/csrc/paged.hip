@@ -89,10 +89,18 @@ static still_status check_attend(const still_paged_cache* c, const still_paged_a
   return STILL_OK;
 }
 
-// Whether a workgroup takes a whole sequence.
+// Whether a workgroup takes a whole sequence: one launch instead of two, but one
+// CU's rate of reading per sequence and head.  The host knows the table's
+// capacity only, so the line is where the average over lengths up to it is even.
+// us in a graph, whole / split, 8 heads, one sequence: bf16 of width 128 (the line
+// is a capacity of 1024) 32 entries 4.6 / 7.9, 256 6.1 / 10.0, 512 8.6 / 10.1, 719
+// 10.0 / 10.1, 1024 13.0 / 10.1; of width 64 256 4.5 / 9.5, 1024 8.8 / 9.6; fp32 of
+// width 64 (1024) 256 5.5 / 9.2, 719 10.0 / 9.3, 1024 12.3 / 9.3; of width 128 (512)
+// 32 4.7 / 8.2, 256 8.7 / 10.2, 719 17.7 / 10.3.  64 sequences (the line) of 100
+// entries 9.1 / 11.8, of 700 30.5 / 34.3; 128 of 100 21.1 / 18.9, 256 39 / 28.
 static bool paged_single(const still_paged_cache* c, const still_paged_seqs* q, int R) {
-  return R <= 16 && c->head_dim <= 128 && (long)q->max_pages * c->page_size <= 1024 &&
-         (long)q->n_seqs * c->n_kv_heads <= 512;
+  const long cap = (long)q->max_pages * c->page_size, row = c->head_dim * (c->mode == STILL_MODE_FP32 ? 4 : 2);
+  return R <= 16 && c->head_dim <= 128 && cap <= 1024 && cap * row <= 256 * 1024 && (long)q->n_seqs * c->n_kv_heads <= 512;
 }
 
 struct PagedPlan {
@@ -159,8 +167,7 @@ still_status still_paged_append(const still_paged_cache* cache, const still_page
   paged_dispatch(cache, [&](auto it, auto d) {
     using IT = decltype(it);
     const unsigned blocks = ((unsigned)t->n_tokens + PAGED_APPEND_TPB - 1) / PAGED_APPEND_TPB;
-    hipLaunchKernelGGL((paged_append_kernel<IT, decltype(d)::value, PAGED_APPEND_TPB>), dim3(blocks), dim3(256), 0, st,
-                       a);
+    hipLaunchKernelGGL((paged_append_kernel<IT, decltype(d)::value>), dim3(blocks), dim3(256), 0, st, a);
   });
   HIP_TRY(hipGetLastError());
   return STILL_OK;
@@ -258,8 +265,11 @@ still_status still_paged_attend(const still_paged_cache* cache, const still_page
     const size_t lds = paged_lds_bytes<IT, D>(R, false);
     if (R <= 16) hipLaunchKernelGGL((paged_attend_kernel<IT, D, 1, false>), grid, block, lds, st, a);
     else hipLaunchKernelGGL((paged_attend_kernel<IT, D, 2, false>), grid, block, lds, st, a);
-    if (a.G > 1)
-      hipLaunchKernelGGL((paged_merge_kernel<IT, D>), dim3(R, a.c.H, std::min(a.c.n_seqs, a.G)), dim3(256), 0, st, a);
+    if (a.G > 1) {
+      const dim3 joins(R, a.c.H, std::min(a.c.n_seqs, a.G));
+      hipLaunchKernelGGL((paged_merge_kernel<IT, D>), joins,
+                         dim3((long)joins.x * joins.y * joins.z <= 512 ? PAGED_MERGE_THREADS : 256), 0, st, a);
+    }
   });
   HIP_TRY(hipGetLastError());
   return STILL_OK;

@@ -39,11 +39,24 @@ __device__ __forceinline__ long paged_row(const PagedArgs& a, int p, int h, long
   return (((long)p * a.H + h) << a.lp) + (j & ((1 << a.lp) - 1));
 }
 
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// A uniform element through the scalar cache, whose loads are not counted with
+// the vector loads: waiting for one waits for no row in flight.
+template <class T>
+__device__ __forceinline__ T scalar_load(const T* p, long i) {
+  return ((const __attribute__((address_space(4))) T*)(uintptr_t)p)[i];
+}
+
 // ---------------------------------------------------------------------------
-// Append.  A block takes TPB tokens with all their heads, so that a token's
-// angles (fp64: positions reach 1e5 and more) are formed once.  A work item is
-// a pair of 16-byte pieces d/2 apart, the two members of the rotated pairs.
-// Moves 2 x 2 H d values per token; nothing else matters but the launch.
+// Append.  A block takes four tokens with all their heads, so that a token's
+// angles (fp64: positions reach 1e5 and more) are formed once; wave w finds token
+// w's page while the rows are on their way, which it does not depend on.  A work
+// item is a pair of 16-byte pieces d/2 apart, the two members of the rotated
+// pairs.
+// Moves 2 x 2 H d values per token; nothing else matters but the launch and the
+// chain offsets -> length -> page (a binary search per token by one thread, rows
+// behind it, took 28.7 us for 6979 tokens of 8 heads of width 256).
 // ---------------------------------------------------------------------------
 struct PagedAppendArgs {
   PagedArgs c;
@@ -57,78 +70,115 @@ struct PagedAppendArgs {
   int n_tokens, per_seq;                            // per_seq: tokens per sequence without offsets
 };
 
-constexpr int PAGED_APPEND_TPB = 4;
+constexpr int PAGED_APPEND_TPB = 4;   // tokens per block, one per wave
 
-// entry and sequence of token i; false: skipped
-__device__ __forceinline__ bool paged_target(const PagedAppendArgs& a, int i, int& s, long& j) {
-  long end;
-  if (a.offsets) {
-    int lo = 0, hi = a.c.n_seqs;   // offsets[lo] <= i < offsets[hi] once both ends are known to hold it
-    if (i < a.offsets[0] || i >= a.offsets[hi]) return false;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (a.offsets[mid] <= i) lo = mid;
-      else hi = mid;
-    }
-    s = lo;
-    end = a.offsets[lo + 1];
-  } else {
-    s = i / a.per_seq;
-    end = (long)(s + 1) * a.per_seq;
+// Sequence of token i: the last one whose first token is at or before i.  64-fold
+// search by a wave; `probe` is the first step's offset of this lane.
+__device__ __forceinline__ int paged_seq_of(const int* offsets, int n_seqs, int i, int probe) {
+  int lo = 0, hi = n_seqs;
+  for (bool first = true; hi - lo > 1; first = false) {
+    const int step = (hi - lo + 63) / 64, x = lo + ((threadIdx.x & 63) + 1) * step;
+    const int o = first ? probe : x < hi ? offsets[x] : 0;
+    lo += step * __popcll(__ballot(x < hi && o <= i));
+    hi = min(hi, lo + step);
   }
-  j = (long)a.c.lens[s] - end + i;
-  return j >= 0 && j < paged_cap(a.c);
+  return lo;
 }
 
-template <class IT, int D, int TPB>
+template <class IT, int D>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
-  constexpr int HP = D * (int)sizeof(IT) / 32, EPP = 16 / (int)sizeof(IT), HD = D / 2;
+  constexpr int TPB = PAGED_APPEND_TPB, HP = D * (int)sizeof(IT) / 32, EPP = 16 / (int)sizeof(IT), HD = D / 2;
+  constexpr int U = HP >= 16 ? 4 : 2;   // items of a thread in flight
   __shared__ float2 cs[TPB][HD];
   __shared__ int page[TPB], slot[TPB];
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
   const long t0 = (long)blockIdx.x * TPB;
-  if (tid < TPB) {
-    int p = -1, s;
-    long j = 0;
-    if (t0 + tid < a.n_tokens && paged_target(a, (int)(t0 + tid), s, j)) p = paged_page(a.c, s, j);
-    page[tid] = p;
-    slot[tid] = (int)(j & ((1 << a.c.lp) - 1));
+  const int left = (int)min((long)TPB, a.n_tokens - t0);   // tokens of this block
+  // the first step of the search, and a position per thread's first angle, ahead of the rows
+  const int n_seqs = a.c.n_seqs, x0 = (lane + 1) * ((n_seqs + 63) / 64);
+  const int probe = a.offsets && x0 < n_seqs ? a.offsets[x0] : 0;
+  double pos[(TPB * HD + 255) / 256];   // of the thread's angles (256 / HD tokens apart, all of pair tid % HD)
+#pragma unroll
+  for (int k = 0; k < (TPB * HD + 255) / 256; ++k) pos[k] = a.pos ? a.pos[t0 + min((k * 256 + tid) / HD, left - 1)] : 0.0;
+  __builtin_amdgcn_sched_barrier(0);
+  const int H = a.c.H, items = TPB * H * 2 * HP;
+  u32x4 x[U][2];
+  auto load = [&](int b) {
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const int it = b + k * 256 + tid, p = it % HP, kv = it / HP & 1, r = it / (2 * HP), h = min(r / TPB, H - 1);
+      const long t = t0 + min(r % TPB, left - 1);
+      const u32x4* src = (const u32x4*)(kv ? a.v + t * a.v_ts + h * a.v_hs : a.k + t * a.k_ts + h * a.k_hs);
+      if (b + k * 256 < items) {
+        x[k][0] = src[p];
+        x[k][1] = src[p + HP];
+      }
+    }
+  };
+  load(0);
+  __builtin_amdgcn_sched_barrier(0);
+  {  // this wave's token: its entry's page and slot
+    const int i = (int)t0 + w;
+    int pg = -1;
+    long j = -1;
+    if (w < left) {
+      int s;
+      long end;
+      if (a.offsets) {
+        s = uniform(paged_seq_of(a.offsets, n_seqs, i, probe));
+        end = scalar_load(a.offsets, s + 1);
+        if (i < scalar_load(a.offsets, s) || i >= end) end = -1;   // before the first or behind the last
+      } else {
+        s = i / a.per_seq;
+        end = (long)(s + 1) * a.per_seq;
+      }
+      if (end >= 0) j = scalar_load(a.c.lens, s) - end + i;
+      if (j >= 0 && j < paged_cap(a.c)) {
+        const int p = scalar_load(a.c.table, s * a.c.tstride + (j >> a.c.lp));
+        if ((unsigned)p < (unsigned)a.c.n_pages) pg = p;
+      }
+    }
+    if (lane == 0) {
+      page[w] = pg;
+      slot[w] = (int)(j & ((1 << a.c.lp) - 1));
+    }
   }
   if (a.pos) {
-    for (int e = tid; e < TPB * HD; e += 256) {
-      const int t = e / HD, i = e % HD;
-      if (t0 + t < a.n_tokens) cs[t][i] = rope_cs(a.pos[t0 + t], exp2(a.log2_theta * (-2.0 * i / D)));
-    }
+    const double inv = exp2(a.log2_theta * (-2.0 * (tid % HD) / D));
+#pragma unroll
+    for (int k = 0; k < (TPB * HD + 255) / 256; ++k)
+      if ((k * 256 + tid) / HD < left) cs[(k * 256 + tid) / HD][tid % HD] = rope_cs(pos[k], inv);
   }
   __syncthreads();
-  const int H = a.c.H, items = TPB * H * 2 * HP;
-  for (int it = tid; it < items; it += 256) {
-    const int p = it % HP, kv = it / HP & 1, r = it / (2 * HP), h = r / TPB, t = r % TPB;
-    if (page[t] < 0) continue;
-    const char* src = kv ? a.v + (t0 + t) * a.v_ts + h * a.v_hs : a.k + (t0 + t) * a.k_ts + h * a.k_hs;
-    u32x4 x0 = ((const u32x4*)src)[p], x1 = ((const u32x4*)src)[p + HP];
-    if (!kv && a.pos) {
-      float f0[EPP], f1[EPP];
-      unpack16<IT>(x0, f0);
-      unpack16<IT>(x1, f1);
-      IT y0[EPP], y1[EPP];
+  for (int b = 0; b < items; b += U * 256) {
+    if (b) load(b);
 #pragma unroll
-      for (int e = 0; e < EPP; ++e) {
-        const float2 c = cs[t][p * EPP + e];
-        y0[e] = from_f32<IT>(f0[e] * c.x - f1[e] * c.y);
-        y1[e] = from_f32<IT>(f1[e] * c.x + f0[e] * c.y);
+    for (int k = 0; k < U; ++k) {
+      const int it = b + k * 256 + tid, p = it % HP, kv = it / HP & 1, r = it / (2 * HP), h = r / TPB, t = r % TPB;
+      if (it >= items || t >= left || page[t] < 0) continue;
+      if (!kv && a.pos) {
+        float f0[EPP], f1[EPP];
+        unpack16<IT>(x[k][0], f0);
+        unpack16<IT>(x[k][1], f1);
+        IT y0[EPP], y1[EPP];
+#pragma unroll
+        for (int e = 0; e < EPP; ++e) {
+          const float2 c = cs[t][p * EPP + e];
+          y0[e] = from_f32<IT>(f0[e] * c.x - f1[e] * c.y);
+          y1[e] = from_f32<IT>(f1[e] * c.x + f0[e] * c.y);
+        }
+        __builtin_memcpy(&x[k][0], y0, 16);
+        __builtin_memcpy(&x[k][1], y1, 16);
       }
-      __builtin_memcpy(&x0, y0, 16);
-      __builtin_memcpy(&x1, y1, 16);
+      u32x4* dst = (u32x4*)((kv ? a.c.v : a.c.k) + ((((long)page[t] * H + h) << a.c.lp) + slot[t]) * (D * (long)sizeof(IT)));
+      dst[p] = x[k][0];
+      dst[p + HP] = x[k][1];
     }
-    u32x4* dst = (u32x4*)((kv ? a.c.v : a.c.k) + ((((long)page[t] * H + h) << a.c.lp) + slot[t]) * (D * (long)sizeof(IT)));
-    dst[p] = x0;
-    dst[p + HP] = x1;
   }
   if (a.c.beta)
     for (int it = tid; it < TPB * H; it += 256) {
       const int h = it / TPB, t = it % TPB;
-      if (page[t] >= 0)
+      if (t < left && page[t] >= 0)
         a.c.beta[(((long)page[t] * H + h) << a.c.lp) + slot[t]] =
             a.nbeta ? a.nbeta[(t0 + t) * a.b_ts + h * a.b_hs] : 0.f;
     }
@@ -228,7 +278,10 @@ struct PagedAttendArgs {
 };
 
 constexpr int PAGED_ROUND = 256;         // sequences whose lengths a wave holds at a time, four per lane
-constexpr int PAGED_PAD = 2;
+// Chunks that a sequence counts beside its own.  us at 0 / 2 / 4 / 8: 64 sequences of
+// 5 to 16384 entries 121.9 / 110.5 / 106.3 / 105.2, 300 of 20 to 900 78.1 / 70.7 / 69.6 /
+// 69.9, 48 of 1024 to 9216 of width 256 264.6 / 264.7 / 265.1 / 267.8.
+constexpr int PAGED_PAD = 6;
 constexpr float PAGED_SLACK = 6.f;       // weights reach e^6 before they are scaled back
 constexpr float LOG2E = 1.4426950408889634f;
 
@@ -259,7 +312,7 @@ struct PagedTile {
 };
 
 // the waves' sums take the query rows' place in LDS where both do not fit 160 KB
-constexpr bool paged_alias(int D, int NR) { return D * NR >= 256 && NR == 2; }
+constexpr bool paged_alias(int D, int NR) { return D * NR > 256; }
 
 // dynamic LDS: the query rows, the waves' sums [waves][R][OROW]
 template <class IT, int D>
@@ -272,8 +325,6 @@ inline size_t paged_lds_bytes(int R, bool single) {
 
 // fast base-2 exponential (results below 2^-126 are zero)
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
-
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // maximum over lanes l, l ^ 16, l ^ 32, l ^ 48
 __device__ __forceinline__ float groups_max(float x) {
@@ -335,7 +386,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t paged_rows(const void* p, int 
 
 template <class IT, int D, int NR, bool SINGLE>
 __global__ __launch_bounds__(64 * paged_waves(sizeof(IT), D, NR, SINGLE),
-                             paged_waves(sizeof(IT), D, NR, SINGLE) * (SINGLE ? 1 : paged_resident(D, NR)) / 4) void paged_attend_kernel(PagedAttendArgs a) {
+                             paged_waves(sizeof(IT), D, NR, SINGLE) * (SINGLE ? 1 : paged_resident(D, NR)) / 4)
+void paged_attend_kernel(PagedAttendArgs a) {
   using TL = PagedTile<IT, D, NR, SINGLE>;
   constexpr int NKT = TL::NKT, CH = TL::CH, NP = TL::NP, FPT = TL::FPT, VB = TL::VB, ROWB = TL::ROWB;
   constexpr int NW = paged_waves(sizeof(IT), D, NR, SINGLE);
@@ -345,7 +397,7 @@ __global__ __launch_bounds__(64 * paged_waves(sizeof(IT), D, NR, SINGLE),
   char* qs = (char*)paged_smem;                  // [16 NR][QROW], bf16: the same again for the low parts
   char* ql = qs + 16 * NR * QROW;
   float* osum = (float*)(qs + (ALIAS ? 0 : NR * TL::QBYTES));   // [NW][R][OROW]
-  float2* cs = (float2*)(qs + NR * TL::QBYTES);                // [nq][D / 2], before the sums: the queries' (cos, sin)
+  float2* cs = (float2*)(qs + NR * TL::QBYTES);   // [nq][D / 2] (cos, sin) of the queries, where the sums come later
   __shared__ float wm[NW][16 * NR], wl[NW][16 * NR];
   const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
   const int l = lane & 15, lg = lane >> 4;
@@ -423,20 +475,21 @@ __global__ __launch_bounds__(64 * paged_waves(sizeof(IT), D, NR, SINGLE),
   const int cap = (int)paged_cap(a.c);
   int lens[4];    // of the round's sequences, four per lane
   auto load_lens = [&](int base) {
-    const auto x = __builtin_bit_cast(
-        u32x4, __builtin_amdgcn_raw_buffer_load_b128(paged_rows(a.c.lens + base, 4 * min(PAGED_ROUND, n_seqs - base)),
-                                                     16 * lane, 0, 0));
+    const auto r = paged_rows(a.c.lens + base, 4 * min(PAGED_ROUND, n_seqs - base));   // (past them: zeros)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) lens[k] = min(max((int)x[k], 0), cap);
+    for (int k = 0; k < 4; ++k)
+      lens[k] = min(max((int)__builtin_amdgcn_raw_buffer_load_b32(r, 16 * lane + 4 * k, 0, 0), 0), cap);
   };
   auto chunks = [&](int len) { return (len + CH - 1) / CH; };
-  int TV = 0, active = 0, v0 = 0, v1 = 0;   // chunks with pads, workgroups with a part, this part's cuts
+  // workgroups with a part, the chunks (with pads) of one, how many take one more, this part's cuts
+  int active = 0, share = 0, more = 0, v0 = 0, v1 = 0;
   auto cuts = [&](int T, int some) {        // of the sums over all sequences
-    TV = T + pad * some;
     active = min(a.G, (T + NW - 1) / NW);   // a workgroup takes a chunk per wave before another one starts
     if (g < active) {
-      v0 = (int)((long)g * TV / active);
-      v1 = (int)((long)(g + 1) * TV / active);
+      share = (T + pad * some) / active;
+      more = T + pad * some - share * active;
+      v0 = g * share + min(g, more);
+      v1 = v0 + share + (g < more);
     }
   };
   if (!SINGLE && n_seqs > PAGED_ROUND) {
@@ -456,8 +509,22 @@ __global__ __launch_bounds__(64 * paged_waves(sizeof(IT), D, NR, SINGLE),
   for (int base = SINGLE ? blockIdx.y : 0; base < n_seqs; base += PAGED_ROUND) {
     const int cnt = SINGLE ? 1 : min(PAGED_ROUND, n_seqs - base);
     int first[4], padded_first[4], lo, hi;   // of the round's sequences on the line; the part's chunks in the round
-    if constexpr (SINGLE) {
-      lens[0] = uniform(min(max(a.c.lens[base], 0), cap));
+    struct Chunk {
+      int i, c, len;    // sequence of the round (none: PAGED_ROUND), chunk in it, its length
+      int p[NKT];       // page numbers of its tiles, as read
+    };
+    auto load_pages = [&](Chunk& k, int i, int c) {   // of chunk c of sequence i (past its end: some page number)
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt)
+        k.p[kt] = a.c.table[(base + i) * a.c.tstride + min((c * CH + 16 * kt) >> a.c.lp, a.c.max_pages - 1)];
+    };
+    Chunk cur_chunk, nxt;
+    if constexpr (SINGLE) {   // rows, page numbers and length are on their way together
+      load_q(base);
+      load_pages(cur_chunk, 0, w);
+      load_pages(nxt, 0, w + NW);
+      __builtin_amdgcn_sched_barrier(0);
+      lens[0] = min(max(scalar_load(a.c.lens, base), 0), cap);
       lo = 0;
       hi = chunks(lens[0]);
     } else {
@@ -502,22 +569,18 @@ __global__ __launch_bounds__(64 * paged_waves(sizeof(IT), D, NR, SINGLE),
         if (!SINGLE && h == 0 && tid == 0 && a.by_seq) a.plan[base + k] = make_int4(-1, 0, 0, 0);
       }
     // ---- the stream of this wave's chunks
-    struct Chunk {
-      int i, c, len;    // sequence of the round (none: PAGED_ROUND), chunk in it, its length
-      int p[NKT];       // page numbers of its tiles, as read
-    };
-    auto lookup = [&](int u) {   // chunk u of the line: the last sequence that starts at or before it
-      Chunk k;
+    auto locate = [&](Chunk& k, int u) {   // chunk u of the line: the last sequence that starts at or before it
       const int i = SINGLE ? 0 : min(list_find(first, u), cnt - 1);
       const bool there = u < hi;
       k.i = there ? i : PAGED_ROUND;
       k.len = there ? len_of(i) : 0;
-      k.c = SINGLE ? u : u - list_get(first, i);
-#pragma unroll
-      for (int kt = 0; kt < NKT; ++kt) {
-        const int j = max(min(k.c * CH + 16 * kt, k.len - 1), 0);
-        k.p[kt] = a.c.table[(base + i) * a.c.tstride + (j >> a.c.lp)];
-      }
+      k.c = SINGLE ? u : max(u - list_get(first, i), 0);
+      return i;
+    };
+    auto lookup = [&](int u) {
+      Chunk k;
+      const int i = locate(k, u);
+      load_pages(k, i, k.c);
       return k;
     };
     struct Tiles {
@@ -553,8 +616,8 @@ __global__ __launch_bounds__(64 * paged_waves(sizeof(IT), D, NR, SINGLE),
         for (int i = 0; i < NP; ++i)
           kp[kt][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off + 64 * i, 0, 0));
         bias[kt] = __builtin_bit_cast(
-            f32x4, __builtin_amdgcn_raw_buffer_load_b128(paged_rows(a.c.beta + k.row[kt], a.c.beta ? k.nv[kt] * 4 : 0),
-                                                         boff, 0, 0));
+            f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                       paged_rows(a.c.beta + k.row[kt], a.c.beta && k.nv[kt] > 0 ? 16 * 4 : 0), boff, 0, 0));
       }
     };
     auto load_v = [&](const Tiles& k) {
@@ -569,9 +632,15 @@ __global__ __launch_bounds__(64 * paged_waves(sizeof(IT), D, NR, SINGLE),
     };
     if (lo < hi) {
       int u = lo + w, i = SINGLE ? 0 : list_find(first, lo), at = lo;
-      load_q(base + i);
-      Tiles cur = resolve(lookup(u));
-      Chunk nxt = lookup(u + NW);
+      if constexpr (SINGLE) {
+        locate(cur_chunk, u);
+        locate(nxt, u + NW);
+      } else {
+        load_q(base + i);
+        cur_chunk = lookup(u);
+        nxt = lookup(u + NW);
+      }
+      Tiles cur = resolve(cur_chunk);
       load_k(cur);
       __builtin_amdgcn_sched_barrier(0);   // (loads stay in this order: their waits count the ones behind)
       load_v(cur);
@@ -799,7 +868,9 @@ __global__ __launch_bounds__(64 * paged_waves(sizeof(IT), D, NR, SINGLE),
         }
         if (!SINGLE && starts) {
           const int v = list_get(padded_first, i) + pad + s1 - s0;   // behind its last chunk
-          const int4 p = whole ? make_int4(-1, 0, 0, 0) : make_int4(s, g, (int)(((long)v * active - 1) / TV), 0);
+          // the workgroup of place v - 1
+          const int to = v <= more * (share + 1) ? (v - 1) / (share + 1) : more + (v - 1 - more * (share + 1)) / share;
+          const int4 p = whole ? make_int4(-1, 0, 0, 0) : make_int4(s, g, to, 0);
           if (a.by_seq) {
             if (h == 0 && tid == 0) a.plan[s] = p;
           } else if (!whole) {
@@ -819,12 +890,16 @@ __global__ __launch_bounds__(64 * paged_waves(sizeof(IT), D, NR, SINGLE),
 }
 
 // Joins the partial sums of the sequences that lie in several parts: block
-// (r, h, k) row r of plan entry k.  Groups of D / 4 lanes take every NG-th part.
+// (r, h, k) row r of plan entry k.  Groups of D / 4 lanes take every NG-th part:
+// many where few blocks read many parts each.
+constexpr int PAGED_MERGE_THREADS = 1024;   // at most
+
 template <class IT, int D>
-__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttendArgs a) {
-  constexpr int LPR = D / 4, NG = 256 / LPR;
-  __shared__ float4 acc[NG][LPR];
-  __shared__ float sum[NG], top[NG];
+__global__ __launch_bounds__(PAGED_MERGE_THREADS) void paged_merge_kernel(PagedAttendArgs a) {
+  constexpr int LPR = D / 4, MAX = PAGED_MERGE_THREADS / LPR;
+  __shared__ float4 acc[MAX][LPR];
+  __shared__ float sum[MAX], top[MAX];
+  const int NG = blockDim.x / LPR;
   const int r = blockIdx.x, h = blockIdx.y, R = a.group * a.nq, Hq = a.c.H * a.group;
   const int4 p = a.plan[blockIdx.z];
   if (p.x < 0) return;
@@ -853,10 +928,9 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttendArgs a) {
   __syncthreads();
   if (k == 0) {
     float S = 0.f, z[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
     for (int i = 0; i < NG; ++i) M = fmaxf(M, top[i]);
     const float ref = M == -INFINITY ? 0.f : M;
-#pragma unroll
+#pragma unroll 4
     for (int i = 0; i < NG; ++i) {
       const float4 v = acc[i][x];
       const float sc = exp_of(top[i] - ref);

@@ -123,6 +123,31 @@ def test_append_skips_what_has_no_place():
                  lens=torch.tensor([-2**31, 0, 2**31 - 1, 49], dtype=torch.int32))
 
 
+@pytest.mark.parametrize("seqs", [63, 64, 65, 130, 5000])
+def test_append_finds_the_sequence_among_many(seqs):
+    new = np.random.default_rng(seqs).integers(0, 3, seqs)
+    new[seqs - 1] = 2
+    lens = new + np.random.default_rng(seqs + 1).integers(0, 30, seqs)
+    c = Paged(17, [32] * seqs, 1, 64, 16, BF16, beta=False)
+    n = int(new.sum())
+    off = torch.from_numpy(np.concatenate([[0], np.cumsum(new)]).astype(np.int32))
+    check_append(c, c.rows(n).cuda(), c.rows(n).cuda(), off, lens=torch.from_numpy(lens.astype(np.int32)))
+
+
+def test_append_offsets_that_make_no_sense_stay_inside():
+    """Offsets that fall, are negative or pass the tokens: every token is skipped or lands in its sequence's pages."""
+    from paper_2606_07878_amd import binding
+    c = Paged(18, [30, 30, 30], 2, 64, 16, BF16, beta=False).cuda()
+    guard = [x.clone() for x in (c.k, c.v)]
+    k = c.rows(12).cuda()
+    for off in ([5, 2, 9, 1], [-7, -3, 2, 2**31 - 1], [0, 100, 50, 12], [2**31 - 1, 0, 0, 0]):
+        binding.paged_append(k, k, c.k, c.v, c.table, c.lens, offsets=torch.tensor(off, dtype=torch.int32).cuda())
+    torch.cuda.synchronize()
+    others = torch.ones(c.n_pages, dtype=torch.bool, device="cuda")
+    others[c.table.reshape(-1).long()] = False
+    assert torch.equal(c.k[others], guard[0][others]) and torch.equal(c.v[others], guard[1][others])
+
+
 def test_append_nothing():
     c = Paged(15, [4, 4], 2, 64, 16, BF16)
     check_append(c, c.rows(0).cuda(), c.rows(0).cuda())
@@ -236,6 +261,63 @@ def test_attend_long_and_short_together():
 def test_attend_many_sequences(seqs):
     c = Paged(34, [int(x) for x in np.random.default_rng(seqs).integers(0, 90, seqs)], 1, 64, 16, BF16)
     check_attend(c, c.rows(seqs, 2))
+
+
+@pytest.mark.parametrize("heads,seqs,long", [(8, 300, 9000), (2, 520, 5000)])
+def test_attend_more_sequences_than_workgroups_per_head(heads, seqs, long):
+    """Several rounds of lengths, parts that hold many sequences, a long one among them split over many."""
+    lens = [int(x) for x in np.random.default_rng(seqs).integers(0, 120, seqs)]
+    lens[seqs // 2], lens[seqs // 2 + 1] = long, 0
+    c = Paged(51, [120] * seqs, heads, 64, 16, BF16)
+    # one long sequence over all the other pages: shared pages are fine to read
+    width = -(-long // 16)
+    table = torch.zeros(seqs, width, dtype=torch.int32)
+    table[:, :8] = c.table
+    table[seqs // 2] = torch.from_numpy(c.rng.integers(0, c.n_pages, width).astype(np.int32))
+    check_attend(c, c.rows(seqs, heads), table=table, lens=torch.tensor(lens, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("mode", [BF16, FP32])
+@pytest.mark.parametrize("group,nq,d", [(4, 8, 256), (1, 32, 128), (1, 32, 64), (2, 4, 128), (1, 3, 256)])
+def test_attend_several_short_sequences_per_workgroup_with_rotation(mode, group, nq, d):
+    """The query rows and angles of one sequence after another in the same LDS."""
+    lens = [5, 30, 16, 1, 0, 33, 9, 2, 31, 64, 7, 12, 40]
+    c = Paged(52, lens, 1, d, 16, mode)
+    n = len(lens) * nq
+    pos = torch.from_numpy(c.rng.uniform(0, 1e5, n))
+    check_attend(c, c.rows(n, group), causal=True, qpos=pos, theta=1e6)
+    wide = torch.zeros(len(lens), 80, dtype=torch.int32)     # capacity above 1024: parts instead of whole sequences
+    wide[:, : c.table.shape[1]] = c.table
+    check_attend(c, c.rows(n, group), causal=True, qpos=pos, theta=1e6, table=wide)
+
+
+@pytest.mark.parametrize("mode", [BF16, FP32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [1, 100, 511, 768])
+def test_attend_narrow_and_wide_tables(mode, d, n):
+    """The same sequence through a table of its own pages and through a wide one (other kernels)."""
+    c = Paged(53, [n, 3], 2, d, 16, mode)
+    wide = torch.full((2, 300), -1, dtype=torch.int32)
+    wide[:, : c.table.shape[1]] = c.table
+    q = c.rows(2, 8)
+    a, b = check_attend(c, q), check_attend(c, q, table=wide)
+    assert (a.double() - b.double()).abs().max() <= 2 * HALF_STEP[mode] * a.double().abs().max() + 1e-5
+
+
+def test_attend_many_heads():
+    """More KV heads than workgroups: one part per head, nothing to join."""
+    c = Paged(54, [70, 300], 600, 64, 16, BF16, width=70)
+    check_attend(c, c.rows(2, 600))
+
+
+def test_attend_is_the_same_every_time():
+    c = Paged(55, [9000, 1, 300, 40], 2, 128, 32, BF16)
+    q = c.rows(4, 8)
+    a = check_attend(c, q)
+    from paper_2606_07878_amd import binding
+    c.cuda()
+    outs = [binding.paged_attend(q.cuda(), *c.pages(), beta_pages=c.beta) for _ in range(20)]
+    assert all(torch.equal(o, a) for o in outs)
 
 
 def test_attend_without_bias_and_with_a_scale():

@@ -108,7 +108,8 @@ BAD_CACHE = [(dict(mode=7), -3), (dict(head_dim=96), -5), (dict(n_kv_heads=0), -
              (dict(page_size=8192), -5), (dict(page_size=-16), -5), (dict(k=None), -1), (dict(v=FAKE + 8), -1),
              (dict(beta=FAKE + 2), -1)]
 BAD_SEQS = [(dict(n_seqs=0), -2), (dict(n_seqs=65536), -5), (dict(max_pages=0), -2), (dict(table_stride=9), -2),
-            (dict(max_pages=1 << 27, table_stride=1 << 27), -5), (dict(table=None), -1), (dict(lens=FAKE + 1), -1)]
+            (dict(max_pages=1 << 27, table_stride=1 << 27), -5),
+            (dict(n_seqs=65535, max_pages=1 << 15, table_stride=1 << 15), -5), (dict(table=None), -1), (dict(lens=FAKE + 1), -1)]
 
 
 @pytest.mark.parametrize("kw,status", BAD_CACHE)
