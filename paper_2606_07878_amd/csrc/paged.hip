@@ -89,18 +89,29 @@ static still_status check_attend(const still_paged_cache* c, const still_paged_a
   return STILL_OK;
 }
 
-// Whether a workgroup takes a whole sequence: one launch instead of two, but one
-// CU's rate of reading per sequence and head.  The host knows the table's
-// capacity only, so the line is where the average over lengths up to it is even.
-// us in a graph, whole / split, 8 heads, one sequence: bf16 of width 128 (the line
-// is a capacity of 1024) 32 entries 4.6 / 7.9, 256 6.1 / 10.0, 512 8.6 / 10.1, 719
-// 10.0 / 10.1, 1024 13.0 / 10.1; of width 64 256 4.5 / 9.5, 1024 8.8 / 9.6; fp32 of
-// width 64 (1024) 256 5.5 / 9.2, 719 10.0 / 9.3, 1024 12.3 / 9.3; of width 128 (512)
-// 32 4.7 / 8.2, 256 8.7 / 10.2, 719 17.7 / 10.3.  64 sequences (the line) of 100
-// entries 9.1 / 11.8, of 700 30.5 / 34.3; 128 of 100 21.1 / 18.9, 256 39 / 28.
-static bool paged_single(const still_paged_cache* c, const still_paged_seqs* q, int R) {
-  const long cap = (long)q->max_pages * c->page_size, row = c->head_dim * (c->mode == STILL_MODE_FP32 ? 4 : 2);
-  return R <= 16 && c->head_dim <= 128 && cap <= 1024 && cap * row <= 256 * 1024 && (long)q->n_seqs * c->n_kv_heads <= 512;
+// Who takes a sequence (and KV head).  Where its table is short one workgroup or
+// one wave takes all of it: one launch instead of two (9.3 us of host time instead
+// of 11.4), nothing joined, but one CU's rate of reading, or one wave's, for the
+// longest one.  The host knows the table's capacity only.  us in a graph, bf16 of
+// width 128, 8 heads unless said.
+// Team or parts (capacity 1024, the line), one sequence of 32 entries 4.5 / 7.9, 256
+// 5.9 / 10.0, 512 8.6 / 10.0, 719 10.2 / 10.0, 1024 12.9 / 10.0; width 64, 719 7.3 /
+// 9.4, 1024 8.9 / 9.4; width 256 (512, the line) 256 9.0 / 12.3, 512 13.2 / 12.4; fp32
+// of width 64 256 5.5 / 8.9, 1024 12.6 / 9.1; 32 rows 256 7.7 / 13.7, 1024 14.7 / 15.1.
+// 64 sequences (the line) of 1000 40 / 45, 72 53 / 47 (waves); 70 of 1 to 1024, spread
+// over their logarithm, 20.6 / 17.5.
+// Wave or team: 30 sequences (below the line) of 30 entries 4.1 / 4.9, 128 6.3 / 5.6, 512
+// 16.1 / 12.5; 40 (above) of 30 4.3 / 7.7, 128 6.5 / 9.0, 512 16.9 / 19.8; width 256, 40
+// of 128 11.7 / 12.7; 32 rows, 40 of 30 9.4 / 11.3, 256 17.7 / 16.9; fp32 of width 64, 40
+// of 30 4.1 / 4.8, 256 15.0 / 11.5.
+// Wave or parts: 256 sequences of 30 7.5 / 21.9, 256 41.8 / 47.4; 32 rows, 30 18.0 / 58;
+// 70 of 1 to 1024 27.8 / 17.5, which is why waves take capacities to 512 only.
+enum PagedWhole { PAGED_PARTS, PAGED_TEAM, PAGED_WAVE };
+static PagedWhole paged_whole(const still_paged_cache* c, const still_paged_seqs* q, int esize) {
+  const long cap = (long)q->max_pages * c->page_size, pairs = (long)q->n_seqs * c->n_kv_heads;
+  if (cap > 1024 || cap * c->head_dim * esize > 256 * 1024) return PAGED_PARTS;
+  if (cap <= 512) return pairs <= 256 ? PAGED_TEAM : PAGED_WAVE;
+  return pairs <= 512 ? PAGED_TEAM : PAGED_PARTS;
 }
 
 struct PagedPlan {
@@ -256,19 +267,35 @@ still_status still_paged_attend(const still_paged_cache* cache, const still_page
   paged_dispatch(cache, [&](auto it, auto d) {
     using IT = decltype(it);
     constexpr int D = decltype(d)::value;
-    if constexpr (D <= 128) if (paged_single(cache, seqs, R)) {
-      hipLaunchKernelGGL((paged_attend_kernel<IT, D, 1, true>), dim3(a.c.H, a.c.n_seqs), dim3(64 * paged_waves(sizeof(IT), D, 1, true)),
-                         (paged_lds_bytes<IT, D>(R, true)), st, a);
-      return;
+    auto launch = [&](auto nr, auto sw) {
+      constexpr int NR = decltype(nr)::value, SW = decltype(sw)::value;
+      using TL = PagedTile<IT, D, NR, SW>;
+      hipLaunchKernelGGL((paged_attend_kernel<IT, D, NR, SW>), dim3(a.c.H, SW ? a.c.n_seqs : a.G), dim3(64 * TL::NW),
+                         (paged_lds_bytes<TL, D, NR, SW>(R, a.nq, a.qpos != nullptr)), st, a);
+    };
+    using One = std::integral_constant<int, 1>;
+    using Two = std::integral_constant<int, 2>;
+    using Parts = std::integral_constant<int, 0>;
+    switch (paged_whole(cache, seqs, sizeof(IT))) {
+      case PAGED_TEAM:
+        if (R <= 16) launch(One(), std::integral_constant<int, paged_team(D, 1)>());
+        else launch(Two(), std::integral_constant<int, paged_team(D, 2)>());
+        return;
+      case PAGED_WAVE:
+        if (R <= 16) launch(One(), One());
+        else launch(Two(), One());
+        return;
+      default: break;
     }
-    const dim3 grid(a.c.H, a.G), block(64 * paged_waves(sizeof(IT), D, R <= 16 ? 1 : 2, false));
-    const size_t lds = paged_lds_bytes<IT, D>(R, false);
-    if (R <= 16) hipLaunchKernelGGL((paged_attend_kernel<IT, D, 1, false>), grid, block, lds, st, a);
-    else hipLaunchKernelGGL((paged_attend_kernel<IT, D, 2, false>), grid, block, lds, st, a);
+    if (R <= 16) launch(One(), Parts());
+    else launch(Two(), Parts());
     if (a.G > 1) {
+      // wide blocks where a few of them may read hundreds of parts each: one sequence of
+      // 400000 entries of one head 58 us with 256 threads, 50 with 1024; of 256 entries of
+      // 8 heads 10.0 with 256, 11.2 with 1024
       const dim3 joins(R, a.c.H, std::min(a.c.n_seqs, a.G));
-      hipLaunchKernelGGL((paged_merge_kernel<IT, D>), joins,
-                         dim3((long)joins.x * joins.y * joins.z <= 512 ? PAGED_MERGE_THREADS : 256), 0, st, a);
+      const bool wide = a.G > 128 && ((long)a.c.max_pages << a.c.lp) > 128 * 128 && (long)joins.x * joins.y * joins.z <= 512;
+      hipLaunchKernelGGL((paged_merge_kernel<IT, D>), joins, dim3(wide ? PAGED_MERGE_THREADS : 256), 0, st, a);
     }
   });
   HIP_TRY(hipGetLastError());

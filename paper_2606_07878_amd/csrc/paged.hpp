@@ -257,7 +257,7 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(PagedGatherArgs a) {
 // and cost nothing, so the loop has no branch and every load's wait counts only
 // the loads behind it.
 //
-// SINGLE: workgroup (h, s) takes all of sequence s; nothing is joined.
+// SW: workgroup (h, s) of SW waves takes all of sequence s; nothing is joined.
 // ---------------------------------------------------------------------------
 struct PagedAttendArgs {
   PagedArgs c;
@@ -288,20 +288,24 @@ constexpr float LOG2E = 1.4426950408889634f;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// Waves per workgroup, workgroups resident on a CU, and 16-entry tiles per chunk:
-// 128 KB of keys and values in flight per CU.
-constexpr int paged_waves(int esize, int D, int NR, bool SINGLE) {
-  return SINGLE || (NR == 2 && D <= 128 && esize == 4) ? 8 : 4;
-}
+// Parts of the line: waves per workgroup, workgroups resident on a CU, and
+// 16-entry tiles per chunk: 128 KB of keys and values in flight per CU (of width 64
+// half of that: its rate is the same, and short sequences take less).
+constexpr int paged_waves(int esize, int D, int NR) { return NR == 2 && D <= 128 && esize == 4 ? 8 : 4; }
 constexpr int paged_resident(int D, int NR) { return NR == 1 && D <= 128 ? 2 : 1; }
 constexpr int paged_tiles(int esize, int D, int NR) {
-  return (NR == 1 && D == 64 ? 64 : 128) * 1024 / (paged_waves(esize, D, NR, false) * paged_resident(D, NR) * 32 * D * esize);
+  return (NR == 1 && D == 64 ? 64 : 128) * 1024 / (paged_waves(esize, D, NR) * paged_resident(D, NR) * 32 * D * esize);
 }
+// Whole sequences: waves per workgroup (two per SIMD, or as the registers allow).
+constexpr int paged_team(int D, int NR) { return NR == 1 && D <= 128 ? 8 : 4; }
 
-template <class IT, int D, int NR, bool SINGLE>
+// SW: waves of a workgroup that takes a whole sequence; 0: parts of the line.
+template <class IT, int D, int NR, int SW>
 struct PagedTile {
   static constexpr bool B16 = sizeof(IT) == 2;
-  static constexpr int NKT = SINGLE ? (B16 ? 2 : 1) : paged_tiles(sizeof(IT), D, NR);   // 16-entry tiles per chunk
+  static constexpr int NW = SW ? SW : paged_waves(sizeof(IT), D, NR);
+  static constexpr int PER_SIMD = SW == 1 ? (D <= 128 ? 2 : 1) : NW * (SW ? 1 : paged_resident(D, NR)) / 4;
+  static constexpr int NKT = SW ? (B16 ? 2 : 1) : paged_tiles(sizeof(IT), D, NR);   // 16-entry tiles per chunk
   static constexpr int CH = 16 * NKT;
   static constexpr int ROWB = D * (int)sizeof(IT);
   static constexpr int NP = ROWB / 64;                  // 16-byte pieces of a key per lane
@@ -311,16 +315,16 @@ struct PagedTile {
   static constexpr int QBYTES = 16 * QROW * (B16 ? 2 : 1);   // per 16 rows; bf16: two parts
 };
 
-// the waves' sums take the query rows' place in LDS where both do not fit 160 KB
-constexpr bool paged_alias(int D, int NR) { return D * NR > 256; }
-
-// dynamic LDS: the query rows, the waves' sums [waves][R][OROW]
-template <class IT, int D>
-inline size_t paged_lds_bytes(int R, bool single) {
-  using TL = PagedTile<IT, D, 1, true>;   // (the row sizes are the same for all)
-  const int nr = R <= 16 ? 1 : 2;
-  const size_t q = (size_t)nr * TL::QBYTES, o = (size_t)paged_waves(sizeof(IT), D, nr, single) * R * TL::OROW * sizeof(float);
-  return paged_alias(D, nr) ? std::max(q, o) : q + o;
+// Dynamic LDS: the query rows, behind them the waves' sums [waves][R][OROW] or,
+// before there are any, the queries' angles [nq][D / 2].  The sums take the rows'
+// place where both do not fit 160 KB, and in workgroups of one wave, many of which
+// share a CU.
+constexpr bool paged_alias(int D, int NR, int SW) { return SW == 1 || D * NR > 256; }
+template <class TL, int D, int NR, int SW>
+inline size_t paged_lds_bytes(int R, int nq, bool rot) {
+  const size_t q = (size_t)NR * TL::QBYTES, o = (size_t)TL::NW * R * TL::OROW * sizeof(float);
+  const size_t angles = rot ? (size_t)nq * D / 2 * sizeof(float2) : 0;
+  return paged_alias(D, NR, SW) ? std::max(q + angles, o) : q + std::max(angles, o);
 }
 
 // fast base-2 exponential (results below 2^-126 are zero)
@@ -384,15 +388,14 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t paged_rows(const void* p, int 
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000);
 }
 
-template <class IT, int D, int NR, bool SINGLE>
-__global__ __launch_bounds__(64 * paged_waves(sizeof(IT), D, NR, SINGLE),
-                             paged_waves(sizeof(IT), D, NR, SINGLE) * (SINGLE ? 1 : paged_resident(D, NR)) / 4)
+template <class IT, int D, int NR, int SW>
+__global__ __launch_bounds__((64 * PagedTile<IT, D, NR, SW>::NW), (PagedTile<IT, D, NR, SW>::PER_SIMD))
 void paged_attend_kernel(PagedAttendArgs a) {
-  using TL = PagedTile<IT, D, NR, SINGLE>;
-  constexpr int NKT = TL::NKT, CH = TL::CH, NP = TL::NP, FPT = TL::FPT, VB = TL::VB, ROWB = TL::ROWB;
-  constexpr int NW = paged_waves(sizeof(IT), D, NR, SINGLE);
+  using TL = PagedTile<IT, D, NR, SW>;
+  constexpr bool SINGLE = SW > 0;
+  constexpr int NKT = TL::NKT, CH = TL::CH, NP = TL::NP, FPT = TL::FPT, VB = TL::VB, ROWB = TL::ROWB, NW = TL::NW;
   constexpr int QROW = TL::QROW, OROW = TL::OROW, NT = 64 * NW, HD = D / 2;
-  constexpr bool ALIAS = paged_alias(D, NR);
+  constexpr bool ALIAS = paged_alias(D, NR, SW);
   extern __shared__ float4 paged_smem[];
   char* qs = (char*)paged_smem;                  // [16 NR][QROW], bf16: the same again for the low parts
   char* ql = qs + 16 * NR * QROW;
@@ -415,7 +418,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
   // thread's pairs of 16-byte pieces D / 2 apart, the members of the rotated pairs
   constexpr int HP = ROWB / 32, EPP = 16 / (int)sizeof(IT), QI = (16 * NR * HP + NT - 1) / NT;
   u32x4 qr[QI][2];
-  static_assert(NT % HD == 0, "a thread's angles belong to one pair");
+  // a thread's angles belong to one pair where the threads are a multiple of the pairs
   const double inv_freq = rot ? exp2(a.log2_theta * (-2.0 * (tid % HD) / D)) : 0.0;
   auto load_q = [&](int s) {
 #pragma unroll
@@ -428,7 +431,9 @@ void paged_attend_kernel(PagedAttendArgs a) {
   };
   auto stage_q = [&](int s) {   // rotated, in LDS; ends with a barrier
     if (rot) {
-      for (int e = tid; e < a.nq * HD; e += NT) cs[e] = rope_cs(a.qpos[(long)s * a.nq + e / HD], inv_freq);
+      for (int e = tid; e < a.nq * HD; e += NT)
+        cs[e] = rope_cs(a.qpos[(long)s * a.nq + e / HD],
+                        NT % HD == 0 ? inv_freq : exp2(a.log2_theta * (-2.0 * (e % HD) / D)));
       __syncthreads();
     }
 #pragma unroll
@@ -484,7 +489,8 @@ void paged_attend_kernel(PagedAttendArgs a) {
   // workgroups with a part, the chunks (with pads) of one, how many take one more, this part's cuts
   int active = 0, share = 0, more = 0, v0 = 0, v1 = 0;
   auto cuts = [&](int T, int some) {        // of the sums over all sequences
-    active = min(a.G, (T + NW - 1) / NW);   // a workgroup takes a chunk per wave before another one starts
+    // a workgroup takes a chunk per wave, but not two short sequences, before another one starts
+    active = min(a.G, max((T + NW - 1) / NW, some));
     if (g < active) {
       share = (T + pad * some) / active;
       more = T + pad * some - share * active;
@@ -892,7 +898,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
 // Joins the partial sums of the sequences that lie in several parts: block
 // (r, h, k) row r of plan entry k.  Groups of D / 4 lanes take every NG-th part:
 // many where few blocks read many parts each.
-constexpr int PAGED_MERGE_THREADS = 1024;   // at most
+constexpr int PAGED_MERGE_THREADS = 1024;   // at most, 256 at least
 
 template <class IT, int D>
 __global__ __launch_bounds__(PAGED_MERGE_THREADS) void paged_merge_kernel(PagedAttendArgs a) {

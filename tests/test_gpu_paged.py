@@ -304,6 +304,20 @@ def test_attend_narrow_and_wide_tables(mode, d, n):
     assert (a.double() - b.double()).abs().max() <= 2 * HALF_STEP[mode] * a.double().abs().max() + 1e-5
 
 
+@pytest.mark.parametrize("mode", [BF16, FP32])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("group,nq", [(4, 1), (3, 5), (4, 8), (1, 32)])
+def test_attend_many_short_sequences(mode, d, group, nq):
+    """Enough sequences and heads that a wave takes each (90 x 3), the table's columns short."""
+    lens = [int(x) for x in np.random.default_rng(d + nq).integers(0, 80, 90)]
+    lens[:4] = [0, 1, 16, 79]
+    c = Paged(56, lens, 3, d, 16, mode)
+    n = 90 * nq
+    pos = torch.from_numpy(c.rng.uniform(0, 1e5, n))
+    rot = nq != 5
+    check_attend(c, c.rows(n, 3 * group), causal=nq > 1, qpos=pos if rot else None, theta=1e4 if rot else 0.0)
+
+
 def test_attend_many_heads():
     """More KV heads than workgroups: one part per head, nothing to join."""
     c = Paged(54, [70, 300], 600, 64, 16, BF16, width=70)
