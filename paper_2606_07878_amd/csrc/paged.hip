@@ -106,12 +106,17 @@ static still_status check_attend(const still_paged_cache* c, const still_paged_a
 // of 30 4.1 / 4.8, 256 15.0 / 11.5.
 // Wave or parts: 256 sequences of 30 7.5 / 21.9, 256 41.8 / 47.4; 32 rows, 30 18.0 / 58;
 // 70 of 1 to 1024 27.8 / 17.5, which is why waves take capacities to 512 only.
-enum PagedWhole { PAGED_PARTS, PAGED_TEAM, PAGED_WAVE };
-static PagedWhole paged_whole(const still_paged_cache* c, const still_paged_seqs* q, int esize) {
+// Streaming loads where the call may read more than the memory-side cache holds (256
+// MB): one sequence of 131136 101 / 91 with ordinary / streaming loads, 64 of up to
+// 16384 101 / 95, 5 of up to 20011 and 32 rows (410 MB) 46.5 / 45.0; below it the entries
+// may still be there from the step before: 4 sequences of up to 9000 (147 MB) 23.8 / 25.8.
+enum PagedKernel { PAGED_PARTS, PAGED_STREAM, PAGED_TEAM, PAGED_WAVE };
+static PagedKernel paged_kernel(const still_paged_cache* c, const still_paged_seqs* q, int esize) {
   const long cap = (long)q->max_pages * c->page_size, pairs = (long)q->n_seqs * c->n_kv_heads;
-  if (cap > 1024 || cap * c->head_dim * esize > 256 * 1024) return PAGED_PARTS;
+  const PagedKernel parts = 2 * pairs * cap * c->head_dim * esize > (256L << 20) ? PAGED_STREAM : PAGED_PARTS;
+  if (cap > 1024 || cap * c->head_dim * esize > 256 * 1024) return parts;
   if (cap <= 512) return pairs <= 256 ? PAGED_TEAM : PAGED_WAVE;
-  return pairs <= 512 ? PAGED_TEAM : PAGED_PARTS;
+  return pairs <= 512 ? PAGED_TEAM : parts;
 }
 
 struct PagedPlan {
@@ -270,13 +275,14 @@ still_status still_paged_attend(const still_paged_cache* cache, const still_page
     auto launch = [&](auto nr, auto sw) {
       constexpr int NR = decltype(nr)::value, SW = decltype(sw)::value;
       using TL = PagedTile<IT, D, NR, SW>;
-      hipLaunchKernelGGL((paged_attend_kernel<IT, D, NR, SW>), dim3(a.c.H, SW ? a.c.n_seqs : a.G), dim3(64 * TL::NW),
+      hipLaunchKernelGGL((paged_attend_kernel<IT, D, NR, SW>), dim3(a.c.H, SW > 0 ? a.c.n_seqs : a.G), dim3(64 * TL::NW),
                          (paged_lds_bytes<TL, D, NR, SW>(R, a.nq, a.qpos != nullptr)), st, a);
     };
     using One = std::integral_constant<int, 1>;
     using Two = std::integral_constant<int, 2>;
     using Parts = std::integral_constant<int, 0>;
-    switch (paged_whole(cache, seqs, sizeof(IT))) {
+    using Stream = std::integral_constant<int, -1>;
+    switch (paged_kernel(cache, seqs, sizeof(IT))) {
       case PAGED_TEAM:
         if (R <= 16) launch(One(), std::integral_constant<int, paged_team(D, 1)>());
         else launch(Two(), std::integral_constant<int, paged_team(D, 2)>());
@@ -285,10 +291,14 @@ still_status still_paged_attend(const still_paged_cache* cache, const still_page
         if (R <= 16) launch(One(), One());
         else launch(Two(), One());
         return;
-      default: break;
+      case PAGED_STREAM:
+        if (R <= 16) launch(One(), Stream());
+        else launch(Two(), Stream());
+        break;
+      default:
+        if (R <= 16) launch(One(), Parts());
+        else launch(Two(), Parts());
     }
-    if (R <= 16) launch(One(), Parts());
-    else launch(Two(), Parts());
     if (a.G > 1) {
       // wide blocks where a few of them may read hundreds of parts each: one sequence of
       // 400000 entries of one head 58 us with 256 threads, 50 with 1024; of 256 entries of

@@ -245,8 +245,9 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(PagedGatherArgs a) {
 //   4 i + lg of its key: the pairing of contraction indices is free, so pieces
 //   feed the product as loaded, against the same pieces of the query row.
 //   O^T[feature][row]: register j of tile kt of S^T holds entry 16 kt + 4 lg + j.
-//   Lane l reads features [l D / 16, ..) of its lane group's entries, so value
-//   rows are read whole too, and output tile e holds features e, D / 16 + e, ...
+//   Lane l reads pieces l, 16 + l, ... of its lane group's entries, so a load
+//   reads whole runs of value rows; output tile e holds feature e of every
+//   lane's.
 //   bf16: the lane's 8 entries are the 8 contraction indices of one
 //   v_mfma_f32_16x16x32_bf16; the 16-bit transposition is v_perm in the lane.
 //   Weights (and rotated queries) go in as two bf16 parts, hi + lo, 16 bits of
@@ -301,17 +302,20 @@ constexpr int paged_tiles(int esize, int D, int NR) {
 // Whole sequences: waves per workgroup (two per SIMD, or as the registers allow).
 constexpr int paged_team(int D, int NR) { return NR == 1 && D <= 128 ? 8 : 4; }
 
-// SW: waves of a workgroup that takes a whole sequence; 0: parts of the line.
+// SW: waves of a workgroup that takes a whole sequence; 0: parts of the line; -1:
+// parts, the entries' loads streaming past the caches.
 template <class IT, int D, int NR, int SW>
 struct PagedTile {
   static constexpr bool B16 = sizeof(IT) == 2;
-  static constexpr int NW = SW ? SW : paged_waves(sizeof(IT), D, NR);
-  static constexpr int PER_SIMD = SW == 1 ? (D <= 128 ? 2 : 1) : NW * (SW ? 1 : paged_resident(D, NR)) / 4;
-  static constexpr int NKT = SW ? (B16 ? 2 : 1) : paged_tiles(sizeof(IT), D, NR);   // 16-entry tiles per chunk
+  static constexpr int NW = SW > 0 ? SW : paged_waves(sizeof(IT), D, NR);
+  static constexpr int PER_SIMD = SW == 1 ? (D <= 128 ? 2 : 1) : NW * (SW > 0 ? 1 : paged_resident(D, NR)) / 4;
+  static constexpr int NKT = SW > 0 ? (B16 ? 2 : 1) : paged_tiles(sizeof(IT), D, NR);   // 16-entry tiles per chunk
   static constexpr int CH = 16 * NKT;
+  static constexpr int AUX = SW < 0 ? 2 : 0;            // cache policy of the entries' loads: 2 non-temporal
   static constexpr int ROWB = D * (int)sizeof(IT);
   static constexpr int NP = ROWB / 64;                  // 16-byte pieces of a key per lane
   static constexpr int FPT = D / 16, VB = FPT * (int)sizeof(IT);
+  static constexpr int PB = VB < 16 ? VB : 16, EPV = PB / (int)sizeof(IT);   // bytes and features of a piece of a value row
   static constexpr int QROW = ROWB + 16;                // query rows in LDS (padded: 16 rows at one piece)
   static constexpr int OROW = D + 4;
   static constexpr int QBYTES = 16 * QROW * (B16 ? 2 : 1);   // per 16 rows; bf16: two parts
@@ -368,19 +372,17 @@ __device__ __forceinline__ int list_find(const int (&x)[4], int v) {
   return i;
 }
 
-// B bytes (4, 8 or a multiple of 16) at byte off of a buffer into words
-template <int B>
-__device__ __forceinline__ void buffer_words(__amdgpu_buffer_rsrc_t r, int off, uint32_t (&w)[B / 4]) {
-  if constexpr (B == 4) {
-    w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0);
-  } else if constexpr (B == 8) {
-    const u32x2 u = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
-    w[0] = u.x;
-    w[1] = u.y;
-  } else {
+// N pieces of PB bytes (8 or 16) of a buffer from byte off, 16 PB apart, as words
+template <int PB, int N, int AUX>
+__device__ __forceinline__ void buffer_pieces(__amdgpu_buffer_rsrc_t r, int off, uint32_t (&w)[N * PB / 4]) {
 #pragma unroll
-    for (int i = 0; i < B / 16; ++i) {
-      const u32x4 u = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off + 16 * i, 0, 0));
+  for (int i = 0; i < N; ++i) {
+    if constexpr (PB == 8) {
+      const u32x2 u = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off + 16 * PB * i, 0, AUX));
+      w[2 * i] = u.x;
+      w[2 * i + 1] = u.y;
+    } else {
+      const u32x4 u = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off + 16 * PB * i, 0, AUX));
 #pragma unroll
       for (int e = 0; e < 4; ++e) w[4 * i + e] = u[e];
     }
@@ -409,7 +411,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
   const int h = blockIdx.x, g = SINGLE ? 0 : blockIdx.y, R = a.group * a.nq, Hq = a.c.H * a.group;
   const int n_seqs = a.c.n_seqs, pad = n_seqs > 1 ? PAGED_PAD : 0;
   const bool rot = a.qpos != nullptr;
-  const int koff = l * ROWB + lg * 16, voff = 4 * lg * ROWB + l * VB;
+  const int koff = l * ROWB + lg * 16, voff = 4 * lg * ROWB + l * TL::PB;
   auto head_of = [&](int r) { return r * a.nq_inv >> 16; };   // of the group; the query is r - nq * that
   auto out_row = [&](int s, int r) {
     const int hr = head_of(r);
@@ -622,7 +624,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
         const auto r = paged_rows(a.c.k + k.row[kt] * ROWB, k.nv[kt] * ROWB);
 #pragma unroll
         for (int i = 0; i < NP; ++i)
-          kp[kt][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off + 64 * i, 0, 0));
+          kp[kt][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off + 64 * i, 0, TL::AUX));
         bias[kt] = __builtin_bit_cast(
             f32x4, __builtin_amdgcn_raw_buffer_load_b128(
                        paged_rows(a.c.beta + k.row[kt], a.c.beta && k.nv[kt] > 0 ? 16 * 4 : 0), boff, 0, 0));
@@ -635,7 +637,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
       for (int kt = 0; kt < NKT; ++kt) {
         const auto r = paged_rows(a.c.v + k.row[kt] * ROWB, k.nv[kt] * ROWB);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) buffer_words<VB>(r, off + j * ROWB, vr[kt * 4 + j]);
+        for (int j = 0; j < 4; ++j) buffer_pieces<TL::PB, VB / TL::PB, TL::AUX>(r, off + j * ROWB, vr[kt * 4 + j]);
       }
     };
     if (lo < hi) {
@@ -834,10 +836,10 @@ void paged_attend_kernel(PagedAttendArgs a) {
           if (r < R) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              float* dst = osum + (w * R + r) * OROW + (4 * lg + j) * FPT;
+              float* dst = osum + (w * R + r) * OROW + (4 * lg + j) * TL::EPV;
 #pragma unroll
               for (int e = 0; e < FPT; e += 4)
-                *(float4*)(dst + e) = make_float4(o[rt][e][j], o[rt][e + 1][j], o[rt][e + 2][j], o[rt][e + 3][j]);
+                *(float4*)(dst + e / TL::EPV * 16 * TL::EPV + e % TL::EPV) = make_float4(o[rt][e][j], o[rt][e + 1][j], o[rt][e + 2][j], o[rt][e + 3][j]);
             }
           }
         }
