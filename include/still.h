@@ -379,8 +379,10 @@ still_status still_paged_gather(const still_paged_cache *cache, const still_page
  * With causal = 1, query i sits at entry lens[s] - n_queries + i and sees
  * entries up to that one.  A query that sees nothing gets zeros (a padded batch
  * row has length 0).  A NaN or an infinity in an entry that some query of the
- * call sees may reach the other queries of its sequence and KV head; one that
- * no query sees reaches none. */
+ * call sees makes that query's output non-finite (an infinity may come out as
+ * NaN) and may reach the other queries of its sequence and KV head; one that no
+ * query sees reaches none.  The result does not depend on the order in which
+ * the device runs: the same inputs give the same bits. */
 typedef struct {
   int32_t group;        /* query heads per KV head, >= 1                                    */
   int32_t n_queries;    /* queries per sequence and query head; group * n_queries <= 32     */

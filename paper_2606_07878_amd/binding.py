@@ -717,8 +717,9 @@ def compact_paged(cfg: configs.CompactorConfig, weights: List[Dict[str, object]]
     (still_compact_layer, or still_compact_model_beta with ``w_beta``) and
     written back behind the preserved prefix, and the entries behind them move
     up with their bias.  ``positions`` [n] are the entries' float64 logical
-    positions.  Sets lens[seq] on the current stream and returns the new
-    positions [n - (end - start) + t]; pages behind the new length are free.
+    positions; lens[seq] holds n, and the pages up to the new length are there.
+    Sets lens[seq] on the current stream and returns the new positions
+    [n - (end - start) + t]; pages behind the new length are free.
     A cache that keeps bias passes ``beta_pages``; new entries without
     ``w_beta`` get bias 0."""
     torch = _torch()
@@ -726,7 +727,7 @@ def compact_paged(cfg: configs.CompactorConfig, weights: List[Dict[str, object]]
     if not (0 <= start < end <= n):
         _refuse(-1, f"subrange [{start}, {end}) outside [0, {n})")
     L = len(k_pages)
-    if len(v_pages) != L or len(weights) != L or any(x is not None and len(x) != L for x in (w_beta, beta_pages)):
+    if L < 1 or len(v_pages) != L or len(weights) != L or any(x is not None and len(x) != L for x in (w_beta, beta_pages)):
         _refuse(-2, "lists of different numbers of layers")
     if w_beta is not None and beta_pages is None:
         _refuse(-1, "w_beta given to a cache without beta")
@@ -742,20 +743,26 @@ def compact_paged(cfg: configs.CompactorConfig, weights: List[Dict[str, object]]
     inside = positions[start:end].contiguous()
     ws = torch.empty(max(still_workspace_size(make_config(cfg, mode), end - start, t, 1), 1), dtype=torch.uint8,
                      device=dev)                                     # shared by the layers (one stream)
+    # every layer is compacted before the first one's pages change: a refusal leaves them as they were
+    new = []
     for i in range(L):
-        bp = None if beta_pages is None else beta_pages[i]
+        if tuple(k_pages[i].shape[1::2]) != (cfg.n_kv_heads, cfg.head_dim):
+            _refuse(-2, f"layer {i}: pages {tuple(k_pages[i].shape)} for a compactor of {cfg.n_kv_heads} heads of width "
+                        f"{cfg.head_dim}")
         K, V = paged_gather(k_pages[i], v_pages[i], table, lens, seq, end - start, start)
-        rest = paged_gather(k_pages[i], v_pages[i], table, lens, seq, n - end, end, beta_pages=bp)
-        beta = None
         if w_beta is None:
             Ck, Cv, pq = compact_layer(cfg, weights[i], K, V, inside, rope_theta, t, rerotate=rerotate, mode=mode,
                                        workspace=ws)
+            beta = None
         else:
             (Ck,), (Cv,), pq, (beta,) = compact_model_beta(cfg, [weights[i]], [K], [V], inside, rope_theta, t,
                                                            [w_beta[i]], beta_max, mass_alpha, log_x, rerotate, mode, ws)
             beta = beta.t()
-        paged_append(Ck.transpose(0, 1), Cv.transpose(0, 1), k_pages[i], v_pages[i], row, to[0], beta=beta,
-                     beta_pages=bp)
+        new.append((Ck.transpose(0, 1), Cv.transpose(0, 1), beta))
+    for i, (Ck, Cv, beta) in enumerate(new):
+        bp = None if beta_pages is None else beta_pages[i]
+        rest = paged_gather(k_pages[i], v_pages[i], table, lens, seq, n - end, end, beta_pages=bp)
+        paged_append(Ck, Cv, k_pages[i], v_pages[i], row, to[0], beta=beta, beta_pages=bp)
         paged_append(rest[0].transpose(0, 1), rest[1].transpose(0, 1), k_pages[i], v_pages[i], row, to[1],
                      beta=None if bp is None else rest[2].t(), beta_pages=bp)
     lens[seq:seq + 1].fill_(length)

@@ -324,6 +324,24 @@ def test_attend_many_heads():
     check_attend(c, c.rows(2, 600))
 
 
+@pytest.mark.parametrize("width", [1, 70])
+def test_attend_as_many_sequences_as_a_call_takes(width):
+    """65535 sequences of one entry (a few of none): each row is its value.
+    Short tables take a wave per sequence, wide ones parts."""
+    from paper_2606_07878_amd import binding
+    n, pages = 65535, 1000
+    g = torch.Generator(device="cuda").manual_seed(5)
+    k = torch.randn(pages, 1, 16, 64, generator=g, device="cuda").bfloat16()
+    v = torch.randn(pages, 1, 16, 64, generator=g, device="cuda").bfloat16()
+    table = torch.randint(0, pages, (n, width), generator=g, device="cuda", dtype=torch.int32)
+    lens = torch.ones(n, dtype=torch.int32, device="cuda")
+    lens[::1000] = 0
+    q = torch.randn(n, 1, 64, generator=g, device="cuda").bfloat16()
+    out = binding.paged_attend(q, k, v, table, lens)
+    want = v[table[:, 0].long(), 0, 0] * lens[:, None]
+    assert torch.equal(out[:, 0], want)
+
+
 def test_attend_is_the_same_every_time():
     c = Paged(55, [9000, 1, 300, 40], 2, 128, 32, BF16)
     q = c.rows(4, 8)
@@ -563,6 +581,26 @@ def test_compact_paged_is_compact_subrange_in_the_pages(mode, start, end, bias):
         others[c.table[1].long()] = False
         for x, y in zip(pages[l], before[l]):
             assert torch.equal(x[others], y[others])
+
+
+def test_compact_paged_changes_nothing_where_a_layer_is_refused():
+    from paper_2606_07878_amd import binding
+    w = configs.shrink(configs.get_workload(1), n_tokens=100, t=32)
+    H, d = w.cfg.n_kv_heads, w.cfg.head_dim
+    c = Paged(64, [100], H, d, 16, BF16).cuda()
+    good, bad = (weights_to_device(synth.make_weights(w, 0, t=t), BF16) for t in (32, 16))
+    k2, v2 = c.k.clone(), c.v.clone()
+    pos = torch.arange(100, dtype=torch.float64, device="cuda")
+    before = c.k.clone(), c.v.clone()
+    with pytest.raises(binding.StillError) as e:
+        binding.compact_paged(w.cfg, [good, bad], [c.k, k2], [c.v, v2], c.table, c.lens, 0, 100, pos, w.rope_theta, 32)
+    assert e.value.status == -2
+    other = Paged(65, [100], H + 1, d, 16, BF16).cuda()
+    with pytest.raises(binding.StillError) as e:
+        binding.compact_paged(w.cfg, [good], [other.k], [other.v], other.table, other.lens, 0, 100, pos, w.rope_theta, 32)
+    assert e.value.status == -2
+    torch.cuda.synchronize()
+    assert torch.equal(c.k, before[0]) and torch.equal(c.v, before[1]) and c.lens.tolist() == [100]
 
 
 def test_steps_captured_in_a_graph_follow_the_lengths():
