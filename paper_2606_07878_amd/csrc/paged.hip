@@ -98,8 +98,8 @@ static still_status check_attend(const still_paged_cache* c, const still_paged_a
 // 5.9 / 10.0, 512 8.6 / 10.0, 719 10.2 / 10.0, 1024 12.9 / 10.0; width 64, 719 7.3 /
 // 9.4, 1024 8.9 / 9.4; width 256 (512, the line) 256 9.0 / 12.3, 512 13.2 / 12.4; fp32
 // of width 64 256 5.5 / 8.9, 1024 12.6 / 9.1; 32 rows 256 7.7 / 13.7, 1024 14.7 / 15.1.
-// 64 sequences (the line) of 1000 40 / 45, 72 53 / 47 (waves); 70 of 1 to 1024, spread
-// over their logarithm, 20.6 / 17.5.
+// 64 sequences (the line) of 1000 41 / 48; 70 of 1 to 1024, spread over their
+// logarithm, 20.6 / 17.5.
 // Wave or team: 30 sequences (below the line) of 30 entries 4.1 / 4.9, 128 6.3 / 5.6, 512
 // 16.1 / 12.5; 40 (above) of 30 4.3 / 7.7, 128 6.5 / 9.0, 512 16.9 / 19.8; width 256, 40
 // of 128 11.7 / 12.7; 32 rows, 40 of 30 9.4 / 11.3, 256 17.7 / 16.9; fp32 of width 64, 40
@@ -107,7 +107,7 @@ static still_status check_attend(const still_paged_cache* c, const still_paged_a
 // Wave or parts: 256 sequences of 30 7.5 / 21.9, 256 41.8 / 47.4; 32 rows, 30 18.0 / 58;
 // 70 of 1 to 1024 27.8 / 17.5, which is why waves take capacities to 512 only.
 // Streaming loads where the call may read more than the memory-side cache holds (256
-// MB): one sequence of 131136 101 / 91 with ordinary / streaming loads, 64 of up to
+// MB): us with ordinary / streaming loads, one sequence of 131136 101 / 91, 64 of up to
 // 16384 101 / 95, 5 of up to 20011 and 32 rows (410 MB) 46.5 / 45.0; below it the entries
 // may still be there from the step before: 4 sequences of up to 9000 (147 MB) 23.8 / 25.8.
 enum PagedKernel { PAGED_PARTS, PAGED_STREAM, PAGED_TEAM, PAGED_WAVE };

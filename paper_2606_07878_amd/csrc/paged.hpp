@@ -257,10 +257,15 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(PagedGatherArgs a) {
 // once P.V has; page numbers are read two chunks ahead, before the keys of the
 // next one, so that they are there with them (loads return in order).  A tile is
 // read through a buffer descriptor of its valid rows: the others read as zeros
-// and cost nothing, so the loop has no branch and every load's wait counts only
+// and cost nothing, so the loop has no branch around a load and every wait counts only
 // the loads behind it.
 //
 // SW: workgroup (h, s) of SW waves takes all of sequence s; nothing is joined.
+//
+// Bound by the entries' bytes: one sequence of 131136 entries of 8 heads of width 128
+// (537 MB) 83 us, 6.5 TB/s, joined in 4.6; 48 of 1024 to 9216 of width 256 (1.48 GB)
+// 225 us, 6.6 TB/s; with 32 rows 166 MB in 39 us, 4.2 TB/s: 370 registers leave one wave
+// per SIMD, whose first and last chunks nothing hides.
 // ---------------------------------------------------------------------------
 struct PagedAttendArgs {
   PagedArgs c;
@@ -281,9 +286,10 @@ struct PagedAttendArgs {
 };
 
 constexpr int PAGED_ROUND = 256;         // sequences whose lengths a wave holds at a time, four per lane
-// Chunks that a sequence counts beside its own.  us at 0 / 2 / 4 / 8: 64 sequences of
-// 5 to 16384 entries 121.9 / 110.5 / 106.3 / 105.2, 300 of 20 to 900 78.1 / 70.7 / 69.6 /
-// 69.9, 48 of 1024 to 9216 of width 256 264.6 / 264.7 / 265.1 / 267.8.
+// Chunks that a sequence counts beside its own.  us at 0 / 2 / 4 / 6 / 8: 64 sequences
+// of 5 to 16384 entries 111.3 / 99.1 / 96.5 / 95.2 / 96.2, 300 of 20 to 900 72.5 / 64.8 /
+// 65.2 / 66.2 / 66.1, 48 of 1024 to 9216 of width 256 237 / 236 / 237 / 239 / 241, 5 of
+// 1500 to 20011 with 32 rows 47.7 / 46.0 / 45.1 / 45.0 / 44.9.
 constexpr int PAGED_PAD = 6;
 constexpr float PAGED_SLACK = 6.f;       // weights reach e^6 before they are scaled back
 constexpr float LOG2E = 1.4426950408889634f;
