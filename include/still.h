@@ -389,7 +389,7 @@ typedef struct {
   int32_t causal;       /* 0 or 1                                                           */
   float scale;          /* logit scale; 0 -> 1/sqrt(d)                                      */
   double rope_theta;    /* > 0: rotate q at q_positions; 0: q used as given                 */
-  int64_t q_stride;     /* elements between tokens of q, a multiple of 16 bytes;
+  int64_t q_stride;     /* elements between tokens of q, >= 0 and a multiple of 16 bytes;
                            0 -> H * group * d                                               */
 } still_paged_attend_config;
 

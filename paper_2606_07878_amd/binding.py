@@ -643,7 +643,9 @@ def paged_gather(k_pages, v_pages, table, lens, seq: int, n: int, start: int = 0
     current stream; into ``out`` (such a tuple) where given."""
     torch = _torch()
     cache, seqs, dev = _paged(torch, k_pages, v_pages, beta_pages, table, lens)
-    n = int(n)
+    seq, start, n = int(seq), int(start), int(n)
+    if max(abs(seq), abs(start), abs(n)) >= 1 << 31:
+        _refuse(-2, f"entries [{start}, {start + n}) of sequence {seq} asked for")
     shape = (cache.n_kv_heads, n, cache.head_dim)
     if out is None:
         if n < 0:
@@ -658,7 +660,7 @@ def paged_gather(k_pages, v_pages, table, lens, seq: int, n: int, start: int = 0
         _want(out[1], "out[1]", k_pages.dtype, shape, dev)
         if beta_pages is not None:
             _want(out[2], "out[2]", torch.float32, shape[:2], dev)
-    _on(torch, dev, (_lib or lib()).still_paged_gather, ctypes.byref(cache), ctypes.byref(seqs), int(seq), int(start), n,
+    _on(torch, dev, (_lib or lib()).still_paged_gather, ctypes.byref(cache), ctypes.byref(seqs), seq, start, n,
         out[0].data_ptr(), out[1].data_ptr(), None if beta_pages is None else out[2].data_ptr())
     return out
 
@@ -683,8 +685,8 @@ def paged_attend(q, k_pages, v_pages, table, lens, causal: bool = False, scale: 
         _refuse(-2, f"q {tuple(shape)} does not fit {n} sequences and pages {tuple(k_pages.shape)}")
     _want_rows(q, "q", k_pages, shape)
     qs = q.stride()
-    if qs[1] != d:
-        _refuse(-1, "q's tokens are not contiguous")
+    if qs[1] != d or (qs[0] == 0 and tokens > 1):   # (a stride of 0 means dense tokens to the C call)
+        _refuse(-1, "q's tokens are not contiguous, or the same one")
     pos = None
     if q_positions is not None:
         _want(q_positions, "q_positions", torch.float64, (tokens,), dev)
@@ -694,8 +696,8 @@ def paged_attend(q, k_pages, v_pages, table, lens, causal: bool = False, scale: 
         out = torch.empty(shape, dtype=q.dtype, device=q.device)
     else:
         _want(out, "out", q.dtype, shape, dev)
-    if workspace is not None and workspace.get_device() != dev:
-        _refuse(-1, f"workspace is on {workspace.device}, the pages on {k_pages.device}")
+    if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
+        _refuse(-1, f"workspace is on {workspace.device}, the pages on {k_pages.device}, or it is not contiguous")
     room = 0 if workspace is None else workspace.numel()
     if room < STILL_PAGED_WORKSPACE_BYTES:
         need = still_paged_attend_workspace_size(cache, cfg)

@@ -238,7 +238,8 @@ still_status still_paged_attend(const still_paged_cache* cache, const still_page
   if (s != STILL_OK || (s = check_seqs(cache, seqs)) != STILL_OK) return s;
   const long esize = cache->mode == STILL_MODE_FP32 ? 4 : 2;
   const long q_row = (long)cache->n_kv_heads * cfg->group * cache->head_dim;
-  if (cfg->q_stride * esize % 16) return fail(STILL_E_SHAPE, "q_stride must be a multiple of 16 bytes");
+  if (cfg->q_stride < 0 || cfg->q_stride * esize % 16)
+    return fail(STILL_E_SHAPE, "q_stride must be >= 0 and a multiple of 16 bytes");
   if ((s = check_pages(cache)) != STILL_OK || (s = check_theta(cfg->rope_theta, q_positions)) != STILL_OK ||
       (s = check_ptr(q, "q", true)) != STILL_OK || (s = check_ptr(out, "out", true)) != STILL_OK)
     return s;

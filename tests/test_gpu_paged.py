@@ -504,6 +504,11 @@ def test_binding_refuses_rows_that_do_not_fit():
     refused(-2, binding.paged_append, k, k, *P, offsets=torch.zeros(2, dtype=torch.int32, device="cuda"))
     refused(-1, binding.paged_append, k, k, *P, beta=torch.zeros(2, 2, device="cuda"))   # a cache without bias
     refused(-2, binding.paged_append, k, k, *P, beta=torch.zeros(2, 3, device="cuda"), beta_pages=c.beta)
+    refused(-1, binding.paged_attend, q[:1].expand(2, 4, 64), *P)       # the same token twice
+    refused(-1, binding.paged_attend, q, *P, workspace=torch.empty(1 << 20, dtype=torch.uint8, device="cuda")[::2])
+    refused(-2, binding.paged_attend, q, P[0], P[1], P[2][:1].expand(2, -1), P[3])       # one table row for both
+    refused(-2, binding.paged_gather, *P, 0, 5, start=1 << 32)
+    refused(-2, binding.paged_gather, *P, 1 << 32, 5)
     refused(-2, binding.paged_gather, *P, 2, 5)
     refused(-2, binding.paged_gather, *P, 0, 33)
     refused(-2, binding.paged_gather, *P, 0, -1)

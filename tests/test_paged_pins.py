@@ -156,7 +156,7 @@ def test_bad_gather(args, status):
 @pytest.mark.parametrize("kw,status", [
     (dict(group=0), -2), (dict(n_queries=0), -2), (dict(n_queries=9), -5), (dict(group=1 << 30, n_queries=4), -5),
     (dict(causal=2), -1), (dict(scale=float("nan")), -1), (dict(scale=-1.0), -1), (dict(rope_theta=1e6), -1),
-    (dict(rope_theta=-1.0), -1), (dict(q_stride=4100), -2)])
+    (dict(rope_theta=-1.0), -1), (dict(q_stride=4100), -2), (dict(q_stride=-4096), -2)])
 def test_bad_attend(kw, status):
     assert _attend(cfg=_acfg(**kw)) == status
     assert binding.still_last_error()
