@@ -560,6 +560,8 @@ def _refuse_paged(torch, k_pages, v_pages, beta_pages, table, lens) -> None:
         _want(beta_pages, "beta_pages", torch.float32, shape[:3], dev)
     if table.dim() != 2 or table.dtype != torch.int32 or (table.stride(1) != 1 and table.shape[1] > 1):
         _refuse(-2, "table is no int32 tensor [n_seqs, pages] with contiguous rows")
+    if table.shape[0] > 1 and table.stride(0) >= 1 << 31:
+        _refuse(-2, f"table rows {table.stride(0)} entries apart")
     if table.get_device() != dev:
         _refuse(-1, f"table is on {table.device}, the pages on {k_pages.device}")
     _want(lens, "lens", torch.int32, table.shape[:1], dev)
@@ -575,7 +577,7 @@ def _paged(torch, k_pages, v_pages, beta_pages, table, lens):
             and v_pages.shape == shape and k_pages.is_contiguous() and v_pages.is_contiguous()
             and v_pages.get_device() == dev and table.dtype is i32 and len(size) == 2 and lens.dtype is i32
             and lens.shape == size[:1] and lens.is_contiguous() and lens.get_device() == dev
-            and table.get_device() == dev and (table.stride(1) == 1 or size[1] <= 1)
+            and table.get_device() == dev and (table.stride(1) == 1 or size[1] <= 1) and (size[0] <= 1 or table.stride(0) < 1 << 31)
             and (beta_pages is None or beta_pages.dtype is torch.float32 and beta_pages.shape == shape[:3]
                  and beta_pages.is_contiguous() and beta_pages.get_device() == dev)):
         _refuse_paged(torch, k_pages, v_pages, beta_pages, table, lens)
@@ -615,6 +617,8 @@ def paged_append(k, v, k_pages, v_pages, table, lens, offsets=None, positions=No
     if k.dim() != 3:
         _refuse(-2, f"k has {k.dim()} dimensions, not [n_tokens, H, d]")
     n = k.shape[0]
+    if n >= 1 << 31:
+        _refuse(-2, f"{n} tokens given")
     shape = (n, cache.n_kv_heads, cache.head_dim)
     _want_rows(k, "k", k_pages, shape)
     _want_rows(v, "v", k_pages, shape)
@@ -681,7 +685,7 @@ def paged_attend(q, k_pages, v_pages, table, lens, causal: bool = False, scale: 
         _refuse(-2, f"q has {len(shape)} dimensions, not [n_seqs * n_queries, H * group, d]")
     tokens, Hq, d = shape
     H, n = cache.n_kv_heads, seqs.n_seqs
-    if d != cache.head_dim or Hq < H or Hq % H or tokens < n or tokens % n:
+    if n < 1 or H < 1 or d != cache.head_dim or Hq < H or Hq % H or tokens < n or tokens % n:
         _refuse(-2, f"q {tuple(shape)} does not fit {n} sequences and pages {tuple(k_pages.shape)}")
     _want_rows(q, "q", k_pages, shape)
     qs = q.stride()
@@ -721,7 +725,8 @@ def compact_paged(cfg: configs.CompactorConfig, weights: List[Dict[str, object]]
     up with their bias.  ``positions`` [n] are the entries' float64 logical
     positions; lens[seq] holds n, and the pages up to the new length are there.
     Sets lens[seq] on the current stream and returns the new positions
-    [n - (end - start) + t]; pages behind the new length are free.
+    [n - (end - start) + t]; pages behind the new length are free.  A page that
+    another sequence's table names too changes for that one as well.
     A cache that keeps bias passes ``beta_pages``; new entries without
     ``w_beta`` get bias 0."""
     torch = _torch()
@@ -736,9 +741,29 @@ def compact_paged(cfg: configs.CompactorConfig, weights: List[Dict[str, object]]
     length = n - (end - start) + t
     if not 0 <= seq < table.shape[0]:
         _refuse(-2, f"sequence {seq} outside [0, {table.shape[0]})")
-    if length > table.shape[1] * k_pages[0].shape[2]:
-        _refuse(-2, f"{length} entries do not fit the sequence's {table.shape[1]} pages")
+    for i in range(L):
+        if tuple(k_pages[i].shape[1::2]) != (cfg.n_kv_heads, cfg.head_dim):
+            _refuse(-2, f"layer {i}: pages {tuple(k_pages[i].shape)} for a compactor of {cfg.n_kv_heads} heads of width "
+                        f"{cfg.head_dim}")
+        if k_pages[i].dtype != k_pages[0].dtype:
+            _refuse(-3, f"layer {i}: pages of {k_pages[i].dtype}, layer 0's of {k_pages[0].dtype}")
+        if max(n, length) > table.shape[1] * k_pages[i].shape[2]:
+            _refuse(-2, f"{max(n, length)} entries do not fit the sequence's {table.shape[1]} pages")
+        if w_beta is not None and beta_pages[i] is None:
+            _refuse(-1, f"layer {i}: w_beta given to a cache without beta")
     _want(positions, "positions", torch.float64, (n,), k_pages[0].get_device())
+    for i in range(L):
+        _paged(torch, k_pages[i], v_pages[i], None if beta_pages is None else beta_pages[i], table, lens)
+    with torch.cuda.device(k_pages[0].device):
+        return _compact_paged(cfg, weights, k_pages, v_pages, table, lens, seq, n, positions, rope_theta, t, start, end,
+                              w_beta, beta_pages, beta_max, mass_alpha, log_x, rerotate)
+
+
+def _compact_paged(cfg, weights, k_pages, v_pages, table, lens, seq, n, positions, rope_theta, t, start, end, w_beta,
+                   beta_pages, beta_max, mass_alpha, log_x, rerotate):
+    """compact_paged behind its checks, with the pages' GPU current."""
+    torch = _torch()
+    L, length = len(k_pages), n - (end - start) + t
     dev, mode = k_pages[0].device, (configs.MODE_FP32 if k_pages[0].dtype == torch.float32 else configs.MODE_BF16)
     row = table[seq:seq + 1]
     to = [torch.full((1,), x, dtype=torch.int32, device=dev) for x in (start + t, length)]
@@ -748,9 +773,6 @@ def compact_paged(cfg: configs.CompactorConfig, weights: List[Dict[str, object]]
     # every layer is compacted before the first one's pages change: a refusal leaves them as they were
     new = []
     for i in range(L):
-        if tuple(k_pages[i].shape[1::2]) != (cfg.n_kv_heads, cfg.head_dim):
-            _refuse(-2, f"layer {i}: pages {tuple(k_pages[i].shape)} for a compactor of {cfg.n_kv_heads} heads of width "
-                        f"{cfg.head_dim}")
         K, V = paged_gather(k_pages[i], v_pages[i], table, lens, seq, end - start, start)
         if w_beta is None:
             Ck, Cv, pq = compact_layer(cfg, weights[i], K, V, inside, rope_theta, t, rerotate=rerotate, mode=mode,

@@ -516,6 +516,38 @@ def test_binding_refuses_rows_that_do_not_fit():
     refused(-2, binding.paged_gather, *P, 0, 5, out=(k, k))
 
 
+def test_binding_refuses_no_sequences_and_counts_past_32_bits():
+    from paper_2606_07878_amd import binding
+    c = Paged(66, [20, 30], 2, 64, 16, BF16).cuda()
+    none = (c.k, c.v, c.table[:0], c.lens[:0])
+    row = c.rows(1).cuda()
+    many = row.expand((1 << 32) + 2, 2, 64)                             # the low 32 bits say 2
+    before = c.k.clone()
+    for f, args in ((binding.paged_attend, (c.rows(2, 4)[:0].cuda(), *none)), (binding.paged_append, (row[:0], row[:0], *none)),
+                    (binding.paged_gather, (*none, 0, 0)), (binding.paged_append, (many, many, *c.pages()))):
+        with pytest.raises(binding.StillError) as e:
+            f(*args)
+        assert e.value.status == -2, str(e.value)
+    assert torch.equal(c.k, before)
+
+
+def test_compact_paged_changes_nothing_where_a_layers_bias_pages_do_not_fit():
+    from paper_2606_07878_amd import binding
+    w = configs.shrink(configs.get_workload(1), n_tokens=100, t=32)
+    c = Paged(67, [100], w.cfg.n_kv_heads, w.cfg.head_dim, 16, BF16).cuda()
+    W = weights_to_device(synth.make_weights(w, 0, t=32), BF16)
+    k2, v2 = c.k.clone(), c.v.clone()
+    pos = torch.arange(100, dtype=torch.float64, device="cuda")
+    before = c.k.clone(), c.v.clone(), c.beta.clone()
+    with pytest.raises(binding.StillError) as e:
+        binding.compact_paged(w.cfg, [W, W], [c.k, k2], [c.v, v2], c.table, c.lens, 0, 100, pos, w.rope_theta, 32,
+                              beta_pages=[c.beta, c.beta[:1]])
+    assert e.value.status == -2
+    torch.cuda.synchronize()
+    assert torch.equal(c.k, before[0]) and torch.equal(c.v, before[1]) and torch.equal(c.beta, before[2])
+    assert c.lens.tolist() == [100]
+
+
 # ---- together ----------------------------------------------------------------
 
 def test_decode_loop_matches_the_oracle():

@@ -242,3 +242,28 @@ def test_compact_paged_refuses_bad_ranges():
     _refused(-2, binding.compact_paged, w.cfg, [{}, {}], [c.k], [c.v], c.table, c.lens, 1, 30, pos, 1e6, 8)
     _refused(-1, binding.compact_paged, *args, 1, 30, pos, 1e6, 8, w_beta=[pos])
     _refused(-2, binding.compact_paged, *args, 1, 30, pos[:5], 1e6, 8)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="CPU refusals only")
+def test_compact_paged_checks_every_layer_before_any_changes():
+    w = configs.get_workload(1)
+    c = Paged(6, [20, 30], w.cfg.n_kv_heads, w.cfg.head_dim, 16, configs.MODE_BF16)
+    pos = torch.arange(30, dtype=torch.float64)
+
+    def refused(status, k2, v2, seq_len=30, **kw):
+        _refused(status, binding.compact_paged, w.cfg, [{}, {}], [c.k, k2], [c.v, v2], c.table, c.lens, 1, seq_len, pos,
+                 1e6, 8, **kw)
+
+    refused(-1, c.k, c.v)                                                        # no GPU tensors
+    refused(-3, c.k.float(), c.v.float())                                        # layers of two types
+    refused(-2, c.k[:, :1], c.v[:, :1])
+    refused(-2, c.k[:, :, :8], c.v[:, :, :8])                                    # layer 1's pages hold less
+    refused(-1, c.k, c.v, w_beta=[pos, pos], beta_pages=[c.beta, None])
+    refused(-2, c.k[0], c.v[0])
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="CPU refusals only")
+def test_binding_refuses_table_rows_too_far_apart():
+    c = Paged(7, [20, 30], 2, 64, 16, configs.MODE_BF16)
+    far = torch.empty_strided((2, 2), (1 << 31, 1), dtype=torch.int32, device="meta")
+    _refused(-2, binding.paged_attend, c.rows(2, 4), c.k, c.v, far, c.lens)
