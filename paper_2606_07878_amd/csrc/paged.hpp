@@ -250,9 +250,8 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(PagedGatherArgs a) {
 //   lane's.
 //   bf16: the lane's 8 entries are the 8 contraction indices of one
 //   v_mfma_f32_16x16x32_bf16; the 16-bit transposition is v_perm in the lane.
-//   Weights (and rotated queries) go in as two bf16 parts, hi + lo, 16 bits of
-//   mantissa: one part alone would round each by 2^-9.  fp32: one
-//   v_mfma_f32_16x16x4_f32 per entry.
+//   Weights go in as three bf16 parts, all their 24 bits (two parts would round them by
+//   2^-17), rotated queries as two.  fp32: one v_mfma_f32_16x16x4_f32 per entry.
 // Keys of the next chunk are loaded once the logits have used this one's, values
 // once P.V has; page numbers are read two chunks ahead, before the keys of the
 // next one, so that they are there with them (loads return in order).  A tile is
@@ -337,6 +336,25 @@ inline size_t paged_lds_bytes(int R, int nq, bool rot) {
   const size_t q = (size_t)NR * TL::QBYTES, o = (size_t)TL::NW * R * TL::OROW * sizeof(float);
   const size_t angles = rot ? (size_t)nq * D / 2 * sizeof(float2) : 0;
   return paged_alias(D, NR, SW) ? std::max(q + angles, o) : q + std::max(angles, o);
+}
+
+// x as the sum of three bf16: each takes the leading 8 bits of what the ones before
+// leave, 24 in all, and the remainders are exact, so nothing of an fp32 value is lost.
+// (Cut instead of rounded: a mask and a subtraction each, words packed by v_perm.)
+__device__ __forceinline__ void bf16_parts(const float (&x)[8], bf16x8 (&p)[3]) {
+  float r[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) r[k] = x[k];
+#pragma unroll
+  for (int part = 0; part < 3; ++part) {
+    u32x4 w;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = __builtin_amdgcn_perm(__float_as_uint(r[2 * k + 1]), __float_as_uint(r[2 * k]), 0x07060302u);
+    p[part] = __builtin_bit_cast(bf16x8, w);
+    if (part < 2)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) r[k] -= __uint_as_float(__float_as_uint(r[k]) & 0xffff0000u);
+  }
 }
 
 // fast base-2 exponential (results below 2^-126 are zero)
@@ -778,15 +796,13 @@ void paged_attend_kernel(PagedAttendArgs a) {
           if constexpr (TL::B16) {
 #pragma unroll
             for (int k2 = 0; k2 < NKT; k2 += 2) {
-              bf16x8 ph[NR], pl[NR];
+              bf16x8 pp[NR][3];
 #pragma unroll
-              for (int rt = 0; rt < NR; ++rt)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                  const float p = x[rt][k2 + (k >> 2)][k & 3];
-                  ph[rt][k] = (__bf16)p;
-                  pl[rt][k] = (__bf16)(p - (float)ph[rt][k]);
-                }
+              for (int rt = 0; rt < NR; ++rt) {
+                const f32x4 &a0 = x[rt][k2], &a1 = x[rt][k2 + 1];
+                const float p[8] = {a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]};
+                bf16_parts(p, pp[rt]);
+              }
 #pragma unroll
               for (int e = 0; e < FPT; e += 2) {   // an even and an odd feature of one word
                 u32x4 t0, t1;
@@ -798,12 +814,12 @@ void paged_attend_kernel(PagedAttendArgs a) {
                 }
                 const bf16x8 w0 = __builtin_bit_cast(bf16x8, t0), w1 = __builtin_bit_cast(bf16x8, t1);
 #pragma unroll
-                for (int rt = 0; rt < NR; ++rt) {
-                  o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w0, ph[rt], o[rt][e], 0, 0, 0);
-                  o[rt][e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w1, ph[rt], o[rt][e + 1], 0, 0, 0);
-                  o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w0, pl[rt], o[rt][e], 0, 0, 0);
-                  o[rt][e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w1, pl[rt], o[rt][e + 1], 0, 0, 0);
-                }
+                for (int rt = 0; rt < NR; ++rt)
+#pragma unroll
+                  for (int part = 0; part < 3; ++part) {
+                    o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w0, pp[rt][part], o[rt][e], 0, 0, 0);
+                    o[rt][e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w1, pp[rt][part], o[rt][e + 1], 0, 0, 0);
+                  }
               }
             }
           } else {

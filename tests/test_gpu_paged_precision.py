@@ -1,0 +1,78 @@
+"""What the paged attention keeps of its weights, rotated queries and
+exponentials: 24 bits, as the dense attention does.
+
+The stored bf16 output would hide anything finer, so the values are made to
+cancel: the output is some 2^-18 of its terms, and what the weights lost shows
+in it whole.  Each bar counts the roundings by 2^-24 (half a step) or 2^-23
+(an instruction that may be off by a step).
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged as O
+from paper_2606_07878_amd import configs
+from tests.helpers import log
+
+pytestmark = pytest.mark.gpu
+
+BF16, FP32 = configs.MODE_BF16, configs.MODE_FP32
+U = 2.0 ** -24
+
+
+def bf(x):
+    """Nearest bf16 of float64 values, as float64."""
+    return torch.from_numpy(np.asarray(x)).to(torch.bfloat16).double().numpy()
+
+
+def f32(x):
+    return np.asarray(x, np.float32).astype(np.float64)
+
+
+def pages_of(rows, P=16):
+    """[S, H, n, ...] (n <= P) as one page per sequence, the slots behind the entries NaN."""
+    full = np.full(rows.shape[:2] + (P,) + rows.shape[3:], np.nan)
+    full[:, :, : rows.shape[2]] = rows
+    return torch.from_numpy(full)
+
+
+def run(k, v, beta, q, dtype, width, pos=None, theta=0.0, scale=0.0):
+    """(output, oracle's) of sequences of n entries: k, v [S, H, n, d], beta [S, H, n], q [S, H, d], values of `dtype`."""
+    from paper_2606_07878_amd import binding
+    S, H, n, d = v.shape
+    table = torch.full((S, width), -1, dtype=torch.int32)
+    table[:, 0] = torch.arange(S, dtype=torch.int32)
+    lens = torch.full((S,), n, dtype=torch.int32)
+    kp, vp, bp = pages_of(k), pages_of(v), pages_of(beta)
+    got = binding.paged_attend(torch.from_numpy(q).to(dtype).cuda(), kp.to(dtype).cuda(), vp.to(dtype).cuda(), table.cuda(),
+                               lens.cuda(), beta_pages=bp.float().cuda(), scale=scale,
+                               q_positions=None if pos is None else torch.from_numpy(pos).cuda(), rope_theta=theta)
+    ref = O.attend(q, kp.numpy(), vp.numpy(), table.numpy(), lens.numpy(), False, scale, bp.numpy(), pos, theta)
+    return got.double().cpu().numpy(), ref
+
+
+# a workgroup per sequence and head, a wave, parts of the line
+KERNELS = [(30, 1), (40, 1), (30, 80)]
+
+
+@pytest.mark.parametrize("seqs,width", KERNELS)
+def test_weights(seqs, width):
+    """Logits are the bias (q = 0): weights 1, p2 in (0.5, 1) and p3 near 2^-9.4;
+    v2 takes v1's weighted value away, v3 what bf16 left of it.  9 products
+    (three entries, at most three parts) are summed in at most 2^-23 of |v1|
+    each; p2's exponential is off by 3 U and p3's counts 2^-8 of that.  A
+    weight of 16 bits is off by up to 2^-17."""
+    rng = np.random.default_rng(seqs + width)
+    H, d = 8, 64
+    beta = f32(np.stack([np.zeros((seqs, H)), rng.uniform(-0.69, 0.0, (seqs, H)), rng.uniform(-7.0, -6.0, (seqs, H))], -1))
+    p = np.exp(beta)
+    v1 = bf(rng.uniform(1.0, 2.0, (seqs, H, d)) * rng.choice([-1.0, 1.0], (seqs, H, d)))
+    v2 = bf(-v1 / p[..., 1:2])
+    v3 = bf(-(v1 + p[..., 1:2] * v2) / p[..., 2:3])
+    v = np.stack([v1, v2, v3], 2)
+    k = bf(rng.standard_normal(v.shape))
+    got, ref = run(k, v, beta, np.zeros((seqs, H, d)), torch.bfloat16, width)
+    bound = 24 * U * np.abs(v1) / p.sum(-1)[..., None] + 2.0 ** -8 * np.abs(ref)
+    worst = (np.abs(got - ref) / bound).max()
+    log(f"  weights: worst error {worst:.2f} of the bound")
+    assert worst <= 1.0
