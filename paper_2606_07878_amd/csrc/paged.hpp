@@ -250,8 +250,10 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(PagedGatherArgs a) {
 //   lane's.
 //   bf16: the lane's 8 entries are the 8 contraction indices of one
 //   v_mfma_f32_16x16x32_bf16; the 16-bit transposition is v_perm in the lane.
-//   Weights go in as three bf16 parts, all their 24 bits (two parts would round them by
-//   2^-17), rotated queries as two.  fp32: one v_mfma_f32_16x16x4_f32 per entry.
+//   Weights and rotated queries go in as three bf16 parts, all their 24 bits.  Two
+//   parts would round each by 2^-17: 45.0 us instead of 48.0 for 8 causal rows of 5
+//   sequences, 87 instead of 97 for 16 sequences of width 64 and 32 rows, no difference
+//   above 1 % to 16 rows.  fp32: one v_mfma_f32_16x16x4_f32 per entry.
 // Keys of the next chunk are loaded once the logits have used this one's, values
 // once P.V has; page numbers are read two chunks ahead, before the keys of the
 // next one, so that they are there with them (loads return in order).  A tile is
@@ -323,17 +325,19 @@ struct PagedTile {
   static constexpr int PB = VB < 16 ? VB : 16, EPV = PB / (int)sizeof(IT);   // bytes and features of a piece of a value row
   static constexpr int QROW = ROWB + 16;                // query rows in LDS (padded: 16 rows at one piece)
   static constexpr int OROW = D + 4;
-  static constexpr int QBYTES = 16 * QROW * (B16 ? 2 : 1);   // per 16 rows; bf16: two parts
+  static constexpr int QPART = 16 * NR * QROW;
 };
 
-// Dynamic LDS: the query rows, behind them the waves' sums [waves][R][OROW] or,
-// before there are any, the queries' angles [nq][D / 2].  The sums take the rows'
-// place where both do not fit 160 KB, and in workgroups of one wave, many of which
-// share a CU.
+// Dynamic LDS: the query rows (rotated bf16 ones in three parts), behind them the
+// waves' sums [waves][R][OROW] or, before there are any, the queries' angles
+// [nq][D / 2].  The sums take the rows' place where both do not fit 160 KB, and in
+// workgroups of one wave, many of which share a CU.
 constexpr bool paged_alias(int D, int NR, int SW) { return SW == 1 || D * NR > 256; }
+template <class TL>
+inline __host__ __device__ int paged_q_bytes(bool rot) { return (TL::B16 && rot ? 3 : 1) * TL::QPART; }
 template <class TL, int D, int NR, int SW>
 inline size_t paged_lds_bytes(int R, int nq, bool rot) {
-  const size_t q = (size_t)NR * TL::QBYTES, o = (size_t)TL::NW * R * TL::OROW * sizeof(float);
+  const size_t q = paged_q_bytes<TL>(rot), o = (size_t)TL::NW * R * TL::OROW * sizeof(float);
   const size_t angles = rot ? (size_t)nq * D / 2 * sizeof(float2) : 0;
   return paged_alias(D, NR, SW) ? std::max(q + angles, o) : q + std::max(angles, o);
 }
@@ -425,16 +429,15 @@ void paged_attend_kernel(PagedAttendArgs a) {
   constexpr int QROW = TL::QROW, OROW = TL::OROW, NT = 64 * NW, HD = D / 2;
   constexpr bool ALIAS = paged_alias(D, NR, SW);
   extern __shared__ float4 paged_smem[];
-  char* qs = (char*)paged_smem;                  // [16 NR][QROW], bf16: the same again for the low parts
-  char* ql = qs + 16 * NR * QROW;
-  float* osum = (float*)(qs + (ALIAS ? 0 : NR * TL::QBYTES));   // [NW][R][OROW]
-  float2* cs = (float2*)(qs + NR * TL::QBYTES);   // [nq][D / 2] (cos, sin) of the queries, where the sums come later
+  char* qs = (char*)paged_smem;                  // [16 NR][QROW], rotated bf16 rows: three parts of that
   __shared__ float wm[NW][16 * NR], wl[NW][16 * NR];
   const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
   const int l = lane & 15, lg = lane >> 4;
   const int h = blockIdx.x, g = SINGLE ? 0 : blockIdx.y, R = a.group * a.nq, Hq = a.c.H * a.group;
   const int n_seqs = a.c.n_seqs, pad = n_seqs > 1 ? PAGED_PAD : 0;
   const bool rot = a.qpos != nullptr;
+  float* osum = (float*)(qs + (ALIAS ? 0 : paged_q_bytes<TL>(rot)));   // [NW][R][OROW]
+  float2* cs = (float2*)(qs + paged_q_bytes<TL>(rot));   // [nq][D / 2] (cos, sin) of the queries, where the sums come later
   const int koff = l * ROWB + lg * 16, voff = 4 * lg * ROWB + l * TL::PB;
   auto head_of = [&](int r) { return r * a.nq_inv >> 16; };   // of the group; the query is r - nq * that
   auto out_row = [&](int s, int r) {
@@ -481,18 +484,16 @@ void paged_attend_kernel(PagedAttendArgs a) {
           x0[u] = y;
         }
         if constexpr (TL::B16) {
-          bf16x8 h0, h1, l0, l1;
+          bf16x8 p0[3], p1[3];
+          bf16_parts(x0, p0);
+          bf16_parts(x1, p1);
+          qr[k][0] = __builtin_bit_cast(u32x4, p0[0]);
+          qr[k][1] = __builtin_bit_cast(u32x4, p1[0]);
 #pragma unroll
-          for (int u = 0; u < EPP; ++u) {
-            h0[u] = (__bf16)x0[u];
-            h1[u] = (__bf16)x1[u];
-            l0[u] = (__bf16)(x0[u] - (float)h0[u]);
-            l1[u] = (__bf16)(x1[u] - (float)h1[u]);
+          for (int part = 1; part < 3; ++part) {
+            *(bf16x8*)(qs + part * TL::QPART + r * QROW + 16 * (e % HP)) = p0[part];
+            *(bf16x8*)(qs + part * TL::QPART + r * QROW + 16 * (e % HP + HP)) = p1[part];
           }
-          qr[k][0] = __builtin_bit_cast(u32x4, h0);
-          qr[k][1] = __builtin_bit_cast(u32x4, h1);
-          *(bf16x8*)(ql + r * QROW + 16 * (e % HP)) = l0;
-          *(bf16x8*)(ql + r * QROW + 16 * (e % HP + HP)) = l1;
         } else {
           qr[k][0] = u32x4{__float_as_uint(x0[0]), __float_as_uint(x0[1]), __float_as_uint(x0[2]), __float_as_uint(x0[3])};
           qr[k][1] = u32x4{__float_as_uint(x1[0]), __float_as_uint(x1[1]), __float_as_uint(x1[2]), __float_as_uint(x1[3])};
@@ -725,15 +726,17 @@ void paged_attend_kernel(PagedAttendArgs a) {
             }
           if (TL::B16 && rot) {
 #pragma unroll
-            for (int p = 0; p < NP; ++p)
+            for (int part = 1; part < 3; ++part)
 #pragma unroll
-              for (int rt = 0; rt < NR; ++rt) {
-                const u32x4 qv = *(const u32x4*)(ql + (16 * rt + l) * QROW + 64 * p + 16 * lg);
+              for (int p = 0; p < NP; ++p)
 #pragma unroll
-                for (int kt = 0; kt < NKT; ++kt)
-                  x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                      __builtin_bit_cast(bf16x8, kp[kt][p]), __builtin_bit_cast(bf16x8, qv), x[rt][kt], 0, 0, 0);
-              }
+                for (int rt = 0; rt < NR; ++rt) {
+                  const u32x4 qv = *(const u32x4*)(qs + part * TL::QPART + (16 * rt + l) * QROW + 64 * p + 16 * lg);
+#pragma unroll
+                  for (int kt = 0; kt < NKT; ++kt)
+                    x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        __builtin_bit_cast(bf16x8, kp[kt][p]), __builtin_bit_cast(bf16x8, qv), x[rt][kt], 0, 0, 0);
+                }
           }
           f32x4 bc[NKT];
 #pragma unroll

@@ -76,3 +76,33 @@ def test_weights(seqs, width):
     worst = (np.abs(got - ref) / bound).max()
     log(f"  weights: worst error {worst:.2f} of the bound")
     assert worst <= 1.0
+
+
+@pytest.mark.parametrize("seqs,width", KERNELS)
+def test_rotated_queries(seqs, width):
+    """A query of one feature a, keys of one feature x and of none: after the
+    rotation one product scale a x cos(phi) remains, some hundreds, against the
+    second entry's bias of the same size.  The logit is off by 2e-7 scale a x
+    (the cosine), 6 U of it (rotation, scale, bias and its sum, each half a
+    step) and three parts summed in a step each (6 U); equal weights turn half
+    of that into output.  A query of 16 bits is off by up to 2^-17."""
+    rng = np.random.default_rng(seqs + width)
+    H, d, theta, scale = 8, 64, 1e6, 0.125
+    pos = rng.integers(0, 131072, seqs).astype(np.float64)
+    q, k, v = np.zeros((seqs, H, d)), np.zeros((seqs, H, 2, d)), np.zeros((seqs, H, 2, d))
+    beta, size = np.zeros((seqs, H, 2)), np.zeros((seqs, H, 1))
+    phi = pos[:, None] * theta ** (-2.0 * np.arange(d // 2) / d)
+    for s in range(seqs):
+        for h in range(H):
+            e = rng.choice(np.flatnonzero(np.abs(np.cos(phi[s])) > 0.8))
+            a, x = bf(rng.uniform(16.0, 32.0)), bf(rng.uniform(64.0, 128.0))
+            q[s, h, e], k[s, h, 0, e] = a, x
+            beta[s, h, 1] = f32(scale * a * x * np.cos(phi[s, e]))
+            size[s, h] = scale * a * x
+    v[:, :, 0] = bf(rng.uniform(1.0, 2.0, (seqs, H, d)))
+    v[:, :, 1] = -v[:, :, 0]
+    got, ref = run(k, v, beta, q, torch.bfloat16, width, pos, theta, scale)
+    bound = np.abs(v[:, :, 0]) * (0.5 * (2e-7 + 12 * U) * size + 12 * U) + 2.0 ** -8 * np.abs(ref)
+    worst = (np.abs(got - ref) / bound).max()
+    log(f"  rotated queries: worst error {worst:.2f} of the bound")
+    assert worst <= 1.0
