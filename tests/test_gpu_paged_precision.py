@@ -106,3 +106,20 @@ def test_rotated_queries(seqs, width):
     worst = (np.abs(got - ref) / bound).max()
     log(f"  rotated queries: worst error {worst:.2f} of the bound")
     assert worst <= 1.0
+
+
+@pytest.mark.parametrize("seqs,width", KERNELS)
+def test_small_weights(seqs, width):
+    """fp32: a weight of e^-3 .. e^-60 beside one of 1 whose value is 0, so that
+    the output is the small weight.  The exponential is off by 3 U (the
+    instruction's step and its correction), the sum, its reciprocal, the two
+    products and the store by a step or half of one each: 9 U."""
+    rng = np.random.default_rng(seqs + width)
+    H, d = 8, 64
+    beta = f32(np.stack([np.zeros((seqs, H)), rng.uniform(-60.0, -3.0, (seqs, H))], -1))
+    v = np.zeros((seqs, H, 2, d))
+    v[:, :, 1] = f32(rng.uniform(1.0, 2.0, (seqs, H, d)))
+    got, ref = run(f32(rng.standard_normal(v.shape)), v, beta, np.zeros((seqs, H, d)), torch.float32, width)
+    worst = (np.abs(got - ref) / np.abs(ref)).max() / (12 * U)
+    log(f"  small weights: worst error {worst:.2f} of the bound")
+    assert worst <= 1.0
