@@ -1,0 +1,106 @@
+"""The kernels of the paged attention that a call reaches by its table's
+capacity, against the fp64 oracle: entries split over workgroups and joined,
+with ordinary and streaming loads, at every width, type and row count; their
+addresses past 4 GiB; and captured, on a workspace that other calls use too.
+"""
+import pytest
+import torch
+
+from paper_2606_07878_amd import configs
+from tests.helpers import log
+from tests.paged_cases import Paged
+from tests.test_gpu_paged import check_attend
+
+pytestmark = pytest.mark.gpu
+
+BF16, FP32 = configs.MODE_BF16, configs.MODE_FP32
+STREAM_BYTES = 256 << 20    # a table that can hold more than this takes streaming loads
+
+
+def columns(c, streaming):
+    """Table columns that take the split kernel (above 1024 entries), below or above the streaming line."""
+    row = 2 * len(c.lens_list) * c.H * c.d * (4 if c.mode == FP32 else 2) * c.P
+    n = STREAM_BYTES // row + 1 if streaming else max(c.table.shape[1], 1024 // c.P + 1)
+    assert (n * row > STREAM_BYTES) == streaming and n * c.P > 1024
+    return n
+
+
+def widened(c, streaming):
+    """c's table with absent pages behind."""
+    table = torch.full((c.table.shape[0], columns(c, streaming)), -1, dtype=torch.int32)
+    table[:, : c.table.shape[1]] = c.table.cpu()
+    return table
+
+
+@pytest.mark.parametrize("mode", [BF16, FP32])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("group,nq", [(4, 1), (3, 8), (4, 8)])
+@pytest.mark.parametrize("streaming", [False, True])
+def test_split_sequences(mode, d, group, nq, streaming):
+    """A sequence over many workgroups, one of a chunk, one of none; rotated, causal, with bias."""
+    log(f"split mode={mode} d={d} group={group} nq={nq} streaming={streaming}")
+    c = Paged(70, [2100, 0, 37, 700], 2, d, 32, mode)
+    n = 4 * nq
+    pos = torch.from_numpy(c.rng.uniform(0, 1e5, n))
+    check_attend(c, c.rows(n, 2 * group), causal=nq > 1, qpos=pos, theta=1e6, table=widened(c, streaming))
+
+
+@pytest.mark.parametrize("mode", [BF16, FP32])
+@pytest.mark.parametrize("streaming", [False, True])
+def test_split_kernels_past_four_gib(mode, streaming):
+    """Pages whose byte and element offsets pass 32 bits, read by the split kernels."""
+    from paper_2606_07878_amd import binding
+    H, P, d = 8, 16, 128
+    pages = (1 << 32) // (H * P * d * 2) + 40          # more than 2^31 elements, 2^32 bytes
+    c = Paged(71, [600, 90], H, d, P, mode)
+    small = c.n_pages
+    k = torch.zeros(pages, H, P, d, dtype=c.k.dtype, device="cuda")
+    v = torch.zeros_like(k)
+    beta = torch.zeros(pages, H, P, device="cuda")
+    k[pages - small:], v[pages - small:], beta[pages - small:] = c.k.cuda(), c.v.cuda(), c.beta.cuda()
+    table = widened(c, streaming)
+    q = c.rows(2, 32)
+    want = check_attend(c, q, table=table)
+    far = torch.where(table >= 0, table + (pages - small), table)
+    got = binding.paged_attend(q.cuda(), k, v, far.cuda(), c.lens.cuda(), beta_pages=beta)
+    assert torch.equal(got, want)
+
+
+def test_split_steps_in_a_graph_share_a_workspace_with_other_calls():
+    """A split call, captured once: its grid stays while sequences go from
+    split to whole to empty and back; the workspace starts as 0xFF bytes, and
+    between the replays other shapes use it, among them one whose joins are
+    planned per workgroup (more sequences than workgroups of a head)."""
+    from paper_2606_07878_amd import binding
+    c = Paged(72, [5000, 300, 0, 40], 2, 128, 16, BF16, width=400)
+    q = c.rows(4, 8)
+    many = Paged(73, [int(x) for x in torch.randint(0, 90, (600,), generator=c.g)], 1, 64, 16, BF16, width=6)
+    many.table = torch.cat([many.table, torch.full((600, 60), -1, dtype=torch.int32)], 1)
+    many.lens[300] = 66 * 16
+    many.table[300] = torch.arange(66, dtype=torch.int32)
+    mq = many.rows(600, 8)
+    few = Paged(74, [1500, 20], 3, 256, 32, FP32)
+    fq = few.rows(2 * 4, 12)
+    others = [(x, y, z, check_attend(x, y, causal=z)) for x, y, z in ((many, mq, False), (few, fq, True))]
+    c.cuda(), many.cuda(), few.cuda()
+    q, mq, fq = q.cuda(), mq.cuda(), fq.cuda()
+    ws = torch.full((binding.STILL_PAGED_WORKSPACE_BYTES,), 255, dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(q)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(g, stream=side):
+            binding.paged_attend(q, *c.pages(), beta_pages=c.beta, workspace=ws, out=out)
+    torch.cuda.current_stream().wait_stream(side)
+    for lens in ([5000, 300, 0, 40], [10, 6000, 300, 0], [0, 0, 0, 0], [6400, 6400, 1, 2000], [30, 30, 30, 30],
+                 [5000, 300, 0, 40]):
+        c.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        for other, oq, causal, want in others:
+            got = binding.paged_attend(oq.cuda(), *other.pages(), causal=causal, beta_pages=other.beta, workspace=ws)
+            torch.cuda.synchronize()
+            assert torch.equal(got, want)
+            out.fill_(float("nan"))
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, check_attend(c, q)), lens
