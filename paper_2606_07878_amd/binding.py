@@ -635,9 +635,13 @@ def paged_append(k, v, k_pages, v_pages, table, lens, offsets=None, positions=No
             _refuse(-2, "beta is no float32 tensor [n_tokens, H] on the pages' device")
         ts, hs = beta.stride()
         b = beta.data_ptr()
-    ks, vs = k.stride(), v.stride()
-    tokens = still_paged_tokens(n, k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1], b, ts, hs, off, pos,
-                                rope_theta)
+    kt, kh, _ = k.stride()
+    vt, vh, _ = v.stride()
+    if n == 1:                       # strides of dimensions of one address nothing and may be any number
+        kt = vt = 0
+    if shape[1] == 1:
+        kh = vh = 0
+    tokens = still_paged_tokens(n, k.data_ptr(), v.data_ptr(), kt, kh, vt, vh, b, ts, hs, off, pos, rope_theta)
     _on(torch, dev, (_lib or lib()).still_paged_append, ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(tokens))
 
 
@@ -689,7 +693,7 @@ def paged_attend(q, k_pages, v_pages, table, lens, causal: bool = False, scale: 
         _refuse(-2, f"q {tuple(shape)} does not fit {n} sequences and pages {tuple(k_pages.shape)}")
     _want_rows(q, "q", k_pages, shape)
     qs = q.stride()
-    if qs[1] != d or (qs[0] == 0 and tokens > 1):   # (a stride of 0 means dense tokens to the C call)
+    if (qs[1] != d and Hq > 1) or (qs[0] == 0 and tokens > 1):   # (a stride of 0 means dense tokens to the C call)
         _refuse(-1, "q's tokens are not contiguous, or the same one")
     pos = None
     if q_positions is not None:

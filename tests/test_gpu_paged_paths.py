@@ -104,3 +104,26 @@ def test_split_steps_in_a_graph_share_a_workspace_with_other_calls():
             g.replay()
             torch.cuda.synchronize()
             assert torch.equal(out, check_attend(c, q)), lens
+
+
+# ---- calls that the documentation allows -----------------------------------------
+
+def test_strides_of_dimensions_of_one_mean_nothing():
+    """One query head (a transposed [1, T, d]), one KV head, one token: their strides address nothing."""
+    from paper_2606_07878_amd import binding
+    c = Paged(75, [20, 33, 5], 1, 64, 16, BF16)
+    heads_first = torch.randn(1, 3, 64, generator=c.g).bfloat16()
+    q = heads_first.cuda().transpose(0, 1)
+    assert q.shape == (3, 1, 64) and q.stride(1) != 64
+    assert torch.equal(check_attend(c, q), check_attend(c, q.contiguous()))
+    rows = torch.randn(3 * 64 + 8, generator=c.g).bfloat16().cuda()
+    odd = rows.as_strided((3, 1, 64), (64, 5, 1))                       # the one head's stride
+    one = rows.as_strided((1, 1, 64), (7, 3, 1))                        # the one token's, too
+    c.cuda()
+    for k, table, lens in ((odd, c.table, c.lens), (one, c.table[:1], c.lens[:1])):
+        pages = [[x.clone() for x in (c.k, c.v)] for _ in range(2)]
+        binding.paged_append(k, k, *pages[0], table, lens)
+        dense = k.reshape(-1).clone().view(k.shape)
+        binding.paged_append(dense, dense, *pages[1], table, lens)
+        assert torch.equal(pages[0][0], pages[1][0]) and torch.equal(pages[0][1], pages[1][1])
+        assert not torch.equal(pages[0][0], c.k)
