@@ -756,8 +756,8 @@ def compact_paged(cfg: configs.CompactorConfig, weights: List[Dict[str, object]]
         if w_beta is not None and beta_pages[i] is None:
             _refuse(-1, f"layer {i}: w_beta given to a cache without beta")
     _want(positions, "positions", torch.float64, (n,), k_pages[0].get_device())
-    for i in range(L):
-        _paged(torch, k_pages[i], v_pages[i], None if beta_pages is None else beta_pages[i], table, lens)
+    for i in range(L):   # (no entry read: the C call's checks, pointers among them)
+        paged_gather(k_pages[i], v_pages[i], table, lens, seq, 0, beta_pages=None if beta_pages is None else beta_pages[i])
     with torch.cuda.device(k_pages[0].device):
         return _compact_paged(cfg, weights, k_pages, v_pages, table, lens, seq, n, positions, rope_theta, t, start, end,
                               w_beta, beta_pages, beta_max, mass_alpha, log_x, rerotate)

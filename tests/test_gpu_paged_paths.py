@@ -127,3 +127,29 @@ def test_strides_of_dimensions_of_one_mean_nothing():
         binding.paged_append(dense, dense, *pages[1], table, lens)
         assert torch.equal(pages[0][0], pages[1][0]) and torch.equal(pages[0][1], pages[1][1])
         assert not torch.equal(pages[0][0], c.k)
+
+
+# ---- compact_paged ---------------------------------------------------------------
+
+def two_layers(t=32, n=100):
+    from paper_2606_07878_amd import synth
+    from tests.helpers import weights_to_device
+    w = configs.shrink(configs.get_workload(1), n_tokens=n, t=t)
+    c = Paged(76, [n, 50], w.cfg.n_kv_heads, w.cfg.head_dim, 16, BF16).cuda()
+    W = weights_to_device(synth.make_weights(w, 0, t=t), BF16)
+    pages = [[x.clone() for x in (c.k, c.v, c.beta)] for _ in range(2)]
+    return w, c, [W, W], pages, torch.arange(n, dtype=torch.float64, device="cuda")
+
+
+def test_compact_paged_changes_nothing_where_a_layers_bias_pages_are_not_aligned():
+    from paper_2606_07878_amd import binding
+    w, c, W, pages, pos = two_layers()
+    odd = torch.empty(c.beta.numel() + 4, device="cuda")[1: 1 + c.beta.numel()].view(c.beta.shape)
+    odd.copy_(c.beta)
+    assert odd.is_contiguous() and odd.data_ptr() % 16 == 4
+    with pytest.raises(binding.StillError) as e:
+        binding.compact_paged(w.cfg, W, [p[0] for p in pages], [p[1] for p in pages], c.table, c.lens, 0, 100, pos,
+                              w.rope_theta, 32, beta_pages=[pages[0][2], odd])
+    assert e.value.status == -1
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for p in pages for x, y in zip(p, (c.k, c.v, c.beta))) and c.lens.tolist() == [100, 50]
