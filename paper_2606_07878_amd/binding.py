@@ -774,7 +774,8 @@ def _compact_paged(cfg, weights, k_pages, v_pages, table, lens, seq, n, position
     inside = positions[start:end].contiguous()
     ws = torch.empty(max(still_workspace_size(make_config(cfg, mode), end - start, t, 1), 1), dtype=torch.uint8,
                      device=dev)                                     # shared by the layers (one stream)
-    # every layer is compacted before the first one's pages change: a refusal leaves them as they were
+    # every layer is compacted, and what the second loop needs allocated, before the first one's
+    # pages change: a refusal, or memory that runs out, leaves them as they were
     new = []
     for i in range(L):
         K, V = paged_gather(k_pages[i], v_pages[i], table, lens, seq, end - start, start)
@@ -787,11 +788,16 @@ def _compact_paged(cfg, weights, k_pages, v_pages, table, lens, seq, n, position
                                                            [w_beta[i]], beta_max, mass_alpha, log_x, rerotate, mode, ws)
             beta = beta.t()
         new.append((Ck.transpose(0, 1), Cv.transpose(0, 1), beta))
+    now_at = torch.cat([positions[:start], pq, positions[end:]])
+    rest = [torch.empty(cfg.n_kv_heads, n - end, cfg.head_dim, dtype=k_pages[0].dtype, device=dev) for _ in range(2)]
+    if beta_pages is not None:
+        rest.append(torch.empty(cfg.n_kv_heads, n - end, dtype=torch.float32, device=dev))
     for i, (Ck, Cv, beta) in enumerate(new):
         bp = None if beta_pages is None else beta_pages[i]
-        rest = paged_gather(k_pages[i], v_pages[i], table, lens, seq, n - end, end, beta_pages=bp)
+        paged_gather(k_pages[i], v_pages[i], table, lens, seq, n - end, end, beta_pages=bp,
+                     out=rest[:2] if bp is None else rest)
         paged_append(Ck, Cv, k_pages[i], v_pages[i], row, to[0], beta=beta, beta_pages=bp)
         paged_append(rest[0].transpose(0, 1), rest[1].transpose(0, 1), k_pages[i], v_pages[i], row, to[1],
                      beta=None if bp is None else rest[2].t(), beta_pages=bp)
     lens[seq:seq + 1].fill_(length)
-    return torch.cat([positions[:start], pq, positions[end:]])
+    return now_at

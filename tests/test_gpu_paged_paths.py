@@ -153,3 +153,20 @@ def test_compact_paged_changes_nothing_where_a_layers_bias_pages_are_not_aligned
     assert e.value.status == -1
     torch.cuda.synchronize()
     assert all(torch.equal(x, y) for p in pages for x, y in zip(p, (c.k, c.v, c.beta))) and c.lens.tolist() == [100, 50]
+
+
+def test_compact_paged_allocates_nothing_once_pages_change(monkeypatch):
+    """What could run out of memory comes before the first page changes."""
+    from paper_2606_07878_amd import binding
+    w, c, W, pages, pos = two_layers()
+    count = lambda: torch.cuda.memory_stats()["allocation.all.allocated"]  # noqa: E731
+    seen, append = [], binding.paged_append
+
+    def counted(*args, **kw):
+        seen.append(count())
+        append(*args, **kw)
+
+    monkeypatch.setattr(binding, "paged_append", counted)
+    binding.compact_paged(w.cfg, W, [p[0] for p in pages], [p[1] for p in pages], c.table, c.lens, 0, 100, pos,
+                          w.rope_theta, 32, start=10, end=60, beta_pages=[p[2] for p in pages])
+    assert len(seen) == 4 and seen[0] == count()
