@@ -720,7 +720,8 @@ def paged_attend(q, k_pages, v_pages, table, lens, causal: bool = False, scale: 
 def compact_paged(cfg: configs.CompactorConfig, weights: List[Dict[str, object]], k_pages: List, v_pages: List,
                   table, lens, seq: int, n: int, positions, rope_theta: float, t: int, start: int = 0,
                   end: Optional[int] = None, w_beta: Optional[List] = None, beta_pages: Optional[List] = None,
-                  beta_max: float = 0.0, mass_alpha: float = 0.0, log_x: float = 0.0, rerotate: bool = True):
+                  beta_max: float = 0.0, mass_alpha: float = 0.0, log_x: float = 0.0, rerotate: bool = True,
+                  drop_bias: bool = True):
     """Compact entries [start, end) (default: all) of sequence ``seq``, which
     holds n entries, to t inside its pages, layer by layer (lists of L layers'
     weights and pages, one table): they are read out, compacted
@@ -732,7 +733,11 @@ def compact_paged(cfg: configs.CompactorConfig, weights: List[Dict[str, object]]
     [n - (end - start) + t]; pages behind the new length are free.  A page that
     another sequence's table names too changes for that one as well.
     A cache that keeps bias passes ``beta_pages``; new entries without
-    ``w_beta`` get bias 0."""
+    ``w_beta`` get bias 0.  The compactor reads keys and values only: bias that
+    entries [start, end) carry (those of an earlier compaction) is not taken in
+    and is lost, each counting as one entry without bias.  To keep it, start
+    behind them; ``drop_bias=False`` waits for the GPU and refuses a range that
+    carries any, before anything changes."""
     torch = _torch()
     end = n if end is None else end
     if not (0 <= start < end <= n):
@@ -760,11 +765,11 @@ def compact_paged(cfg: configs.CompactorConfig, weights: List[Dict[str, object]]
         paged_gather(k_pages[i], v_pages[i], table, lens, seq, 0, beta_pages=None if beta_pages is None else beta_pages[i])
     with torch.cuda.device(k_pages[0].device):
         return _compact_paged(cfg, weights, k_pages, v_pages, table, lens, seq, n, positions, rope_theta, t, start, end,
-                              w_beta, beta_pages, beta_max, mass_alpha, log_x, rerotate)
+                              w_beta, beta_pages, beta_max, mass_alpha, log_x, rerotate, drop_bias)
 
 
 def _compact_paged(cfg, weights, k_pages, v_pages, table, lens, seq, n, positions, rope_theta, t, start, end, w_beta,
-                   beta_pages, beta_max, mass_alpha, log_x, rerotate):
+                   beta_pages, beta_max, mass_alpha, log_x, rerotate, drop_bias):
     """compact_paged behind its checks, with the pages' GPU current."""
     torch = _torch()
     L, length = len(k_pages), n - (end - start) + t
@@ -778,7 +783,10 @@ def _compact_paged(cfg, weights, k_pages, v_pages, table, lens, seq, n, position
     # pages change: a refusal, or memory that runs out, leaves them as they were
     new = []
     for i in range(L):
-        K, V = paged_gather(k_pages[i], v_pages[i], table, lens, seq, end - start, start)
+        K, V, *carried = paged_gather(k_pages[i], v_pages[i], table, lens, seq, end - start, start,
+                                      beta_pages=None if drop_bias or beta_pages is None else beta_pages[i])
+        if carried and bool((carried[0] != 0).any()):
+            _refuse(-5, f"layer {i}: entries [{start}, {end}) carry bias, which a compaction does not take in")
         if w_beta is None:
             Ck, Cv, pq = compact_layer(cfg, weights[i], K, V, inside, rope_theta, t, rerotate=rerotate, mode=mode,
                                        workspace=ws)

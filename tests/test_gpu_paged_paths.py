@@ -170,3 +170,50 @@ def test_compact_paged_allocates_nothing_once_pages_change(monkeypatch):
     binding.compact_paged(w.cfg, W, [p[0] for p in pages], [p[1] for p in pages], c.table, c.lens, 0, 100, pos,
                           w.rope_theta, 32, start=10, end=60, beta_pages=[p[2] for p in pages])
     assert len(seen) == 4 and seen[0] == count()
+
+
+@pytest.mark.parametrize("with_head", [False, True])
+def test_compact_paged_of_entries_that_carry_bias(with_head):
+    """A sequence whose first 20 entries (an earlier compaction's) carry bias.
+    Behind them a compaction leaves them alone; over them it gives what it gives
+    without their bias, or, asked not to drop it, nothing changes."""
+    from paper_2606_07878_amd import binding, synth
+    from tests.helpers import dev_tensor
+    w, c, W, pages, pos = two_layers()
+    kw = {}
+    if with_head:
+        head = dev_tensor(synth.make_beta_weight(w, 0), BF16)
+        kw = dict(w_beta=[head, head], beta_max=2.0, mass_alpha=0.5)
+
+    def compact(pages, lens, **more):
+        return binding.compact_paged(w.cfg, W, [p[0] for p in pages], [p[1] for p in pages], c.table, lens, 0, 100, pos,
+                                     w.rope_theta, 32, beta_pages=[p[2] for p in pages], **kw, **more)
+
+    for p in pages:   # bias on entries 0 .. 19 alone
+        keep = [binding.paged_gather(*p[:2], c.table, c.lens, 0, 20, beta_pages=p[2])[2]]
+        p[2].zero_()
+        k, v, _ = binding.paged_gather(*p[:2], c.table, c.lens, 0, 20, beta_pages=p[2])
+        binding.paged_append(k.transpose(0, 1), v.transpose(0, 1), *p[:2], c.table[:1],
+                             torch.tensor([20], dtype=torch.int32, device="cuda"), beta=keep[0].t(), beta_pages=p[2])
+    before = [[x.clone() for x in p] for p in pages]
+    with pytest.raises(binding.StillError) as e:
+        compact(pages, c.lens, drop_bias=False)
+    assert e.value.status == -5 and "layer 0" in str(e.value)
+    with pytest.raises(binding.StillError) as e:
+        compact(pages, c.lens, start=19, drop_bias=False)
+    assert e.value.status == -5
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for p, b in zip(pages, before) for x, y in zip(p, b)) and c.lens.tolist() == [100, 50]
+
+    bare = [[p[0].clone(), p[1].clone(), torch.zeros_like(p[2])] for p in pages]
+    over = [[x.clone() for x in p] for p in pages]
+    lens = [c.lens.clone() for _ in range(3)]
+    assert torch.equal(compact(bare, lens[0], drop_bias=False), compact(over, lens[1]))
+    for x, y in zip(bare, over):
+        got, want = (binding.paged_gather(*p[:2], c.table, lens[0], 0, 32, beta_pages=p[2]) for p in (x, y))
+        assert all(torch.equal(g, r) for g, r in zip(got, want))
+    compact(pages, lens[2], start=20, drop_bias=False)
+    assert lens[2].tolist() == [52, 50]
+    for p, b in zip(pages, before):
+        got, want = (binding.paged_gather(*x[:2], c.table, c.lens, 0, 20, beta_pages=x[2]) for x in (p, b))
+        assert all(torch.equal(g, r) for g, r in zip(got, want)) and got[2].any()
