@@ -562,6 +562,8 @@ def _refuse_paged(torch, k_pages, v_pages, beta_pages, table, lens) -> None:
         _refuse(-2, "table is no int32 tensor [n_seqs, pages] with contiguous rows")
     if table.shape[0] > 1 and table.stride(0) >= 1 << 31:
         _refuse(-2, f"table rows {table.stride(0)} entries apart")
+    if max(table.shape) >= 1 << 31:
+        _refuse(-2, f"a table of {table.shape[0]} x {table.shape[1]} entries")
     if table.get_device() != dev:
         _refuse(-1, f"table is on {table.device}, the pages on {k_pages.device}")
     _want(lens, "lens", torch.int32, table.shape[:1], dev)
@@ -578,6 +580,7 @@ def _paged(torch, k_pages, v_pages, beta_pages, table, lens):
             and v_pages.get_device() == dev and table.dtype is i32 and len(size) == 2 and lens.dtype is i32
             and lens.shape == size[:1] and lens.is_contiguous() and lens.get_device() == dev
             and table.get_device() == dev and (table.stride(1) == 1 or size[1] <= 1) and (size[0] <= 1 or table.stride(0) < 1 << 31)
+            and size[0] < 1 << 31 and size[1] < 1 << 31
             and (beta_pages is None or beta_pages.dtype is torch.float32 and beta_pages.shape == shape[:3]
                  and beta_pages.is_contiguous() and beta_pages.get_device() == dev)):
         _refuse_paged(torch, k_pages, v_pages, beta_pages, table, lens)

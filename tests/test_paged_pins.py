@@ -267,3 +267,14 @@ def test_binding_refuses_table_rows_too_far_apart():
     c = Paged(7, [20, 30], 2, 64, 16, configs.MODE_BF16)
     far = torch.empty_strided((2, 2), (1 << 31, 1), dtype=torch.int32, device="meta")
     _refused(-2, binding.paged_attend, c.rows(2, 4), c.k, c.v, far, c.lens)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="CPU refusals only")
+@pytest.mark.parametrize("shape", [((1 << 32) + 2, 2), (1, (1 << 32) + 2)])
+def test_binding_refuses_table_sizes_past_32_bits(shape):
+    """Their low 32 bits say 2."""
+    c = Paged(8, [20, 30], 2, 64, 16, configs.MODE_BF16)
+    table = torch.empty(shape, dtype=torch.int32, device="meta")
+    lens = torch.empty(shape[:1], dtype=torch.int32, device="meta")
+    _refused(-2, binding.paged_attend, c.rows(2, 4), c.k, c.v, table, lens)
+    _refused(-2, binding.paged_gather, c.k, c.v, table, lens, 0, 5)
