@@ -751,6 +751,8 @@ def compact_paged(cfg: configs.CompactorConfig, weights: List[Dict[str, object]]
     if w_beta is not None and beta_pages is None:
         _refuse(-1, "w_beta given to a cache without beta")
     length = n - (end - start) + t
+    if table.dim() != 2:
+        _refuse(-2, f"table has {table.dim()} dimensions, not [n_seqs, pages]")
     if not 0 <= seq < table.shape[0]:
         _refuse(-2, f"sequence {seq} outside [0, {table.shape[0]})")
     for i in range(L):

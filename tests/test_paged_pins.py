@@ -278,3 +278,12 @@ def test_binding_refuses_table_sizes_past_32_bits(shape):
     lens = torch.empty(shape[:1], dtype=torch.int32, device="meta")
     _refused(-2, binding.paged_attend, c.rows(2, 4), c.k, c.v, table, lens)
     _refused(-2, binding.paged_gather, c.k, c.v, table, lens, 0, 5)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="CPU refusals only")
+def test_compact_paged_refuses_a_table_of_other_dimensions():
+    c = Paged(9, [20, 30], 2, 64, 16, configs.MODE_BF16)
+    w = configs.get_workload(1)
+    pos = torch.arange(30, dtype=torch.float64)
+    for table in (c.table[0], c.table[None], torch.tensor(3, dtype=torch.int32)):
+        _refused(-2, binding.compact_paged, w.cfg, [{}], [c.k], [c.v], table, c.lens, 0, 20, pos, 1e6, 8)
