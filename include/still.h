@@ -396,7 +396,7 @@ typedef struct {
 /* Bytes of device workspace that serve still_paged_attend at this group,
  * n_queries, head count and head_dim, whatever the sequences and their lengths
  * (0: invalid configuration).  Never above STILL_PAGED_WORKSPACE_BYTES. */
-enum { STILL_PAGED_WORKSPACE_BYTES = 72 << 20 };
+enum { STILL_PAGED_WORKSPACE_BYTES = 17 << 20 };
 size_t still_paged_attend_workspace_size(const still_paged_cache *cache, const still_paged_attend_config *cfg);
 
 /*   q            [n_seqs * n_queries] tokens, sequence by sequence, of [H*group][d]

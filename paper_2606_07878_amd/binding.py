@@ -280,7 +280,7 @@ def still_paged_attend(cache: still_paged_cache, seqs: still_paged_seqs, cfg: st
                                     _ptr(q_positions), _ptr(out), _ptr(workspace), workspace_bytes, _ptr(stream))
 
 
-STILL_PAGED_WORKSPACE_BYTES = 72 << 20
+STILL_PAGED_WORKSPACE_BYTES = 17 << 20
 
 
 def still_status_string(status: int) -> str:

@@ -269,6 +269,13 @@ def test_binding_refuses_table_rows_too_far_apart():
     _refused(-2, binding.paged_attend, c.rows(2, 4), c.k, c.v, far, c.lens)
 
 
+def test_workspace_bound_is_near_what_the_largest_call_needs():
+    """A loop holds one such buffer per stream: no more than a sixteenth of it is spare."""
+    most = max(binding.still_paged_attend_workspace_size(_cache(n_kv_heads=H, head_dim=d), _acfg(group=group))
+               for H in (*range(1, 520), 65535) for d in (64, 128, 256) for group in (1, 16, 17, 32))
+    assert 15 / 16 * binding.STILL_PAGED_WORKSPACE_BYTES < most <= binding.STILL_PAGED_WORKSPACE_BYTES
+
+
 @pytest.mark.skipif(torch.cuda.is_available(), reason="CPU refusals only")
 @pytest.mark.parametrize("shape", [((1 << 32) + 2, 2), (1, (1 << 32) + 2)])
 def test_binding_refuses_table_sizes_past_32_bits(shape):
