@@ -377,11 +377,12 @@ still_status still_paged_gather(const still_paged_cache *cache, const still_page
  *   out = sum_j exp(s_j) v_j / sum_j exp(s_j),   s_j = scale q . k_j + beta_j
  * over the entries j < lens[s] of present pages (cache->beta NULL: beta = 0).
  * With causal = 1, query i sits at entry lens[s] - n_queries + i and sees
- * entries up to that one.  A query that sees nothing gets zeros (a padded batch
- * row has length 0).  A NaN or an infinity in an entry that some query of the
- * call sees makes that query's output non-finite (an infinity may come out as
- * NaN) and may reach the other queries of its sequence and KV head; one that no
- * query sees reaches none.  The result does not depend on the order in which
+ * entries up to that one.  A logit of minus infinity (by its bias or by its key)
+ * leaves an entry of finite value out.  A query with no entry left gets zeros (a
+ * padded batch row has length 0).  Any other NaN or infinity in an entry that some
+ * query of the call sees makes that query's output non-finite (an infinity may
+ * come out as NaN) and may reach the other queries of its sequence and KV head;
+ * one that no query sees reaches none.  The result does not depend on the order in which
  * the device runs: the same inputs give the same bits. */
 typedef struct {
   int32_t group;        /* query heads per KV head, >= 1                                    */

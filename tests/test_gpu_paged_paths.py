@@ -217,3 +217,35 @@ def test_compact_paged_of_entries_that_carry_bias(with_head):
     for p, b in zip(pages, before):
         got, want = (binding.paged_gather(*x[:2], c.table, c.lens, 0, 20, beta_pages=x[2]) for x in (p, b))
         assert all(torch.equal(g, r) for g, r in zip(got, want)) and got[2].any()
+
+
+@pytest.mark.parametrize("mode", [BF16, FP32])
+@pytest.mark.parametrize("streaming", [None, False])
+def test_a_logit_of_minus_infinity_leaves_its_entry_out(mode, streaming):
+    """An infinite key whose product is minus infinity is the same as a bias of
+    minus infinity, bit for bit; a query whose product is plus infinity, and an
+    infinite value, come out non-finite."""
+    from paper_2606_07878_amd import binding
+    c = Paged(77, [40, 90], 2, 64, 16, mode)
+    q = c.rows(2, 4)
+    q[:, :, 0] = -q[:, :, 0].abs() - 0.5
+    q[1, 1, 0] = 0.5
+    table = c.table if streaming is None else widened(c, streaming)
+    page, at = int(c.table[1, 2]), 5
+
+    def run(k, v, b):
+        return binding.paged_attend(q.cuda(), k.cuda(), v.cuda(), table.cuda(), c.lens.cuda(), beta_pages=b.cuda())
+
+    k, v, b = c.k.clone(), c.v.clone(), c.beta.clone()
+    b[page, 0, at] = float("-inf")
+    want = run(k, v, b)
+    k[page, 0, at, 0] = float("inf")
+    got = run(k, v, c.beta)
+    same = torch.ones(2, 4, dtype=torch.bool)
+    same[1, :2] = False                    # the query, and the other one of its sequence and KV head
+    assert torch.isfinite(want).all() and not torch.isfinite(got[1, 1]).any()
+    assert torch.equal(got[same.cuda()], want[same.cuda()])
+    q[1, 1, 0] = -0.5
+    assert torch.equal(run(k, v, c.beta), run(c.k, v, b))
+    v[page, 0, at, 3] = float("inf")
+    assert not torch.isfinite(run(c.k, v, b)[1, :2, 3]).any()
