@@ -311,8 +311,9 @@ still_status still_attend_scratch(const still_attend_config *cfg, const void *q,
  *
  * One layer's pages hold `page_size` entries of every KV head each.  A
  * sequence's entry j lives in slot j % page_size of page
- * table[s * table_stride + j / page_size].  lens[s] is its number of entries;
- * a length below 0 counts as 0, one above max_pages * page_size as that.  A
+ * table[s * table_stride + j / page_size].  lens[s] is its number of entries; to
+ * a call that reads, one below 0 counts as 0 and one above max_pages * page_size as
+ * that (an append takes it as it is and skips what it puts outside).  A
  * table entry outside [0, n_pages) is an absent page: nothing is written to
  * it, its entries read as zeros and no query sees them.  Both arrays are read
  * on the device, so calls can be captured into a graph while they change.
