@@ -61,6 +61,14 @@ static still_status check_theta(double theta, const double* positions) {
   return STILL_OK;
 }
 
+// Blocks of 256 threads along a grid's first dimension, and the rest of them along another:
+// a dimension of 2^32 threads and more is cut to 32 bits without an error.
+constexpr unsigned PAGED_GRID_X = 1u << 23;
+struct PagedGrid {
+  unsigned x, more;
+  explicit PagedGrid(unsigned blocks) : x(std::min(blocks, PAGED_GRID_X)), more((blocks + PAGED_GRID_X - 1) / PAGED_GRID_X) {}
+};
+
 // f(IT(), head_dim constant) for the cache's element type and head width
 template <class F>
 static void paged_dispatch(const still_paged_cache* c, F f) {
@@ -182,8 +190,8 @@ still_status still_paged_append(const still_paged_cache* cache, const still_page
   TIMED(STILL_K_OTHER);
   paged_dispatch(cache, [&](auto it, auto d) {
     using IT = decltype(it);
-    const unsigned blocks = ((unsigned)t->n_tokens + PAGED_APPEND_TPB - 1) / PAGED_APPEND_TPB;
-    hipLaunchKernelGGL((paged_append_kernel<IT, decltype(d)::value>), dim3(blocks), dim3(256), 0, st, a);
+    const PagedGrid g(((unsigned)t->n_tokens + PAGED_APPEND_TPB - 1) / PAGED_APPEND_TPB);
+    hipLaunchKernelGGL((paged_append_kernel<IT, decltype(d)::value>), dim3(g.x, g.more), dim3(256), 0, st, a);
   });
   HIP_TRY(hipGetLastError());
   return STILL_OK;
@@ -215,8 +223,8 @@ still_status still_paged_gather(const still_paged_cache* cache, const still_page
   TIMED(STILL_K_OTHER);
   paged_dispatch(cache, [&](auto it, auto d) {
     using IT = decltype(it);
-    const unsigned blocks = ((unsigned)n + PAGED_GATHER_ROWS - 1) / PAGED_GATHER_ROWS;
-    hipLaunchKernelGGL((paged_gather_kernel<IT, decltype(d)::value>), dim3(blocks, a.c.H), dim3(256), 0, st, a);
+    const PagedGrid g(((unsigned)n + PAGED_GATHER_ROWS - 1) / PAGED_GATHER_ROWS);
+    hipLaunchKernelGGL((paged_gather_kernel<IT, decltype(d)::value>), dim3(g.x, a.c.H, g.more), dim3(256), 0, st, a);
   });
   HIP_TRY(hipGetLastError());
   return STILL_OK;

@@ -93,7 +93,8 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
   __shared__ float2 cs[TPB][HD];
   __shared__ int page[TPB], slot[TPB];
   const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
-  const long t0 = (long)blockIdx.x * TPB;
+  const long t0 = ((long)blockIdx.y * gridDim.x + blockIdx.x) * TPB;
+  if (t0 >= a.n_tokens) return;
   const int left = (int)min((long)TPB, a.n_tokens - t0);   // tokens of this block
   // the first step of the search, and a position per thread's first angle, ahead of the rows
   const int n_seqs = a.c.n_seqs, x0 = (lane + 1) * ((n_seqs + 63) / 64);
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Gather: block (x, h) copies PAGED_GATHER_ROWS entries of head h, a thread
+// Gather: block (x, h, z) copies PAGED_GATHER_ROWS entries of head h, a thread
 // 16-byte pieces of keys and values.  Bound by the copy: 65536 entries of 8 heads of
 // width 256 (1.07 GB) 201 us, 5.3 TB/s, with streaming stores, 206 with ordinary ones.
 // ---------------------------------------------------------------------------
@@ -203,7 +204,7 @@ template <class IT, int D>
 __global__ __launch_bounds__(256) void paged_gather_kernel(PagedGatherArgs a) {
   constexpr int PPR = D * (int)sizeof(IT) / 16;
   const int tid = threadIdx.x, h = blockIdx.y, len = paged_len(a.c, a.seq);
-  const long i0 = (long)blockIdx.x * PAGED_GATHER_ROWS;
+  const long i0 = ((long)blockIdx.z * gridDim.x + blockIdx.x) * PAGED_GATHER_ROWS;
   for (int it = tid; it < PAGED_GATHER_ROWS * PPR; it += 256) {
     const long i = i0 + it / PPR, j = a.start + i;
     const int p = it % PPR;

@@ -249,3 +249,43 @@ def test_a_logit_of_minus_infinity_leaves_its_entry_out(mode, streaming):
     assert torch.equal(run(k, v, c.beta), run(c.k, v, b))
     v[page, 0, at, 3] = float("inf")
     assert not torch.isfinite(run(c.k, v, b)[1, :2, 3]).any()
+
+
+def test_append_of_more_tokens_than_a_grid_has_threads_for():
+    """2^26 tokens and some: 64 threads each pass 2^32, which one dimension of a grid cannot hold."""
+    from paper_2606_07878_amd import binding
+    n, P = (1 << 26) + 5000, 4096
+    pages = -(-n // P)
+    log(f"{n} tokens, {pages} pages, {3 * pages * P * 128 / 2**30:.1f} GiB")
+    k = torch.empty(n, 1, 64, dtype=torch.bfloat16, device="cuda")
+    k.view(torch.int16).copy_(torch.arange(n, device="cuda", dtype=torch.int32).to(torch.int16)[:, None, None])
+    pool = [torch.zeros(pages, 1, P, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    table = torch.arange(pages, dtype=torch.int32, device="cuda")[None]
+    binding.paged_append(k, k, *pool, table, torch.tensor([n], dtype=torch.int32, device="cuda"))
+    for x in pool:
+        rows = x.view(torch.int16).view(pages * P, 64)
+        assert torch.equal(rows[:n], k.view(torch.int16)[:, 0]) and not rows[n:].any()
+    del k, pool, x, rows
+    torch.cuda.empty_cache()
+
+
+def test_gather_of_as_many_entries_as_a_table_holds():
+    """2^30 entries, 2^24 blocks of 256 threads: their number passes 32 bits too.  Keys and values, the
+    same, go into one buffer (128 GiB), the table repeats a few pages."""
+    from paper_2606_07878_amd import binding
+    P, pages, n = 4096, 5, 1 << 30
+    width = n // P
+    pool = torch.randint(-32768, 32767, (pages, 1, P, 64), dtype=torch.int16, device="cuda").view(torch.bfloat16)
+    table = (torch.arange(width, dtype=torch.int32, device="cuda") % pages)[None]
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    out = torch.empty(n, 64, dtype=torch.bfloat16, device="cuda")
+    chunks = out.view(torch.int16).view(width, P * 64)
+    chunks[-1] = 7
+    cache = binding.still_paged_cache(1, 64, P, pages, BF16, pool.data_ptr(), pool.data_ptr(), None)
+    seqs = binding.still_paged_seqs(1, width, width, table.data_ptr(), lens.data_ptr())
+    assert binding.still_paged_gather(cache, seqs, 0, 0, n, out, out, None, torch.cuda.current_stream().cuda_stream) == 0
+    rows = pool.view(torch.int16).view(pages, P * 64)
+    for i in (*range(0, width, 9973), width - 2, width - 1):
+        assert torch.equal(chunks[i], rows[i % pages]), i
+    del out, chunks
+    torch.cuda.empty_cache()
