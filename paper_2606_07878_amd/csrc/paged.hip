@@ -100,24 +100,27 @@ static still_status check_attend(const still_paged_cache* c, const still_paged_a
 // Who takes a sequence (and KV head).  Where its table is short one workgroup or
 // one wave takes all of it: one launch instead of two (9.3 us of host time instead
 // of 11.4), nothing joined, but one CU's rate of reading, or one wave's, for the
-// longest one.  The host knows the table's capacity only.  us in a graph, bf16 of
-// width 128, 8 heads unless said.
-// Team or parts (capacity 1024, the line), one sequence of 32 entries 4.5 / 7.9, 256
-// 5.9 / 10.0, 512 8.6 / 10.0, 719 10.2 / 10.0, 1024 12.9 / 10.0; width 64, 719 7.3 /
-// 9.4, 1024 8.9 / 9.4; width 256 (512, the line) 256 9.0 / 12.3, 512 13.2 / 12.4; fp32
-// of width 64 256 5.5 / 8.9, 1024 12.6 / 9.1; 32 rows 256 7.7 / 13.7, 1024 14.7 / 15.1.
+// longest one.  The host knows the table's capacity only, so a table as wide as the
+// longest context takes parts, and streaming loads, while its sequences are short.  us in
+// a graph, bf16 of width 128, 8 heads unless said.
+// Team or parts (capacity 1024, the line), one sequence of 32 entries 4.9 / 8.3, 256
+// 6.2 / 10.3, 512 8.9 / 10.3, 719 10.9 / 10.3, 1024 13.5 / 10.3; width 64, 719 7.6 /
+// 9.7, 1024 9.1 / 9.7; width 256 (512, the line) 256 9.2 / 12.5, 512 13.4 / 12.5; fp32
+// of width 64 256 6.2 / 9.6, 1024 13.5 / 9.6; 32 rows 256 8.0 / 14.1, 1024 15.9 / 15.4.
 // 64 sequences (the line) of 1000 41 / 48; 70 of 1 to 1024, spread over their
-// logarithm, 20.6 / 17.5.
-// Wave or team: 30 sequences (below the line) of 30 entries 4.1 / 4.9, 128 6.3 / 5.6, 512
-// 16.1 / 12.5; 40 (above) of 30 4.3 / 7.7, 128 6.5 / 9.0, 512 16.9 / 19.8; width 256, 40
-// of 128 11.7 / 12.7; 32 rows, 40 of 30 9.4 / 11.3, 256 17.7 / 16.9; fp32 of width 64, 40
-// of 30 4.1 / 4.8, 256 15.0 / 11.5.
-// Wave or parts: 256 sequences of 30 7.5 / 21.9, 256 41.8 / 47.4; 32 rows, 30 18.0 / 58;
-// 70 of 1 to 1024 27.8 / 17.5, which is why waves take capacities to 512 only.
+// logarithm, 19.2 / 19.3.  So on the card parts are the faster ones for a few sequences of
+// more than 700 entries; most tables of this width hold shorter ones, and outside a graph
+// the second launch takes up to 2 us of that back.
+// Wave or team: 30 sequences (below the line) of 30 entries 4.2 / 5.1, 128 6.5 / 5.8, 512
+// 16.9 / 12.8; 40 (above) of 30 4.4 / 7.9, 128 6.7 / 9.3, 512 17.2 / 20.0; width 256, 40
+// of 128 11.4 / 12.6; fp32 of width 64, 40 of 30 4.3 / 4.9, 256 15.7 / 11.5; 32 rows, 40 of
+// 30 9.3 / 7.4, 256 19.1 / 14.1, rotated 12.7 / 14.7 and 25.1 / 21.6.
+// Wave or parts: 256 sequences of 30 7.5 / 22.9, 256 41.8 / 54.8; 32 rows, 30 18.3 / 62;
+// 70 of 1 to 1024 29.8 / 19.3, which is why waves take capacities to 512 only.
 // Streaming loads where the call may read more than the memory-side cache holds (256
-// MB): us with ordinary / streaming loads, one sequence of 131136 101 / 91, 64 of up to
-// 16384 101 / 95, 5 of up to 20011 and 32 rows (410 MB) 46.5 / 45.0; below it the entries
-// may still be there from the step before: 4 sequences of up to 9000 (147 MB) 23.8 / 25.8.
+// MB): us with ordinary / streaming loads, one sequence of 131136 99 / 89, 64 of up to
+// 16384 108 / 98, 5 of up to 20011 and 32 rows (410 MB) 48.8 / 47.6; below it the entries
+// may still be there from the step before: 4 sequences of up to 9000 (147 MB) 23.6 / 25.8.
 enum PagedKernel { PAGED_PARTS, PAGED_STREAM, PAGED_TEAM, PAGED_WAVE };
 static PagedKernel paged_kernel(const still_paged_cache* c, const still_paged_seqs* q, int esize) {
   const long cap = (long)q->max_pages * c->page_size, pairs = (long)q->n_seqs * c->n_kv_heads;

@@ -266,8 +266,8 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(PagedGatherArgs a) {
 //
 // Bound by the entries' bytes: one sequence of 131136 entries of 8 heads of width 128
 // (537 MB) 83 us, 6.5 TB/s, joined in 4.6; 48 of 1024 to 9216 of width 256 (1.48 GB)
-// 225 us, 6.6 TB/s; with 32 rows 166 MB in 39 us, 4.2 TB/s: 370 registers leave one wave
-// per SIMD, whose first and last chunks nothing hides.
+// 230 us, 6.5 TB/s (a plain read reaches 7.1); with 32 rows 166 MB in 42 us, 3.9 TB/s:
+// 372 registers leave one wave per SIMD, whose first and last chunks nothing hides.
 // ---------------------------------------------------------------------------
 struct PagedAttendArgs {
   PagedArgs c;
@@ -289,9 +289,9 @@ struct PagedAttendArgs {
 
 constexpr int PAGED_ROUND = 256;         // sequences whose lengths a wave holds at a time, four per lane
 // Chunks that a sequence counts beside its own.  us at 0 / 2 / 4 / 6 / 8: 64 sequences
-// of 5 to 16384 entries 111.3 / 99.1 / 96.5 / 95.2 / 96.2, 300 of 20 to 900 72.5 / 64.8 /
-// 65.2 / 66.2 / 66.1, 48 of 1024 to 9216 of width 256 237 / 236 / 237 / 239 / 241, 5 of
-// 1500 to 20011 with 32 rows 47.7 / 46.0 / 45.1 / 45.0 / 44.9.
+// of 5 to 16384 entries 113.5 / 101.5 / 96.7 / 96.1 / 97.0, 300 of 20 to 900 73.0 / 65.3 /
+// 64.9 / 66.0 / 66.0, 48 of 1024 to 9216 of width 256 238 / 239 / 239 / 241 / 243, 5 of
+// 1500 to 20011 with 32 rows 50.8 / 49.0 / 47.7 / 47.5 / 47.6: flat from 4 on.
 constexpr int PAGED_PAD = 6;
 constexpr float PAGED_SLACK = 6.f;       // weights reach e^6 before they are scaled back
 constexpr float LOG2E = 1.4426950408889634f, LOG2E_REST = (float)(1.4426950408889634 - (double)LOG2E), LN2 = 0.6931471805599453f;
