@@ -409,6 +409,56 @@ still_status still_paged_attend(const still_paged_cache *cache, const still_page
                                 const still_paged_attend_config *cfg, const void *q, const double *q_positions,
                                 void *out, void *workspace, size_t workspace_bytes, void *stream);
 
+/* The same, and with `lse` (not NULL) the log of every row's sum of exponentials,
+ *   lse = log sum_j exp(s_j)   [n_seqs * n_queries][H*group] float32 (4-byte aligned),
+ * minus infinity where no entry is left: what still_paged_score takes. */
+still_status still_paged_attend_lse(const still_paged_cache *cache, const still_paged_seqs *seqs,
+                                    const still_paged_attend_config *cfg, const void *q, const double *q_positions,
+                                    void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * The same cache in 8 bits: half the memory, and half the time of an attention
+ * that is bound by reading it.
+ *
+ * Entries are OCP e4m3 codes (4 exponent bits, 3 fraction bits, largest 448, no
+ * infinity), and blocks of 16 entries (slots 16 b .. 16 b + 15 of a page) of a head
+ * share a float scale: an entry's key stands for its codes times k_scale of its
+ * block, its value for its codes times v_scale.  The append makes scales that are
+ * powers of two; the calls that read take any.  Sequences, tables, lengths and
+ * absent pages as above.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t n_kv_heads, head_dim, page_size, n_pages;   /* as still_paged_cache                 */
+  int32_t mode;               /* still_mode: element type of the rows given and given out     */
+  void *k, *v;                /* codes [n_pages][H][page_size][d] (device, 16-byte aligned)   */
+  float *k_scale, *v_scale;   /* [n_pages][H][page_size / 16] (device, 16-byte aligned)       */
+  float *beta;                /* as still_paged_cache                                         */
+} still_paged8_cache;
+
+/* still_paged_append into 8 bits.  Keys are rotated in 64 bits and rounded to 32; a
+ * block's scale is the smallest power of two (2^-100 at least) with which no finite
+ * number of it exceeds 448 scales, and numbers are rounded to the nearest code, ties to
+ * the even one.  Infinities and NaN are held as NaN and leave the scale alone.  A block
+ * that holds entries before the call's first one keeps its scale if that still serves;
+ * otherwise their codes are rescaled, which is exact but for what falls below
+ * the smallest code (rounded once more).  A block whose first slot the call writes starts
+ * anew, whatever its scale was.  The blocks that one call writes must be those of one
+ * sequence each.  Otherwise as still_paged_append. */
+still_status still_paged8_append(const still_paged8_cache *cache, const still_paged_seqs *seqs,
+                                 const still_paged_tokens *tokens, void *stream);
+
+/* still_paged_gather of what the entries stand for, rounded to the rows' type (exact
+ * where scales are powers of two and nothing leaves its range). */
+still_status still_paged8_gather(const still_paged8_cache *cache, const still_paged_seqs *seqs, int32_t seq,
+                                 int32_t start, int32_t n, void *K, void *V, float *beta, void *stream);
+
+/* still_paged_attend_lse over such a cache (`lse` may be NULL): queries and outputs
+ * are of the cache's mode, products and sums of 32 bits as there. */
+size_t still_paged8_attend_workspace_size(const still_paged8_cache *cache, const still_paged_attend_config *cfg);
+still_status still_paged8_attend(const still_paged8_cache *cache, const still_paged_seqs *seqs,
+                                 const still_paged_attend_config *cfg, const void *q, const double *q_positions,
+                                 void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Human-readable name of a status code (static string). */
 const char *still_status_string(int32_t status);
 

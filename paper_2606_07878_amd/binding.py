@@ -71,6 +71,13 @@ class still_paged_cache(ctypes.Structure):
                 ("v", ctypes.c_void_p), ("beta", ctypes.c_void_p)]
 
 
+class still_paged8_cache(ctypes.Structure):
+    _fields_ = [("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("mode", ctypes.c_int32), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("beta", ctypes.c_void_p)]
+
+
 class still_paged_seqs(ctypes.Structure):
     _fields_ = [("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("table_stride", ctypes.c_int32),
                 ("table", ctypes.c_void_p), ("lens", ctypes.c_void_p)]
@@ -148,6 +155,15 @@ def lib():
         L.still_paged_attend.argtypes = [cache, seqs, ctypes.POINTER(still_paged_attend_config),
                                          *[ctypes.c_void_p] * 4, ctypes.c_size_t, ctypes.c_void_p]
         L.still_paged_attend.restype = ctypes.c_int32
+        L.still_paged_attend_lse.argtypes = [cache, seqs, ctypes.POINTER(still_paged_attend_config),
+                                             *[ctypes.c_void_p] * 5, ctypes.c_size_t, ctypes.c_void_p]
+        L.still_paged_attend_lse.restype = ctypes.c_int32
+        cache8 = ctypes.POINTER(still_paged8_cache)
+        for plain, eight in ((L.still_paged_append, L.still_paged8_append), (L.still_paged_gather, L.still_paged8_gather),
+                             (L.still_paged_attend_workspace_size, L.still_paged8_attend_workspace_size),
+                             (L.still_paged_attend_lse, L.still_paged8_attend)):
+            eight.argtypes = [cache8, *plain.argtypes[1:]]
+            eight.restype = plain.restype
         L.still_status_string.argtypes = [ctypes.c_int32]
         L.still_status_string.restype = ctypes.c_char_p
         L.still_last_error.argtypes = []
@@ -278,6 +294,38 @@ def still_paged_attend(cache: still_paged_cache, seqs: still_paged_seqs, cfg: st
     """Raw entry point (pointers or tensors); returns the status code."""
     return lib().still_paged_attend(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(cfg), _ptr(q),
                                     _ptr(q_positions), _ptr(out), _ptr(workspace), workspace_bytes, _ptr(stream))
+
+
+def still_paged_attend_lse(cache: still_paged_cache, seqs: still_paged_seqs, cfg: still_paged_attend_config, q,
+                           q_positions, out, lse, workspace, workspace_bytes: int, stream) -> int:
+    """Raw entry point (pointers or tensors); returns the status code."""
+    return lib().still_paged_attend_lse(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(cfg), _ptr(q),
+                                        _ptr(q_positions), _ptr(out), _ptr(lse), _ptr(workspace), workspace_bytes,
+                                        _ptr(stream))
+
+
+def still_paged8_append(cache: still_paged8_cache, seqs: still_paged_seqs, tokens: still_paged_tokens, stream) -> int:
+    """Raw entry point; returns the status code."""
+    return lib().still_paged8_append(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(tokens), _ptr(stream))
+
+
+def still_paged8_gather(cache: still_paged8_cache, seqs: still_paged_seqs, seq: int, start: int, n: int, K, V, beta,
+                        stream) -> int:
+    """Raw entry point (pointers or tensors); returns the status code."""
+    return lib().still_paged8_gather(ctypes.byref(cache), ctypes.byref(seqs), seq, start, n, _ptr(K), _ptr(V),
+                                     _ptr(beta), _ptr(stream))
+
+
+def still_paged8_attend_workspace_size(cache: still_paged8_cache, cfg: still_paged_attend_config) -> int:
+    return int(lib().still_paged8_attend_workspace_size(ctypes.byref(cache), ctypes.byref(cfg)))
+
+
+def still_paged8_attend(cache: still_paged8_cache, seqs: still_paged_seqs, cfg: still_paged_attend_config, q,
+                        q_positions, out, lse, workspace, workspace_bytes: int, stream) -> int:
+    """Raw entry point (pointers or tensors); returns the status code."""
+    return lib().still_paged8_attend(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(cfg), _ptr(q),
+                                     _ptr(q_positions), _ptr(out), _ptr(lse), _ptr(workspace), workspace_bytes,
+                                     _ptr(stream))
 
 
 STILL_PAGED_WORKSPACE_BYTES = 17 << 20
@@ -533,12 +581,13 @@ def _want(x, name: str, dtype, shape, dev: int) -> None:
     _refuse(-1, f"{name} is not contiguous")
 
 
-def _want_rows(x, name: str, pages, shape) -> None:
-    """x is a tensor of the pages' type with this shape and whole rows, on their GPU."""
-    if x.dtype == pages.dtype and x.shape == shape and x.stride(2) == 1 and x.get_device() == pages.get_device():
+def _want_rows(x, name: str, pages, shape, dtype=None) -> None:
+    """x is a tensor of the pages' type (or the one given) with this shape and whole rows, on their GPU."""
+    dtype = dtype or pages.dtype
+    if x.dtype == dtype and x.shape == shape and x.stride(2) == 1 and x.get_device() == pages.get_device():
         return
-    if x.dtype != pages.dtype:
-        _refuse(-3, f"{name} is {x.dtype}, the pages {pages.dtype}")
+    if x.dtype != dtype:
+        _refuse(-3, f"{name} is {x.dtype}, the pages {dtype}" if dtype == pages.dtype else f"{name} is {x.dtype}, not {dtype}")
     if x.shape != shape:
         _refuse(-2, f"{name} has shape {tuple(x.shape)}, not {tuple(shape)}")
     if x.get_device() != pages.get_device():
@@ -546,12 +595,12 @@ def _want_rows(x, name: str, pages, shape) -> None:
     _refuse(-1, f"{name}'s rows are not contiguous")
 
 
-def _refuse_paged(torch, k_pages, v_pages, beta_pages, table, lens) -> None:
+def _refuse_paged(torch, k_pages, v_pages, beta_pages, table, lens, dtypes=None) -> None:
     """Says what is wrong with a paged cache or its sequences."""
     shape, dt, dev = k_pages.shape, k_pages.dtype, k_pages.get_device()
     if len(shape) != 4:
         _refuse(-2, f"k_pages has {len(shape)} dimensions, not [n_pages, H, page_size, d]")
-    if dt != torch.bfloat16 and dt != torch.float32:
+    if dt not in (dtypes or (torch.bfloat16, torch.float32)):
         _refuse(-3, f"pages of {dt}: bfloat16 and float32 are supported")
     if not k_pages.is_contiguous():
         _refuse(-1, "k_pages is not contiguous")
@@ -602,29 +651,16 @@ def _on(torch, dev: int, call, *args) -> None:
         _check(status)
 
 
-def paged_append(k, v, k_pages, v_pages, table, lens, offsets=None, positions=None, rope_theta: float = 0.0,
-                 beta=None, beta_pages=None) -> None:
-    """Append rows k, v [n_tokens, H, d] to the pages [n_pages, H, P, d] of
-    their sequences on the current stream (still_paged_append).  table
-    [n_seqs, pages] and lens [n_seqs] are int32 device tensors; lens counts the
-    new entries already.  Sequence s's tokens are offsets[s] .. offsets[s + 1] - 1
-    (int32 [n_seqs + 1]); without offsets every sequence has n_tokens / n_seqs.
-    With ``positions`` (float64 [n_tokens] logical positions) and
-    ``rope_theta`` the keys are rotated there first.  k and v may be strided
-    views with contiguous rows (slices of a fused projection, transposed [H, t, d]
-    outputs of the compactor).  A cache that keeps bias passes ``beta_pages``
-    [n_pages, H, P] float32 always, and the entries' ``beta`` [n_tokens, H]
-    float32 where it is not zero."""
-    torch = _torch()
-    cache, seqs, dev = _paged(torch, k_pages, v_pages, beta_pages, table, lens)
+def _tokens(torch, k, v, k_pages, dtype, cache, seqs, dev, offsets, positions, rope_theta, beta):
+    """C view of rows k, v of this type to append, checked."""
     if k.dim() != 3:
         _refuse(-2, f"k has {k.dim()} dimensions, not [n_tokens, H, d]")
     n = k.shape[0]
     if n >= 1 << 31:
         _refuse(-2, f"{n} tokens given")
     shape = (n, cache.n_kv_heads, cache.head_dim)
-    _want_rows(k, "k", k_pages, shape)
-    _want_rows(v, "v", k_pages, shape)
+    _want_rows(k, "k", k_pages, shape, dtype)
+    _want_rows(v, "v", k_pages, shape, dtype)
     off = pos = b = None
     if offsets is not None:
         _want(offsets, "offsets", torch.int32, (seqs.n_seqs + 1,), dev)
@@ -644,8 +680,48 @@ def paged_append(k, v, k_pages, v_pages, table, lens, offsets=None, positions=No
         kt = vt = 0
     if shape[1] == 1:
         kh = vh = 0
-    tokens = still_paged_tokens(n, k.data_ptr(), v.data_ptr(), kt, kh, vt, vh, b, ts, hs, off, pos, rope_theta)
+    return still_paged_tokens(n, k.data_ptr(), v.data_ptr(), kt, kh, vt, vh, b, ts, hs, off, pos, rope_theta)
+
+
+def paged_append(k, v, k_pages, v_pages, table, lens, offsets=None, positions=None, rope_theta: float = 0.0,
+                 beta=None, beta_pages=None) -> None:
+    """Append rows k, v [n_tokens, H, d] to the pages [n_pages, H, P, d] of
+    their sequences on the current stream (still_paged_append).  table
+    [n_seqs, pages] and lens [n_seqs] are int32 device tensors; lens counts the
+    new entries already.  Sequence s's tokens are offsets[s] .. offsets[s + 1] - 1
+    (int32 [n_seqs + 1]); without offsets every sequence has n_tokens / n_seqs.
+    With ``positions`` (float64 [n_tokens] logical positions) and
+    ``rope_theta`` the keys are rotated there first.  k and v may be strided
+    views with contiguous rows (slices of a fused projection, transposed [H, t, d]
+    outputs of the compactor).  A cache that keeps bias passes ``beta_pages``
+    [n_pages, H, P] float32 always, and the entries' ``beta`` [n_tokens, H]
+    float32 where it is not zero."""
+    torch = _torch()
+    cache, seqs, dev = _paged(torch, k_pages, v_pages, beta_pages, table, lens)
+    tokens = _tokens(torch, k, v, k_pages, k_pages.dtype, cache, seqs, dev, offsets, positions, rope_theta, beta)
     _on(torch, dev, (_lib or lib()).still_paged_append, ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(tokens))
+
+
+def _dense(torch, k_pages, dtype, cache, dev, seq, start, n, beta_pages, out):
+    """(seq, start, n, (K, V) or (K, V, beta) of this type to fill), checked."""
+    seq, start, n = int(seq), int(start), int(n)
+    if max(abs(seq), abs(start), abs(n)) >= 1 << 31:
+        _refuse(-2, f"entries [{start}, {start + n}) of sequence {seq} asked for")
+    shape = (cache.n_kv_heads, n, cache.head_dim)
+    if out is None:
+        if n < 0:
+            _refuse(-2, f"{n} entries asked for")
+        out = tuple(torch.empty(shape, dtype=dtype, device=k_pages.device) for _ in range(2))
+        if beta_pages is not None:
+            out += (torch.empty(shape[:2], dtype=torch.float32, device=k_pages.device),)
+    elif len(out) != (2 if beta_pages is None else 3):
+        _refuse(-2, "out holds K, V and, with beta_pages, beta")
+    else:
+        _want(out[0], "out[0]", dtype, shape, dev)
+        _want(out[1], "out[1]", dtype, shape, dev)
+        if beta_pages is not None:
+            _want(out[2], "out[2]", torch.float32, shape[:2], dev)
+    return seq, start, n, out
 
 
 def paged_gather(k_pages, v_pages, table, lens, seq: int, n: int, start: int = 0, beta_pages=None, out=None):
@@ -654,39 +730,14 @@ def paged_gather(k_pages, v_pages, table, lens, seq: int, n: int, start: int = 0
     current stream; into ``out`` (such a tuple) where given."""
     torch = _torch()
     cache, seqs, dev = _paged(torch, k_pages, v_pages, beta_pages, table, lens)
-    seq, start, n = int(seq), int(start), int(n)
-    if max(abs(seq), abs(start), abs(n)) >= 1 << 31:
-        _refuse(-2, f"entries [{start}, {start + n}) of sequence {seq} asked for")
-    shape = (cache.n_kv_heads, n, cache.head_dim)
-    if out is None:
-        if n < 0:
-            _refuse(-2, f"{n} entries asked for")
-        out = tuple(torch.empty(shape, dtype=k_pages.dtype, device=k_pages.device) for _ in range(2))
-        if beta_pages is not None:
-            out += (torch.empty(shape[:2], dtype=torch.float32, device=k_pages.device),)
-    elif len(out) != (2 if beta_pages is None else 3):
-        _refuse(-2, "out holds K, V and, with beta_pages, beta")
-    else:
-        _want(out[0], "out[0]", k_pages.dtype, shape, dev)
-        _want(out[1], "out[1]", k_pages.dtype, shape, dev)
-        if beta_pages is not None:
-            _want(out[2], "out[2]", torch.float32, shape[:2], dev)
+    seq, start, n, out = _dense(torch, k_pages, k_pages.dtype, cache, dev, seq, start, n, beta_pages, out)
     _on(torch, dev, (_lib or lib()).still_paged_gather, ctypes.byref(cache), ctypes.byref(seqs), seq, start, n,
         out[0].data_ptr(), out[1].data_ptr(), None if beta_pages is None else out[2].data_ptr())
     return out
 
 
-def paged_attend(q, k_pages, v_pages, table, lens, causal: bool = False, scale: float = 0.0, beta_pages=None,
-                 q_positions=None, rope_theta: float = 0.0, workspace=None, out=None):
-    """Attention of the newest tokens q [n_seqs * n_queries, H * group, d]
-    (sequence by sequence) over their sequences' pages through
-    still_paged_attend on the current stream; returns out, contiguous, like q.
-    q may be a strided view with contiguous tokens.  With ``q_positions``
-    (float64, one per token) and ``rope_theta`` the kernel rotates q first.
-    ``out`` and ``workspace`` (STILL_PAGED_WORKSPACE_BYTES serve every call)
-    may be given, so that the call allocates nothing (graph capture)."""
-    torch = _torch()
-    cache, seqs, dev = _paged(torch, k_pages, v_pages, beta_pages, table, lens)
+def _queries(torch, q, k_pages, dtype, cache, seqs, dev, causal, scale, q_positions, rope_theta):
+    """(C view of how the newest tokens q of this type attend, their positions' address), checked."""
     shape = q.shape
     if len(shape) != 3:
         _refuse(-2, f"q has {len(shape)} dimensions, not [n_seqs * n_queries, H * group, d]")
@@ -694,7 +745,7 @@ def paged_attend(q, k_pages, v_pages, table, lens, causal: bool = False, scale: 
     H, n = cache.n_kv_heads, seqs.n_seqs
     if n < 1 or H < 1 or d != cache.head_dim or Hq < H or Hq % H or tokens < n or tokens % n:
         _refuse(-2, f"q {tuple(shape)} does not fit {n} sequences and pages {tuple(k_pages.shape)}")
-    _want_rows(q, "q", k_pages, shape)
+    _want_rows(q, "q", k_pages, shape, dtype)
     qs = q.stride()
     if (qs[1] != d and Hq > 1) or (qs[0] == 0 and tokens > 1):   # (a stride of 0 means dense tokens to the C call)
         _refuse(-1, "q's tokens are not contiguous, or the same one")
@@ -702,22 +753,126 @@ def paged_attend(q, k_pages, v_pages, table, lens, causal: bool = False, scale: 
     if q_positions is not None:
         _want(q_positions, "q_positions", torch.float64, (tokens,), dev)
         pos = q_positions.data_ptr()
-    cfg = still_paged_attend_config(Hq // H, tokens // n, causal, scale, rope_theta, qs[0] if tokens > 1 else 0)
+    return still_paged_attend_config(Hq // H, tokens // n, causal, scale, rope_theta, qs[0] if tokens > 1 else 0), pos
+
+
+def _attend(torch, q, k_pages, cache, seqs, dev, causal, scale, q_positions, rope_theta, workspace, out, lse):
+    """Attention over checked pages, of 8 bits or of q's type."""
+    eight = type(cache) is still_paged8_cache
+    cfg, pos = _queries(torch, q, k_pages, q.dtype if eight else k_pages.dtype, cache, seqs, dev, causal, scale, q_positions,
+                        rope_theta)
+    shape = q.shape
     if out is None:
         out = torch.empty(shape, dtype=q.dtype, device=q.device)
     else:
         _want(out, "out", q.dtype, shape, dev)
+    if lse is not None:
+        _want(lse, "lse", torch.float32, shape[:2], dev)
     if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
         _refuse(-1, f"workspace is on {workspace.device}, the pages on {k_pages.device}, or it is not contiguous")
     room = 0 if workspace is None else workspace.numel()
     if room < STILL_PAGED_WORKSPACE_BYTES:
-        need = still_paged_attend_workspace_size(cache, cfg)
+        need = (still_paged8_attend_workspace_size if eight else still_paged_attend_workspace_size)(cache, cfg)
         if room < need:
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
             room = need
-    _on(torch, dev, (_lib or lib()).still_paged_attend, ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(cfg), q.data_ptr(),
-        pos, out.data_ptr(), _ptr(workspace), room)
+    call = (_lib or lib()).still_paged8_attend if eight else (_lib or lib()).still_paged_attend_lse
+    _on(torch, dev, call, ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(cfg), q.data_ptr(), pos, out.data_ptr(),
+        None if lse is None else lse.data_ptr(), _ptr(workspace), room)
     return out
+
+
+def paged_attend(q, k_pages, v_pages, table, lens, causal: bool = False, scale: float = 0.0, beta_pages=None,
+                 q_positions=None, rope_theta: float = 0.0, workspace=None, out=None, lse=None):
+    """Attention of the newest tokens q [n_seqs * n_queries, H * group, d]
+    (sequence by sequence) over their sequences' pages through
+    still_paged_attend on the current stream; returns out, contiguous, like q.
+    q may be a strided view with contiguous tokens.  With ``q_positions``
+    (float64, one per token) and ``rope_theta`` the kernel rotates q first.
+    ``out`` and ``workspace`` (STILL_PAGED_WORKSPACE_BYTES serve every call)
+    may be given, so that the call allocates nothing (graph capture).  ``lse``
+    (float32 [n_seqs * n_queries, H * group], contiguous) is filled with the log of each row's
+    sum of exponentials, minus infinity for a row that sees nothing."""
+    torch = _torch()
+    cache, seqs, dev = _paged(torch, k_pages, v_pages, beta_pages, table, lens)
+    return _attend(torch, q, k_pages, cache, seqs, dev, causal, scale, q_positions, rope_theta, workspace, out, lse)
+
+
+# ---- pages of 8 bits
+
+def _refuse_paged8(torch, k_pages, v_pages, k_scales, v_scales, beta_pages, table, lens, dtype) -> None:
+    """Says what is wrong with a paged cache in 8 bits or its sequences."""
+    shape, dev = k_pages.shape, k_pages.get_device()
+    if len(shape) != 4:
+        _refuse(-2, f"k_pages has {len(shape)} dimensions, not [n_pages, H, page_size, d]")
+    if k_pages.dtype != torch.float8_e4m3fn:
+        _refuse(-3, f"pages of {k_pages.dtype}, not float8_e4m3fn")
+    if dtype != torch.bfloat16 and dtype != torch.float32:
+        _refuse(-3, f"rows of {dtype}: bfloat16 and float32 are supported")
+    blocks = (shape[0], shape[1], shape[2] // 16)
+    _want(v_pages, "v_pages", k_pages.dtype, shape, dev)
+    _want(k_scales, "k_scales", torch.float32, blocks, dev)
+    _want(v_scales, "v_scales", torch.float32, blocks, dev)
+    _refuse_paged(torch, k_pages, v_pages, beta_pages, table, lens, (torch.float8_e4m3fn,))
+
+
+def _paged8(torch, k_pages, v_pages, k_scales, v_scales, beta_pages, table, lens, dtype):
+    """(C view of a paged cache in 8 bits with rows of this type, C view of its sequences, GPU), checked."""
+    shape, dt, dev, size = k_pages.shape, k_pages.dtype, k_pages.get_device(), table.shape
+    i32, f32 = torch.int32, torch.float32
+    # one expression: this runs before every call of a decode step
+    if not (dev >= 0 and len(shape) == 4 and dt is torch.float8_e4m3fn and (dtype is f32 or dtype is torch.bfloat16)
+            and v_pages.dtype is dt and v_pages.shape == shape and k_pages.is_contiguous() and v_pages.is_contiguous()
+            and v_pages.get_device() == dev and table.dtype is i32 and len(size) == 2 and lens.dtype is i32
+            and k_scales.dtype is f32 and v_scales.dtype is f32
+            and k_scales.shape == v_scales.shape == (shape[0], shape[1], shape[2] // 16)
+            and k_scales.is_contiguous() and v_scales.is_contiguous()
+            and k_scales.get_device() == dev and v_scales.get_device() == dev
+            and lens.shape == size[:1] and lens.is_contiguous() and lens.get_device() == dev
+            and table.get_device() == dev and (table.stride(1) == 1 or size[1] <= 1) and (size[0] <= 1 or table.stride(0) < 1 << 31)
+            and size[0] < 1 << 31 and size[1] < 1 << 31
+            and (beta_pages is None or beta_pages.dtype is f32 and beta_pages.shape == shape[:3]
+                 and beta_pages.is_contiguous() and beta_pages.get_device() == dev)):
+        _refuse_paged8(torch, k_pages, v_pages, k_scales, v_scales, beta_pages, table, lens, dtype)
+    n_pages, H, P, d = shape
+    n, width = size
+    return (still_paged8_cache(H, d, P, n_pages, dtype is f32, k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(),
+                               v_scales.data_ptr(), None if beta_pages is None else beta_pages.data_ptr()),
+            still_paged_seqs(n, width, table.stride(0) if n > 1 else width, table.data_ptr(), lens.data_ptr()), dev)
+
+
+def paged8_append(k, v, k_pages, v_pages, k_scales, v_scales, table, lens, offsets=None, positions=None,
+                  rope_theta: float = 0.0, beta=None, beta_pages=None) -> None:
+    """paged_append into pages of 8 bits (still_paged8_append): k_pages, v_pages
+    [n_pages, H, P, d] float8_e4m3fn and their scales [n_pages, H, P // 16] float32, one
+    for each block of 16 entries and head, which the call sets: powers of two, that grow
+    with what their blocks get.  k and v [n_tokens, H, d] are bfloat16 or float32."""
+    torch = _torch()
+    cache, seqs, dev = _paged8(torch, k_pages, v_pages, k_scales, v_scales, beta_pages, table, lens, k.dtype)
+    tokens = _tokens(torch, k, v, k_pages, k.dtype, cache, seqs, dev, offsets, positions, rope_theta, beta)
+    _on(torch, dev, (_lib or lib()).still_paged8_append, ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(tokens))
+
+
+def paged8_gather(k_pages, v_pages, k_scales, v_scales, table, lens, seq: int, n: int, start: int = 0, dtype=None,
+                  beta_pages=None, out=None):
+    """paged_gather from pages of 8 bits (still_paged8_gather): the rows that entries
+    [start, start + n) stand for, of ``dtype`` (bfloat16, or out's type)."""
+    torch = _torch()
+    dtype = dtype or (out[0].dtype if out else torch.bfloat16)
+    cache, seqs, dev = _paged8(torch, k_pages, v_pages, k_scales, v_scales, beta_pages, table, lens, dtype)
+    seq, start, n, out = _dense(torch, k_pages, dtype, cache, dev, seq, start, n, beta_pages, out)
+    _on(torch, dev, (_lib or lib()).still_paged8_gather, ctypes.byref(cache), ctypes.byref(seqs), seq, start, n,
+        out[0].data_ptr(), out[1].data_ptr(), None if beta_pages is None else out[2].data_ptr())
+    return out
+
+
+def paged8_attend(q, k_pages, v_pages, k_scales, v_scales, table, lens, causal: bool = False, scale: float = 0.0,
+                  beta_pages=None, q_positions=None, rope_theta: float = 0.0, workspace=None, out=None, lse=None):
+    """paged_attend over pages of 8 bits (still_paged8_attend); q and out are
+    bfloat16 or float32."""
+    torch = _torch()
+    cache, seqs, dev = _paged8(torch, k_pages, v_pages, k_scales, v_scales, beta_pages, table, lens, q.dtype)
+    return _attend(torch, q, k_pages, cache, seqs, dev, causal, scale, q_positions, rope_theta, workspace, out, lse)
 
 
 def compact_paged(cfg: configs.CompactorConfig, weights: List[Dict[str, object]], k_pages: List, v_pages: List,

@@ -17,6 +17,7 @@ namespace still {
 struct PagedArgs {
   char* k;              // pages
   char* v;
+  float *ks, *vs;       // pages of 8 bits: scales [n_pages][H][P / 16], else NULL
   float* beta;          // [n_pages][H][P] or NULL
   const int* table;
   const int* lens;
@@ -274,6 +275,7 @@ struct PagedAttendArgs {
   const char* q;       // tokens of [H * group][d]
   long q_ts;           // bytes
   char* out;
+  float* lse;          // [tokens][H * group] or NULL
   const double* qpos;  // NULL: q as given
   double log2_theta;
   int group, nq, causal;
@@ -305,26 +307,35 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr int paged_waves(int esize, int D, int NR) { return NR == 2 && D <= 128 && esize == 4 ? 8 : 4; }
 constexpr int paged_resident(int D, int NR) { return NR == 1 && D <= 128 ? 2 : 1; }
 constexpr int paged_tiles(int esize, int D, int NR) {
-  return (NR == 1 && D == 64 ? 64 : 128) * 1024 / (paged_waves(esize, D, NR) * paged_resident(D, NR) * 32 * D * esize);
+  return std::min(8, (NR == 1 && D == 64 ? 64 : 128) * 1024 / (paged_waves(esize, D, NR) * paged_resident(D, NR) * 32 * D * esize));
 }
 // Whole sequences: waves per workgroup (two per SIMD, or as the registers allow).
 constexpr int paged_team(int D, int NR) { return NR == 1 && D <= 128 ? 8 : 4; }
 
+// An e4m3 code of a cache in 8 bits (OCP: 4 exponent bits, bias 7, 3 fraction bits, no infinities).
+struct e4m3 {
+  uint8_t bits;
+};
+constexpr int PAGED_BLOCK = 16;   // entries of a head that share a scale: those of a tile
+
 // SW: waves of a workgroup that takes a whole sequence; 0: parts of the line; -1:
-// parts, the entries' loads streaming past the caches.
-template <class IT, int D, int NR, int SW>
+// parts, the entries' loads streaming past the caches.  IT: queries and outputs, CT: entries.
+template <class IT, int D, int NR, int SW, class CT = IT>
 struct PagedTile {
-  static constexpr bool B16 = sizeof(IT) == 2;
-  static constexpr int NW = SW > 0 ? SW : paged_waves(sizeof(IT), D, NR);
+  static constexpr bool C8 = sizeof(CT) == 1, B16 = C8 || sizeof(IT) == 2;   // B16: products of bf16
+  static constexpr int NW = SW > 0 ? SW : paged_waves(sizeof(CT), D, NR);
   static constexpr int PER_SIMD = SW == 1 ? (D <= 128 ? 2 : 1) : NW * (SW > 0 ? 1 : paged_resident(D, NR)) / 4;
-  static constexpr int NKT = SW > 0 ? (B16 ? 2 : 1) : paged_tiles(sizeof(IT), D, NR);   // 16-entry tiles per chunk
+  static constexpr int NKT = SW > 0 ? (B16 ? 2 : 1) : paged_tiles(sizeof(CT), D, NR);   // 16-entry tiles per chunk
   static constexpr int CH = 16 * NKT;
   static constexpr int AUX = SW < 0 ? 2 : 0;            // cache policy of the entries' loads: 2 non-temporal
-  static constexpr int ROWB = D * (int)sizeof(IT);
+  static constexpr int ROWB = D * (int)sizeof(CT);
   static constexpr int NP = ROWB / 64;                  // 16-byte pieces of a key per lane
-  static constexpr int FPT = D / 16, VB = FPT * (int)sizeof(IT);
-  static constexpr int PB = VB < 16 ? VB : 16, EPV = PB / (int)sizeof(IT);   // bytes and features of a piece of a value row
-  static constexpr int QROW = ROWB + 16;                // query rows in LDS (padded: 16 rows at one piece)
+  static constexpr int FPT = D / 16, VB = FPT * (int)sizeof(CT);
+  static constexpr int PB = VB < 16 ? VB : 16, EPV = PB / (int)sizeof(CT);   // bytes and features of a piece of a value row
+  static constexpr int IROWB = D * (int)sizeof(IT);     // a row of q and out
+  static constexpr int QROW = D * (B16 ? 2 : 4) + 16;   // query rows in LDS (padded: 16 rows at one piece)
+  // queries that no single bf16 holds go in as three
+  static __host__ __device__ bool split(bool rot) { return B16 && (rot || sizeof(IT) == 4); }
   static constexpr int OROW = D + 4;
   static constexpr int QPART = 16 * NR * QROW;
 };
@@ -335,7 +346,7 @@ struct PagedTile {
 // workgroups of one wave, many of which share a CU.
 constexpr bool paged_alias(int D, int NR, int SW) { return SW == 1 || D * NR > 256; }
 template <class TL>
-inline __host__ __device__ int paged_q_bytes(bool rot) { return (TL::B16 && rot ? 3 : 1) * TL::QPART; }
+inline __host__ __device__ int paged_q_bytes(bool rot) { return (TL::split(rot) ? 3 : 1) * TL::QPART; }
 template <class TL, int D, int NR, int SW>
 inline size_t paged_lds_bytes(int R, int nq, bool rot) {
   const size_t q = paged_q_bytes<TL>(rot), o = (size_t)TL::NW * R * TL::OROW * sizeof(float);
@@ -410,12 +421,14 @@ __device__ __forceinline__ int list_find(const int (&x)[4], int v) {
   return i;
 }
 
-// N pieces of PB bytes (8 or 16) of a buffer from byte off, 16 PB apart, as words
+// N pieces of PB bytes (4, 8 or 16) of a buffer from byte off, 16 PB apart, as words
 template <int PB, int N, int AUX>
 __device__ __forceinline__ void buffer_pieces(__amdgpu_buffer_rsrc_t r, int off, uint32_t (&w)[N * PB / 4]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    if constexpr (PB == 8) {
+    if constexpr (PB == 4) {
+      w[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_raw_buffer_load_b32(r, off + 16 * PB * i, 0, AUX));
+    } else if constexpr (PB == 8) {
       const u32x2 u = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off + 16 * PB * i, 0, AUX));
       w[2 * i] = u.x;
       w[2 * i + 1] = u.y;
@@ -430,11 +443,17 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t paged_rows(const void* p, int 
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000);
 }
 
-template <class IT, int D, int NR, int SW>
-__global__ __launch_bounds__((64 * PagedTile<IT, D, NR, SW>::NW), (PagedTile<IT, D, NR, SW>::PER_SIMD))
+// Two of the four e4m3 codes of a word (HI: the upper two) as bf16, which holds them exactly.
+template <bool HI>
+__device__ __forceinline__ uint32_t e4m3_pair(uint32_t w) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, HI));
+}
+
+template <class IT, int D, int NR, int SW, class CT = IT>
+__global__ __launch_bounds__((64 * PagedTile<IT, D, NR, SW, CT>::NW), (PagedTile<IT, D, NR, SW, CT>::PER_SIMD))
 void paged_attend_kernel(PagedAttendArgs a) {
-  using TL = PagedTile<IT, D, NR, SW>;
-  constexpr bool SINGLE = SW > 0;
+  using TL = PagedTile<IT, D, NR, SW, CT>;
+  constexpr bool SINGLE = SW > 0, C8 = TL::C8;
   constexpr int NKT = TL::NKT, CH = TL::CH, NP = TL::NP, FPT = TL::FPT, VB = TL::VB, ROWB = TL::ROWB, NW = TL::NW;
   constexpr int QROW = TL::QROW, OROW = TL::OROW, NT = 64 * NW, HD = D / 2;
   constexpr bool ALIAS = paged_alias(D, NR, SW);
@@ -457,17 +476,21 @@ void paged_attend_kernel(PagedAttendArgs a) {
 
   // ---- a sequence's query rows, row g * nq + i query i of head h * group + g: a
   // thread's pairs of 16-byte pieces D / 2 apart, the members of the rotated pairs
-  constexpr int HP = ROWB / 32, EPP = 16 / (int)sizeof(IT), QI = (16 * NR * HP + NT - 1) / NT;
-  u32x4 qr[QI][2];
+  // (of 8 values where they end up as bf16)
+  constexpr int EPP = TL::B16 ? 8 : 4, NV = EPP * (int)sizeof(IT) / 16, HP = HD / EPP, QI = (16 * NR * HP + NT - 1) / NT;
+  u32x4 qr[QI][2][NV];
   // a thread's angles belong to one pair where the threads are a multiple of the pairs
   const double inv_freq = rot ? exp2(a.log2_theta * (-2.0 * (tid % HD) / D)) : 0.0;
   auto load_q = [&](int s) {
 #pragma unroll
     for (int k = 0; k < QI; ++k) {
       const int e = k * NT + tid, r = min(e / HP, R - 1), hr = head_of(r);   // (rows past R repeat the last one)
-      const u32x4* q = (const u32x4*)(a.q + ((long)s * a.nq + r - hr * a.nq) * a.q_ts + (h * a.group + hr) * ROWB);
-      qr[k][0] = q[e % HP];
-      qr[k][1] = q[e % HP + HP];
+      const u32x4* q = (const u32x4*)(a.q + ((long)s * a.nq + r - hr * a.nq) * a.q_ts + (h * a.group + hr) * TL::IROWB);
+#pragma unroll
+      for (int u = 0; u < NV; ++u) {
+        qr[k][0][u] = q[e % HP * NV + u];
+        qr[k][1][u] = q[(e % HP + HP) * NV + u];
+      }
     }
   };
   auto stage_q = [&](int s) {   // rotated, in LDS; ends with a barrier
@@ -481,36 +504,41 @@ void paged_attend_kernel(PagedAttendArgs a) {
     for (int k = 0; k < QI; ++k) {
       const int e = k * NT + tid, r = e / HP, j = e % HP * EPP;
       if (16 * NR * HP % NT && r >= 16 * NR) break;
-      if (rot) {
-        const int i = min(r, R - 1);
-        const float2* c = cs + (i - head_of(i) * a.nq) * HD + j;
+      if (TL::split(rot) || rot) {
         float x0[EPP], x1[EPP];
-        unpack16<IT>(qr[k][0], x0);
-        unpack16<IT>(qr[k][1], x1);
 #pragma unroll
-        for (int u = 0; u < EPP; ++u) {
-          const float y = x0[u] * c[u].x - x1[u] * c[u].y;
-          x1[u] = x1[u] * c[u].x + x0[u] * c[u].y;
-          x0[u] = y;
+        for (int u = 0; u < NV; ++u) {
+          unpack16<IT>(qr[k][0][u], *(float(*)[EPP / NV])(x0 + u * (EPP / NV)));
+          unpack16<IT>(qr[k][1][u], *(float(*)[EPP / NV])(x1 + u * (EPP / NV)));
+        }
+        if (rot) {
+          const int i = min(r, R - 1);
+          const float2* c = cs + (i - head_of(i) * a.nq) * HD + j;
+#pragma unroll
+          for (int u = 0; u < EPP; ++u) {
+            const float y = x0[u] * c[u].x - x1[u] * c[u].y;
+            x1[u] = x1[u] * c[u].x + x0[u] * c[u].y;
+            x0[u] = y;
+          }
         }
         if constexpr (TL::B16) {
           bf16x8 p0[3], p1[3];
           bf16_parts(x0, p0);
           bf16_parts(x1, p1);
-          qr[k][0] = __builtin_bit_cast(u32x4, p0[0]);
-          qr[k][1] = __builtin_bit_cast(u32x4, p1[0]);
+          qr[k][0][0] = __builtin_bit_cast(u32x4, p0[0]);
+          qr[k][1][0] = __builtin_bit_cast(u32x4, p1[0]);
 #pragma unroll
           for (int part = 1; part < 3; ++part) {
             *(bf16x8*)(qs + part * TL::QPART + r * QROW + 16 * (e % HP)) = p0[part];
             *(bf16x8*)(qs + part * TL::QPART + r * QROW + 16 * (e % HP + HP)) = p1[part];
           }
         } else {
-          qr[k][0] = u32x4{__float_as_uint(x0[0]), __float_as_uint(x0[1]), __float_as_uint(x0[2]), __float_as_uint(x0[3])};
-          qr[k][1] = u32x4{__float_as_uint(x1[0]), __float_as_uint(x1[1]), __float_as_uint(x1[2]), __float_as_uint(x1[3])};
+          qr[k][0][0] = u32x4{__float_as_uint(x0[0]), __float_as_uint(x0[1]), __float_as_uint(x0[2]), __float_as_uint(x0[3])};
+          qr[k][1][0] = u32x4{__float_as_uint(x1[0]), __float_as_uint(x1[1]), __float_as_uint(x1[2]), __float_as_uint(x1[3])};
         }
       }
-      *(u32x4*)(qs + r * QROW + 16 * (e % HP)) = qr[k][0];
-      *(u32x4*)(qs + r * QROW + 16 * (e % HP + HP)) = qr[k][1];
+      *(u32x4*)(qs + r * QROW + 16 * (e % HP)) = qr[k][0][0];
+      *(u32x4*)(qs + r * QROW + 16 * (e % HP + HP)) = qr[k][1][0];
     }
     __syncthreads();
   };
@@ -606,10 +634,13 @@ void paged_attend_kernel(PagedAttendArgs a) {
     auto len_of = [&](int i) { return SINGLE ? lens[0] : list_get(lens, i); };
     // rows of sequences without entries
     for (int k = SINGLE ? 0 : g; k < cnt; k += SINGLE ? 1 : a.G)
-      if (len_of(k) == 0) {
-        for (int e = tid; e < R * (ROWB / 16); e += NT) {
+      if (len_of(k) == 0) {   // (minus infinity is the log of an empty sum)
+        constexpr int PPR = TL::IROWB / 16;
+        for (int e = tid; e < R * PPR; e += NT) {
           const u32x4 z = {0, 0, 0, 0};
-          ((u32x4*)(a.out + out_row(base + k, e / (ROWB / 16)) * (long)sizeof(IT)))[e % (ROWB / 16)] = z;
+          const long row = out_row(base + k, e / PPR);
+          ((u32x4*)(a.out + row * (long)sizeof(IT)))[e % PPR] = z;
+          if (a.lse && e % PPR == 0) a.lse[row / D] = -INFINITY;
         }
         if (!SINGLE && h == 0 && tid == 0 && a.by_seq) a.plan[base + k] = make_int4(-1, 0, 0, 0);
       }
@@ -648,6 +679,11 @@ void paged_attend_kernel(PagedAttendArgs a) {
     };
     u32x4 kp[NKT][NP];
     f32x4 bias[NKT];
+    float ks[C8 ? NKT : 1], vs[C8 ? NKT : 1];   // scales of the tiles' keys and values
+    auto scale_of = [&](const float* scales, const Tiles& k, int kt) {   // (of a tile without entries: 0)
+      return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(
+                                           paged_rows(scales + k.row[kt] / PAGED_BLOCK, k.nv[kt] > 0 ? 4 : 0), 0, 0, 0));
+    };
     uint32_t vr[NKT * 4][VB / 4];
     // (the offsets are opaque to the compiler, which would keep every sum of one with
     // a constant in a register of its own instead of in the load)
@@ -663,6 +699,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
         bias[kt] = __builtin_bit_cast(
             f32x4, __builtin_amdgcn_raw_buffer_load_b128(
                        paged_rows(a.c.beta + k.row[kt], a.c.beta && k.nv[kt] > 0 ? 16 * 4 : 0), boff, 0, 0));
+        if constexpr (C8) ks[kt] = scale_of(a.c.ks, k, kt);
       }
     };
     auto load_v = [&](const Tiles& k) {
@@ -673,6 +710,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
         const auto r = paged_rows(a.c.v + k.row[kt] * ROWB, k.nv[kt] * ROWB);
 #pragma unroll
         for (int j = 0; j < 4; ++j) buffer_pieces<TL::PB, VB / TL::PB, TL::AUX>(r, off + j * ROWB, vr[kt * 4 + j]);
+        if constexpr (C8) vs[kt] = scale_of(a.c.vs, k, kt);
       }
     };
     if (lo < hi) {
@@ -716,41 +754,64 @@ void paged_attend_kernel(PagedAttendArgs a) {
           for (int rt = 0; rt < NR; ++rt)
 #pragma unroll
             for (int kt = 0; kt < NKT; ++kt) x[rt][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int p = 0; p < NP; ++p)
+          // piece u of a key (8 bits: of two operands) against the same values of the query rows
+          auto product = [&](int part, int p, const u32x4 (&kv)[NKT], int at) {
 #pragma unroll
             for (int rt = 0; rt < NR; ++rt) {
-              const u32x4 qv = *(const u32x4*)(qs + (16 * rt + l) * QROW + 64 * p + 16 * lg);
+              const u32x4 qv = *(const u32x4*)(qs + part * TL::QPART + (16 * rt + l) * QROW + at);
 #pragma unroll
               for (int kt = 0; kt < NKT; ++kt) {
                 if constexpr (TL::B16) {
                   x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                      __builtin_bit_cast(bf16x8, kp[kt][p]), __builtin_bit_cast(bf16x8, qv), x[rt][kt], 0, 0, 0);
+                      __builtin_bit_cast(bf16x8, kv[kt]), __builtin_bit_cast(bf16x8, qv), x[rt][kt], 0, 0, 0);
                 } else {
 #pragma unroll
                   for (int e = 0; e < 4; ++e)
-                    x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kp[kt][p][e]),
+                    x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kv[kt][e]),
                                                                      __uint_as_float(qv[e]), x[rt][kt], 0, 0, 0);
                 }
               }
             }
-          if (TL::B16 && rot) {
+          };
+          if constexpr (C8) {
 #pragma unroll
-            for (int part = 1; part < 3; ++part)
+            for (int p = 0; p < NP; ++p)
 #pragma unroll
-              for (int p = 0; p < NP; ++p)
+              for (int half = 0; half < 2; ++half) {
+                u32x4 kv[NKT];
 #pragma unroll
-                for (int rt = 0; rt < NR; ++rt) {
-                  const u32x4 qv = *(const u32x4*)(qs + part * TL::QPART + (16 * rt + l) * QROW + 64 * p + 16 * lg);
-#pragma unroll
-                  for (int kt = 0; kt < NKT; ++kt)
-                    x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        __builtin_bit_cast(bf16x8, kp[kt][p]), __builtin_bit_cast(bf16x8, qv), x[rt][kt], 0, 0, 0);
+                for (int kt = 0; kt < NKT; ++kt) {
+                  const uint32_t w0 = kp[kt][p][2 * half], w1 = kp[kt][p][2 * half + 1];
+                  kv[kt] = u32x4{e4m3_pair<false>(w0), e4m3_pair<true>(w0), e4m3_pair<false>(w1), e4m3_pair<true>(w1)};
                 }
+                product(0, p, kv, 128 * p + 32 * lg + 16 * half);
+                if (TL::split(rot)) {
+                  product(1, p, kv, 128 * p + 32 * lg + 16 * half);
+                  product(2, p, kv, 128 * p + 32 * lg + 16 * half);
+                }
+              }
+          } else {
+            auto all = [&](int part) {
+#pragma unroll
+              for (int p = 0; p < NP; ++p) {
+                u32x4 kv[NKT];
+#pragma unroll
+                for (int kt = 0; kt < NKT; ++kt) kv[kt] = kp[kt][p];
+                product(part, p, kv, 64 * p + 16 * lg);
+              }
+            };
+            all(0);
+            if (TL::split(rot)) {
+              all(1);
+              all(2);
+            }
           }
           f32x4 bc[NKT];
 #pragma unroll
           for (int kt = 0; kt < NKT; ++kt) bc[kt] = bias[kt];
+          float kc[NKT];   // a tile's logit scale
+#pragma unroll
+          for (int kt = 0; kt < NKT; ++kt) kc[kt] = C8 ? a.scale * ks[C8 ? kt : 0] : a.scale;
           const Tiles next = resolve(nxt);
           load_k(next);
           __builtin_amdgcn_sched_barrier(0);
@@ -766,7 +827,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
 #pragma unroll
             for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) x[rt][kt][j] = fmaf(x[rt][kt][j], a.scale, bc[kt][j]);
+              for (int j = 0; j < 4; ++j) x[rt][kt][j] = fmaf(x[rt][kt][j], kc[kt], bc[kt][j]);
             if (!full) {
 #pragma unroll
               for (int kt = 0; kt < NKT; ++kt) {
@@ -813,11 +874,40 @@ void paged_attend_kernel(PagedAttendArgs a) {
 #pragma unroll
               for (int rt = 0; rt < NR; ++rt) {
                 const f32x4 &a0 = x[rt][k2], &a1 = x[rt][k2 + 1];
-                const float p[8] = {a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]};
+                float p[8] = {a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]};
+                if constexpr (C8) {   // (powers of two: exact)
+#pragma unroll
+                  for (int k = 0; k < 8; ++k) p[k] *= vs[k < 4 ? k2 : k2 + 1];
+                }
                 bf16_parts(p, pp[rt]);
               }
+              auto into = [&](int e, const u32x4& t) {
 #pragma unroll
-              for (int e = 0; e < FPT; e += 2) {   // an even and an odd feature of one word
+                for (int rt = 0; rt < NR; ++rt)
+#pragma unroll
+                  for (int part = 0; part < 3; ++part)
+                    o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t), pp[rt][part], o[rt][e], 0, 0, 0);
+              };
+              if constexpr (C8) {
+#pragma unroll
+                for (int e = 0; e < FPT; e += 4) {   // four features of one word
+                  u32x4 t[4];
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) {
+                    const uint32_t a0 = vr[4 * k2 + 2 * k][e >> 2], a1 = vr[4 * k2 + 2 * k + 1][e >> 2];
+                    const uint32_t w0 = __builtin_amdgcn_perm(a1, a0, 0x05010400u), w1 = __builtin_amdgcn_perm(a1, a0, 0x07030602u);
+                    t[0][k] = e4m3_pair<false>(w0);
+                    t[1][k] = e4m3_pair<true>(w0);
+                    t[2][k] = e4m3_pair<false>(w1);
+                    t[3][k] = e4m3_pair<true>(w1);
+                  }
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) into(e + k, t[k]);
+                }
+                continue;
+              }
+#pragma unroll
+              for (int e = 0; e < (C8 ? 0 : FPT); e += 2) {   // an even and an odd feature of one word
                 u32x4 t0, t1;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
@@ -903,6 +993,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
             IT* dst = (IT*)a.out + out_row(s, r) + x;
 #pragma unroll
             for (int k = 0; k < 4; ++k) dst[k] = from_f32<IT>(acc[k] * inv);
+            if (a.lse && x == 0) a.lse[out_row(s, r) / D] = M + logf(L);
           } else {
             *(float4*)(a.opart + (slot * R + r) * D + x) = make_float4(acc[0], acc[1], acc[2], acc[3]);
             if (x == 0) {
@@ -989,6 +1080,7 @@ __global__ __launch_bounds__(PAGED_MERGE_THREADS) void paged_merge_kernel(PagedA
     IT* dst = (IT*)a.out + (((long)p.x * a.nq + r % a.nq) * Hq + h * a.group + r / a.nq) * D + 4 * x;
 #pragma unroll
     for (int u = 0; u < 4; ++u) dst[u] = from_f32<IT>(z[u] * inv);
+    if (a.lse && x == 0) a.lse[((long)p.x * a.nq + r % a.nq) * Hq + h * a.group + r / a.nq] = M + logf(S);
   }
 }
 
