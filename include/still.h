@@ -459,6 +459,58 @@ still_status still_paged8_attend(const still_paged8_cache *cache, const still_pa
                                  const still_paged_attend_config *cfg, const void *q, const double *q_positions,
                                  void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Eviction by accumulated attention weight: what the entries of a sequence were
+ * looked at decides which of them stay.
+ * ------------------------------------------------------------------------- */
+
+/* Attention weights of the n_queries newest tokens, as still_paged_attend_lse
+ * takes them (the same cfg, q, q_positions and cache), summed over the rows of
+ * a KV head and added to the entries' scores:
+ *   scores_j += sum_r exp(s_rj - lse_r)
+ * over the rows r of the KV head that see entry j.  Entries j >= known[s] get the
+ * sum in place of what their score was: new entries, whose slot another sequence
+ * may have left (known NULL: there are none).  Entries behind the
+ * lengths and on absent pages keep theirs.  A row whose lse is minus infinity
+ * adds nothing.  The pages that a call's sequences name must be distinct.
+ *   lse     [n_seqs * n_queries][H*group] float32
+ *   known   [n_seqs] int32 or NULL
+ *   scores  [n_pages][H][page_size] float32 (16-byte aligned)
+ * The cache's v is not read and may be NULL.  The same inputs give the same bits. */
+still_status still_paged_score(const still_paged_cache *cache, const still_paged_seqs *seqs,
+                               const still_paged_attend_config *cfg, const void *q, const double *q_positions,
+                               const float *lse, const int32_t *known, float *scores, void *stream);
+still_status still_paged8_score(const still_paged8_cache *cache, const still_paged_seqs *seqs,
+                                const still_paged_attend_config *cfg, const void *q, const double *q_positions,
+                                const float *lse, const int32_t *known, float *scores, void *stream);
+
+typedef struct {
+  int32_t keep;     /* entries that a sequence keeps at most, >= 1                         */
+  int32_t first;    /* of them: its first ones, whatever their scores, >= 0                */
+  int32_t recent;   /* and its last ones, >= 0; first + recent <= keep                     */
+  int32_t shared;   /* 0: every KV head keeps its own entries; 1: all heads the same, by
+                       the sum of their scores (so that an entry still has one position)  */
+} still_paged_evict_config;
+
+/* Every sequence of more than `keep` entries is cut to that many inside its pages:
+ * the first and the recent ones, then those of the largest scores (ties: the
+ * earlier entry; NaN counts as minus infinity) move to the front in their order,
+ * with their bias and scores.  In 8 bits, a block of 16 new places takes the
+ * largest scale that its entries had, and their codes are rescaled to it (exact but
+ * for what falls below the smallest code).  Places behind the new length stay as
+ * they were.  An entry on an absent page counts as one of score minus infinity and
+ * moves as zeros; an absent place is not written.
+ *   kept      [n_seqs][shared ? 1 : H][keep] int32: the entries that stay, rising,
+ *             -1 behind them
+ *   new_lens  [n_seqs] int32: the lengths behind the call; may be seqs->lens
+ * The pages that the sequences name must be distinct. */
+still_status still_paged_evict(const still_paged_cache *cache, const still_paged_seqs *seqs,
+                               const still_paged_evict_config *cfg, float *scores, int32_t *kept, int32_t *new_lens,
+                               void *stream);
+still_status still_paged8_evict(const still_paged8_cache *cache, const still_paged_seqs *seqs,
+                                const still_paged_evict_config *cfg, float *scores, int32_t *kept, int32_t *new_lens,
+                                void *stream);
+
 /* Human-readable name of a status code (static string). */
 const char *still_status_string(int32_t status);
 

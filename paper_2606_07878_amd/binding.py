@@ -97,6 +97,11 @@ class still_paged_attend_config(ctypes.Structure):
                 ("scale", ctypes.c_float), ("rope_theta", ctypes.c_double), ("q_stride", ctypes.c_int64)]
 
 
+class still_paged_evict_config(ctypes.Structure):
+    _fields_ = [("keep", ctypes.c_int32), ("first", ctypes.c_int32), ("recent", ctypes.c_int32),
+                ("shared", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -164,6 +169,11 @@ def lib():
                              (L.still_paged_attend_lse, L.still_paged8_attend)):
             eight.argtypes = [cache8, *plain.argtypes[1:]]
             eight.restype = plain.restype
+        for kind, score, evict in ((cache, L.still_paged_score, L.still_paged_evict),
+                                   (cache8, L.still_paged8_score, L.still_paged8_evict)):
+            score.argtypes = [kind, seqs, ctypes.POINTER(still_paged_attend_config), *[ctypes.c_void_p] * 6]
+            evict.argtypes = [kind, seqs, ctypes.POINTER(still_paged_evict_config), *[ctypes.c_void_p] * 4]
+            score.restype = evict.restype = ctypes.c_int32
         L.still_status_string.argtypes = [ctypes.c_int32]
         L.still_status_string.restype = ctypes.c_char_p
         L.still_last_error.argtypes = []
@@ -326,6 +336,23 @@ def still_paged8_attend(cache: still_paged8_cache, seqs: still_paged_seqs, cfg: 
     return lib().still_paged8_attend(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(cfg), _ptr(q),
                                      _ptr(q_positions), _ptr(out), _ptr(lse), _ptr(workspace), workspace_bytes,
                                      _ptr(stream))
+
+
+def still_paged_score(cache, seqs: still_paged_seqs, cfg: still_paged_attend_config, q, q_positions, lse, known, scores,
+                      stream) -> int:
+    """Raw entry points still_paged_score and, for a still_paged8_cache, still_paged8_score (pointers or
+    tensors); returns the status code."""
+    call = lib().still_paged8_score if isinstance(cache, still_paged8_cache) else lib().still_paged_score
+    return call(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(cfg), _ptr(q), _ptr(q_positions), _ptr(lse),
+                _ptr(known), _ptr(scores), _ptr(stream))
+
+
+def still_paged_evict(cache, seqs: still_paged_seqs, cfg: still_paged_evict_config, scores, kept, new_lens, stream) -> int:
+    """Raw entry points still_paged_evict and, for a still_paged8_cache, still_paged8_evict (pointers or
+    tensors); returns the status code."""
+    call = lib().still_paged8_evict if isinstance(cache, still_paged8_cache) else lib().still_paged_evict
+    return call(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(cfg), _ptr(scores), _ptr(kept), _ptr(new_lens),
+                _ptr(stream))
 
 
 STILL_PAGED_WORKSPACE_BYTES = 17 << 20
@@ -875,11 +902,77 @@ def paged8_attend(q, k_pages, v_pages, k_scales, v_scales, table, lens, causal: 
     return _attend(torch, q, k_pages, cache, seqs, dev, causal, scale, q_positions, rope_theta, workspace, out, lse)
 
 
+# ---- what entries are worth, and eviction by it
+
+def _cache(torch, k_pages, v_pages, k_scales, v_scales, beta_pages, table, lens, dtype):
+    """_paged or, for pages of 8 bits, _paged8 with rows of this type."""
+    if k_pages.dtype is torch.float8_e4m3fn and k_scales is not None and v_scales is not None:
+        return _paged8(torch, k_pages, v_pages, k_scales, v_scales, beta_pages, table, lens, dtype)
+    if k_scales is not None or v_scales is not None:
+        _refuse(-1, f"scales given to pages of {k_pages.dtype}, or to keys or values alone")
+    return _paged(torch, k_pages, v_pages, beta_pages, table, lens)
+
+
+def paged_score(q, lse, k_pages, scores, table, lens, causal: bool = False, scale: float = 0.0, k_scales=None,
+                beta_pages=None, known=None, q_positions=None, rope_theta: float = 0.0) -> None:
+    """Add the attention weights of the newest tokens q, summed over the rows of each
+    KV head, to the entries' scores [n_pages, H, P] float32 on the current stream
+    (still_paged_score; still_paged8_score for pages of 8 bits, with ``k_scales``).
+    Arguments as in paged_attend, whose ``lse`` of the same rows the call takes.
+    Entries from ``known`` on (int32 [n_seqs]: the lengths at the call before) get the
+    weights in place of their slots' old scores."""
+    torch = _torch()
+    cache, seqs, dev = _cache(torch, k_pages, k_pages, k_scales, k_scales, beta_pages, table, lens, q.dtype)
+    cfg, pos = _queries(torch, q, k_pages, k_pages.dtype if k_scales is None else q.dtype, cache, seqs, dev, causal, scale,
+                        q_positions, rope_theta)
+    _want(lse, "lse", torch.float32, q.shape[:2], dev)
+    _want(scores, "scores", torch.float32, k_pages.shape[:3], dev)
+    if known is not None:
+        _want(known, "known", torch.int32, table.shape[:1], dev)
+    call = (_lib or lib()).still_paged_score if k_scales is None else (_lib or lib()).still_paged8_score
+    _on(torch, dev, call, ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(cfg), q.data_ptr(), pos, lse.data_ptr(),
+        None if known is None else known.data_ptr(), scores.data_ptr())
+
+
+def paged_evict(k_pages, v_pages, table, lens, scores, keep: int, first: int = 0, recent: int = 0, shared: bool = False,
+                k_scales=None, v_scales=None, beta_pages=None, kept=None, new_lens=None):
+    """Cut every sequence to its ``keep`` entries of largest score inside its pages, on
+    the current stream (still_paged_evict; still_paged8_evict with ``k_scales`` and
+    ``v_scales``): the ``first`` and the ``recent`` ones always stay.  Each KV head
+    keeps entries of its own or, with ``shared``, all the same by the sum of their
+    scores: then an entry still has one position, and compact_paged can take the
+    sequence with ``positions[kept]``.  Returns (kept [n_seqs, H or 1, keep] int32: the entries that
+    stay, rising, -1 behind them; new lengths [n_seqs] int32), into ``kept`` and
+    ``new_lens`` where given; ``new_lens`` may be ``lens``."""
+    torch = _torch()
+    cache, seqs, dev = _cache(torch, k_pages, v_pages, k_scales, v_scales, beta_pages, table, lens, torch.bfloat16)
+    keep, first, recent = int(keep), int(first), int(recent)
+    if max(abs(keep), abs(first), abs(recent)) >= 1 << 31:
+        _refuse(-2, f"{keep} entries to keep, {first} first and {recent} recent ones")
+    _want(scores, "scores", torch.float32, k_pages.shape[:3], dev)
+    shape = (seqs.n_seqs, 1 if shared else cache.n_kv_heads, keep)
+    if kept is None:
+        if keep < 1:
+            _refuse(-2, f"{keep} entries to keep")
+        kept = torch.empty(shape, dtype=torch.int32, device=k_pages.device)
+    else:
+        _want(kept, "kept", torch.int32, shape, dev)
+    if new_lens is None:
+        new_lens = torch.empty(seqs.n_seqs, dtype=torch.int32, device=k_pages.device)
+    else:
+        _want(new_lens, "new_lens", torch.int32, table.shape[:1], dev)
+    call = (_lib or lib()).still_paged_evict if k_scales is None else (_lib or lib()).still_paged8_evict
+    _on(torch, dev, call, ctypes.byref(cache), ctypes.byref(seqs),
+        ctypes.byref(still_paged_evict_config(keep, first, recent, bool(shared))), scores.data_ptr(), kept.data_ptr(),
+        new_lens.data_ptr())
+    return kept, new_lens
+
+
 def compact_paged(cfg: configs.CompactorConfig, weights: List[Dict[str, object]], k_pages: List, v_pages: List,
                   table, lens, seq: int, n: int, positions, rope_theta: float, t: int, start: int = 0,
                   end: Optional[int] = None, w_beta: Optional[List] = None, beta_pages: Optional[List] = None,
                   beta_max: float = 0.0, mass_alpha: float = 0.0, log_x: float = 0.0, rerotate: bool = True,
-                  drop_bias: bool = True):
+                  drop_bias: bool = True, scales: Optional[List] = None):
     """Compact entries [start, end) (default: all) of sequence ``seq``, which
     holds n entries, to t inside its pages, layer by layer (lists of L layers'
     weights and pages, one table): they are read out, compacted
@@ -895,14 +988,18 @@ def compact_paged(cfg: configs.CompactorConfig, weights: List[Dict[str, object]]
     entries [start, end) carry (those of an earlier compaction) is not taken in
     and is lost, each counting as one entry without bias.  To keep it, start
     behind them; ``drop_bias=False`` waits for the GPU and refuses a range that
-    carries any, before anything changes."""
+    carries any, before anything changes.
+    Pages of 8 bits pass ``scales``, a (k_scales, v_scales) for each layer; the
+    compactor then works in bfloat16."""
     torch = _torch()
     end = n if end is None else end
     if not (0 <= start < end <= n):
         _refuse(-1, f"subrange [{start}, {end}) outside [0, {n})")
     L = len(k_pages)
-    if L < 1 or len(v_pages) != L or len(weights) != L or any(x is not None and len(x) != L for x in (w_beta, beta_pages)):
+    if L < 1 or len(v_pages) != L or len(weights) != L or any(x is not None and len(x) != L for x in (w_beta, beta_pages, scales)):
         _refuse(-2, "lists of different numbers of layers")
+    if scales is not None and any(x is None or len(x) != 2 for x in scales):
+        _refuse(-1, "scales hold a (k_scales, v_scales) for each layer")
     if w_beta is not None and beta_pages is None:
         _refuse(-1, "w_beta given to a cache without beta")
     length = n - (end - start) + t
@@ -921,19 +1018,31 @@ def compact_paged(cfg: configs.CompactorConfig, weights: List[Dict[str, object]]
         if w_beta is not None and beta_pages[i] is None:
             _refuse(-1, f"layer {i}: w_beta given to a cache without beta")
     _want(positions, "positions", torch.float64, (n,), k_pages[0].get_device())
+    def read(i, count, at, bias, out=None):
+        if scales is None:
+            return paged_gather(k_pages[i], v_pages[i], table, lens, seq, count, at, beta_pages=bias, out=out)
+        return paged8_gather(k_pages[i], v_pages[i], *scales[i], table, lens, seq, count, at, beta_pages=bias, out=out)
+
+    def write(i, k, v, row, to, beta, bias):
+        if scales is None:
+            return paged_append(k, v, k_pages[i], v_pages[i], row, to, beta=beta, beta_pages=bias)
+        return paged8_append(k, v, k_pages[i], v_pages[i], *scales[i], row, to, beta=beta, beta_pages=bias)
+
     for i in range(L):   # (no entry read: the C call's checks, pointers among them)
-        paged_gather(k_pages[i], v_pages[i], table, lens, seq, 0, beta_pages=None if beta_pages is None else beta_pages[i])
+        read(i, 0, 0, None if beta_pages is None else beta_pages[i])
     with torch.cuda.device(k_pages[0].device):
-        return _compact_paged(cfg, weights, k_pages, v_pages, table, lens, seq, n, positions, rope_theta, t, start, end,
-                              w_beta, beta_pages, beta_max, mass_alpha, log_x, rerotate, drop_bias)
+        return _compact_paged(cfg, weights, read, write, k_pages[0].device,
+                              k_pages[0].dtype if scales is None else torch.bfloat16, L, table, lens, seq, n, positions,
+                              rope_theta, t, start, end, w_beta, beta_pages, beta_max, mass_alpha, log_x, rerotate, drop_bias)
 
 
-def _compact_paged(cfg, weights, k_pages, v_pages, table, lens, seq, n, positions, rope_theta, t, start, end, w_beta,
-                   beta_pages, beta_max, mass_alpha, log_x, rerotate, drop_bias):
-    """compact_paged behind its checks, with the pages' GPU current."""
+def _compact_paged(cfg, weights, read, write, dev, dtype, L, table, lens, seq, n, positions, rope_theta, t, start, end,
+                   w_beta, beta_pages, beta_max, mass_alpha, log_x, rerotate, drop_bias):
+    """compact_paged behind its checks, with the pages' GPU current: read(layer, n, start, bias pages, out)
+    and write(layer, k, v, table, lens, beta, bias pages) as dense rows of this type."""
     torch = _torch()
-    L, length = len(k_pages), n - (end - start) + t
-    dev, mode = k_pages[0].device, (configs.MODE_FP32 if k_pages[0].dtype == torch.float32 else configs.MODE_BF16)
+    length = n - (end - start) + t
+    mode = configs.MODE_FP32 if dtype == torch.float32 else configs.MODE_BF16
     row = table[seq:seq + 1]
     to = [torch.full((1,), x, dtype=torch.int32, device=dev) for x in (start + t, length)]
     inside = positions[start:end].contiguous()
@@ -943,8 +1052,7 @@ def _compact_paged(cfg, weights, k_pages, v_pages, table, lens, seq, n, position
     # pages change: a refusal, or memory that runs out, leaves them as they were
     new = []
     for i in range(L):
-        K, V, *carried = paged_gather(k_pages[i], v_pages[i], table, lens, seq, end - start, start,
-                                      beta_pages=None if drop_bias or beta_pages is None else beta_pages[i])
+        K, V, *carried = read(i, end - start, start, None if drop_bias or beta_pages is None else beta_pages[i])
         if carried and bool((carried[0] != 0).any()):
             _refuse(-5, f"layer {i}: entries [{start}, {end}) carry bias, which a compaction does not take in")
         if w_beta is None:
@@ -957,15 +1065,13 @@ def _compact_paged(cfg, weights, k_pages, v_pages, table, lens, seq, n, position
             beta = beta.t()
         new.append((Ck.transpose(0, 1), Cv.transpose(0, 1), beta))
     now_at = torch.cat([positions[:start], pq, positions[end:]])
-    rest = [torch.empty(cfg.n_kv_heads, n - end, cfg.head_dim, dtype=k_pages[0].dtype, device=dev) for _ in range(2)]
+    rest = [torch.empty(cfg.n_kv_heads, n - end, cfg.head_dim, dtype=dtype, device=dev) for _ in range(2)]
     if beta_pages is not None:
         rest.append(torch.empty(cfg.n_kv_heads, n - end, dtype=torch.float32, device=dev))
     for i, (Ck, Cv, beta) in enumerate(new):
         bp = None if beta_pages is None else beta_pages[i]
-        paged_gather(k_pages[i], v_pages[i], table, lens, seq, n - end, end, beta_pages=bp,
-                     out=rest[:2] if bp is None else rest)
-        paged_append(Ck, Cv, k_pages[i], v_pages[i], row, to[0], beta=beta, beta_pages=bp)
-        paged_append(rest[0].transpose(0, 1), rest[1].transpose(0, 1), k_pages[i], v_pages[i], row, to[1],
-                     beta=None if bp is None else rest[2].t(), beta_pages=bp)
+        read(i, n - end, end, bp, rest[:2] if bp is None else rest)
+        write(i, Ck, Cv, row, to[0], beta, bp)
+        write(i, rest[0].transpose(0, 1), rest[1].transpose(0, 1), row, to[1], None if bp is None else rest[2].t(), bp)
     lens[seq:seq + 1].fill_(length)
     return now_at

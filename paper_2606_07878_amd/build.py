@@ -1,9 +1,9 @@
 """Build libstill.so (HIP, gfx950) in-tree with hipcc.
 
-The library is seven translation units compiled in parallel (the C ABI and
+The library is eight translation units compiled in parallel (the C ABI and
 the consumer attention; the fp16 attention kernels; the per-layer launch sequence for bf16 I/O; the same
-for the fp32 validation mode; the backward pass; the paged cache; the paged cache in 8 bits) and linked into
-one shared object."""
+for the fp32 validation mode; the backward pass; the paged cache; the paged cache in 8 bits; scores and
+eviction) and linked into one shared object."""
 from __future__ import annotations
 
 import os
@@ -16,10 +16,12 @@ ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libstill.so")
 CSRC = os.path.join(PKG, "csrc")
 SOURCES = [os.path.join(CSRC, f) for f in ("still.hip", "xattn.hip", "layer_bf16.hip", "layer_fp32.hip",
-                                            "backward.hip", "paged.hip", "paged8.hip")]
+                                            "backward.hip", "paged.hip", "paged8.hip",
+                                            "evict.hip")]
 HEADERS = [os.path.join(CSRC, f) for f in ("common.hpp", "gemm.hpp", "attn.hpp", "misc.hpp", "kproj.hpp",
                                            "consumer.hpp", "refine.hpp", "refine64.hpp", "host.hpp",
-                                           "layer.hpp", "bwd.hpp", "paged.hpp", "paged_host.hpp", "paged8.hpp")] + [os.path.join(ROOT, "include", "still.h")]
+                                           "layer.hpp", "bwd.hpp", "paged.hpp", "paged_host.hpp", "paged8.hpp",
+                                           "evict.hpp")] + [os.path.join(ROOT, "include", "still.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

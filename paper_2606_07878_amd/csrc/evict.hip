@@ -1,0 +1,163 @@
+// evict.hip - C ABI (include/still.h) of the scores of a paged cache's entries and of
+// the eviction by them, for pages of every type.
+#include "paged_host.hpp"
+#include "evict.hpp"
+
+namespace still {
+
+static still_paged_cache plain_view(const still_paged8_cache* c) {
+  return {c->n_kv_heads, c->head_dim, c->page_size, c->n_pages, c->mode, c->k, c->v, c->beta};
+}
+
+// C8: keys of 8 bits, with scales ks.
+template <bool C8>
+static still_status paged_score_call(const still_paged_cache* cache, const float* ks, const still_paged_seqs* seqs,
+                                     const still_paged_attend_config* cfg, const void* q, const double* q_positions,
+                                     const float* lse, const int32_t* known, float* scores, void* stream) {
+  still_status s = check_attend(cache, cfg);
+  if (s != STILL_OK || (s = check_seqs(cache, seqs)) != STILL_OK) return s;
+  const long esize = cache->mode == STILL_MODE_FP32 ? 4 : 2;
+  const long q_row = (long)cache->n_kv_heads * cfg->group * cache->head_dim;
+  if (cfg->q_stride < 0 || cfg->q_stride * esize % 16)
+    return fail(STILL_E_SHAPE, "q_stride must be >= 0 and a multiple of 16 bytes");
+  if ((s = check_ptr(cache->k, "cache k", true)) != STILL_OK || (s = check_ptr(cache->beta, "cache beta", false)) != STILL_OK ||
+      (s = check_theta(cfg->rope_theta, q_positions)) != STILL_OK || (s = check_ptr(q, "q", true)) != STILL_OK ||
+      (s = check_ptr(scores, "scores", true)) != STILL_OK)
+    return s;
+  if (!lse || ((uintptr_t)lse & 3u)) return fail(STILL_E_INVAL, "lse is NULL or not 4-byte aligned");
+  if ((uintptr_t)known & 3u) return fail(STILL_E_INVAL, "known is not 4-byte aligned");
+  PagedScoreArgs a;
+  a.c = paged_args(cache, seqs);
+  a.c.ks = const_cast<float*>(ks);
+  a.q = (const char*)q;
+  a.q_ts = (cfg->q_stride ? cfg->q_stride : q_row) * esize;
+  a.lse = lse;
+  a.known = known;
+  a.scores = scores;
+  a.qpos = cfg->rope_theta > 0.0 ? q_positions : nullptr;
+  a.log2_theta = cfg->rope_theta > 0.0 ? std::log2(cfg->rope_theta) : 0.0;
+  a.group = cfg->group;
+  a.nq = cfg->n_queries;
+  a.causal = cfg->causal;
+  a.scale = cfg->scale != 0.f ? cfg->scale : 1.f / std::sqrt((float)cache->head_dim);
+  hipStream_t st = (hipStream_t)stream;
+  (void)hipGetLastError();
+  TIMED(STILL_K_ATTEND);
+  const long pairs = (long)cache->n_kv_heads * seqs->n_seqs, cap = (long)seqs->max_pages * cache->page_size;
+  const long z = std::min((cap + SCORE_CHUNK - 1) / SCORE_CHUNK, std::max(1L, 8192 / pairs));
+  paged_dispatch(cache, [&](auto it, auto d) {
+    using IT = decltype(it);
+    using CT = std::conditional_t<C8, e4m3, IT>;
+    constexpr int D = decltype(d)::value;
+    const dim3 grid(cache->n_kv_heads, seqs->n_seqs, z);
+    const bool rot = a.qpos != nullptr;
+    if (cfg->group * cfg->n_queries <= 16)
+      hipLaunchKernelGGL((paged_score_kernel<IT, D, 1, CT>), grid, dim3(256), (ScoreTile<IT, D, 1, CT>::lds_bytes(rot)), st, a);
+    else
+      hipLaunchKernelGGL((paged_score_kernel<IT, D, 2, CT>), grid, dim3(256), (ScoreTile<IT, D, 2, CT>::lds_bytes(rot)), st, a);
+  });
+  HIP_TRY(hipGetLastError());
+  return STILL_OK;
+}
+
+// ks, vs: scales of pages of 8 bits, else NULL.
+static still_status paged_evict_call(const still_paged_cache* cache, float* ks, float* vs, const still_paged_seqs* seqs,
+                                     const still_paged_evict_config* cfg, float* scores, int32_t* kept, int32_t* new_lens,
+                                     void* stream) {
+  still_status s;
+  if ((s = check_cache(cache)) != STILL_OK || (s = check_seqs(cache, seqs)) != STILL_OK) return s;
+  if (!cfg) return fail(STILL_E_INVAL, "paged evict config is NULL");
+  if (cfg->keep < 1 || cfg->first < 0 || cfg->recent < 0 || (long)cfg->first + cfg->recent > cfg->keep)
+    return fail(STILL_E_SHAPE, "keep %d must be >= 1 and hold first %d and recent %d", cfg->keep, cfg->first, cfg->recent);
+  if (cfg->shared != 0 && cfg->shared != 1) return fail(STILL_E_INVAL, "shared must be 0 or 1");
+  if ((s = check_pages(cache)) != STILL_OK || (s = check_ptr(scores, "scores", true)) != STILL_OK) return s;
+  if (!kept || !new_lens || ((uintptr_t)kept & 3u) || ((uintptr_t)new_lens & 3u))
+    return fail(STILL_E_INVAL, "kept or new_lens is NULL or not 4-byte aligned");
+  PagedEvictArgs a;
+  a.c = paged_args(cache, seqs);
+  a.c.ks = ks;
+  a.c.vs = vs;
+  a.scores = scores;
+  a.kept = kept;
+  a.new_lens = new_lens;
+  a.keep = cfg->keep;
+  a.first = cfg->first;
+  a.recent = cfg->recent;
+  a.shared = cfg->shared;
+  hipStream_t st = (hipStream_t)stream;
+  (void)hipGetLastError();
+  TIMED(STILL_K_OTHER);
+  const long cap = (long)seqs->max_pages * cache->page_size;
+  const int H = cache->n_kv_heads, n_seqs = seqs->n_seqs;
+  const dim3 lists(cfg->shared ? 1 : H, n_seqs);
+  if (cap <= 4096) hipLaunchKernelGGL((paged_select_kernel<256>), lists, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((paged_select_kernel<1024>), lists, dim3(1024), 0, st, a);
+  HIP_TRY(hipGetLastError());
+  const bool few = (long)H * n_seqs <= 64;
+  const int pieces = ks || !few ? 1 : 4;
+  const dim3 grid(H, n_seqs, 2 * pieces + 1), threads(few ? 1024 : 256);
+  auto move = [&](auto rowb, auto c8) {
+    hipLaunchKernelGGL((paged_move_kernel<decltype(rowb)::value, decltype(c8)::value>), grid, threads, 0, st, a, pieces);
+  };
+  using No = std::false_type;
+  using Yes = std::true_type;
+  const int rowb = cache->head_dim * (ks ? 1 : cache->mode == STILL_MODE_FP32 ? 4 : 2);
+  if (ks) {
+    switch (rowb) {
+      case 64: move(std::integral_constant<int, 64>(), Yes()); break;
+      case 128: move(std::integral_constant<int, 128>(), Yes()); break;
+      default: move(std::integral_constant<int, 256>(), Yes());
+    }
+  } else {
+    switch (rowb) {
+      case 128: move(std::integral_constant<int, 128>(), No()); break;
+      case 256: move(std::integral_constant<int, 256>(), No()); break;
+      case 512: move(std::integral_constant<int, 512>(), No()); break;
+      default: move(std::integral_constant<int, 1024>(), No());
+    }
+  }
+  HIP_TRY(hipGetLastError());
+  return STILL_OK;
+}
+
+}  // namespace still
+
+using namespace still;
+
+extern "C" {
+
+still_status still_paged_score(const still_paged_cache* cache, const still_paged_seqs* seqs,
+                               const still_paged_attend_config* cfg, const void* q, const double* q_positions,
+                               const float* lse, const int32_t* known, float* scores, void* stream) {
+  return paged_score_call<false>(cache, nullptr, seqs, cfg, q, q_positions, lse, known, scores, stream);
+}
+
+still_status still_paged8_score(const still_paged8_cache* cache, const still_paged_seqs* seqs,
+                                const still_paged_attend_config* cfg, const void* q, const double* q_positions,
+                                const float* lse, const int32_t* known, float* scores, void* stream) {
+  if (!cache) return fail(STILL_E_INVAL, "paged cache is NULL");
+  const still_paged_cache c = plain_view(cache);
+  still_status s;
+  if ((s = check_attend(&c, cfg)) != STILL_OK || (s = check_ptr(cache->k_scale, "cache k_scale", true)) != STILL_OK) return s;
+  return paged_score_call<true>(&c, cache->k_scale, seqs, cfg, q, q_positions, lse, known, scores, stream);
+}
+
+still_status still_paged_evict(const still_paged_cache* cache, const still_paged_seqs* seqs,
+                               const still_paged_evict_config* cfg, float* scores, int32_t* kept, int32_t* new_lens,
+                               void* stream) {
+  return paged_evict_call(cache, nullptr, nullptr, seqs, cfg, scores, kept, new_lens, stream);
+}
+
+still_status still_paged8_evict(const still_paged8_cache* cache, const still_paged_seqs* seqs,
+                                const still_paged_evict_config* cfg, float* scores, int32_t* kept, int32_t* new_lens,
+                                void* stream) {
+  if (!cache) return fail(STILL_E_INVAL, "paged cache is NULL");
+  const still_paged_cache c = plain_view(cache);
+  still_status s;
+  if ((s = check_cache(&c)) != STILL_OK || (s = check_ptr(cache->k_scale, "cache k_scale", true)) != STILL_OK ||
+      (s = check_ptr(cache->v_scale, "cache v_scale", true)) != STILL_OK)
+    return s;
+  return paged_evict_call(&c, cache->k_scale, cache->v_scale, seqs, cfg, scores, kept, new_lens, stream);
+}
+
+}  // extern "C"

@@ -155,3 +155,71 @@ def test_binding_refuses_what_does_not_fit():
     _raises(-3, binding.paged8_append, rows.half(), rows.half(), *good)
     _raises(-3, binding.paged8_gather, *good, 0, 5, dtype=torch.float16)
     _raises(-3, binding.paged8_attend, c.rows(2, heads=4).double(), *good)
+
+
+# ---- scores and eviction -----------------------------------------------------
+
+def _ecfg(**kw):
+    base = dict(keep=64, first=4, recent=16, shared=0)
+    base.update(kw)
+    return binding.still_paged_evict_config(**base)
+
+
+def _plain(**kw):
+    base = dict(n_kv_heads=8, head_dim=128, page_size=16, n_pages=100, mode=configs.MODE_BF16, k=FAKE, v=FAKE, beta=None)
+    base.update(kw)
+    return binding.still_paged_cache(**base)
+
+
+def _score(cache=None, seqs=None, cfg=None, q=FAKE, pos=None, lse=FAKE, known=None, scores=FAKE):
+    return binding.still_paged_score(cache or _cache8(), seqs or _seqs(), cfg or _acfg(), q, pos, lse, known, scores, None)
+
+
+def _evict(cache=None, seqs=None, cfg=None, scores=FAKE, kept=FAKE, new_lens=FAKE):
+    return binding.still_paged_evict(cache or _cache8(), seqs or _seqs(), cfg or _ecfg(), scores, kept, new_lens, None)
+
+
+@pytest.mark.parametrize("make", [_cache8, _plain])
+def test_score_and_evict_refuse(make):
+    for kw, status in BAD_CACHE:
+        if "v" not in kw:
+            assert _score(cache=make(**kw)) == status
+        assert _evict(cache=make(**kw)) == status
+    for kw, status in BAD_SEQS:
+        assert _score(cache=make(), seqs=_seqs(**kw)) == status
+        assert _evict(cache=make(), seqs=_seqs(**kw)) == status
+    for kw in (dict(q=None), dict(lse=None), dict(lse=FAKE + 2), dict(known=FAKE + 1), dict(scores=None), dict(scores=FAKE + 4)):
+        assert _score(cache=make(), **kw) == -1
+    for kw, status in ((dict(group=33), -5), (dict(n_queries=0), -2), (dict(causal=2), -1), (dict(scale=-1.0), -1),
+                       (dict(rope_theta=1e6), -1), (dict(q_stride=4), -2)):
+        assert _score(cache=make(), cfg=_acfg(**kw)) == status
+    for kw in (dict(scores=None), dict(scores=FAKE + 8), dict(kept=None), dict(kept=FAKE + 2), dict(new_lens=None), dict(new_lens=FAKE + 3)):
+        assert _evict(cache=make(), **kw) == -1
+    for kw, status in ((dict(keep=0), -2), (dict(keep=-5), -2), (dict(first=-1), -2), (dict(recent=-1), -2),
+                       (dict(first=50, recent=15), -2), (dict(first=2 ** 31 - 1, recent=2 ** 31 - 1), -2), (dict(shared=2), -1)):
+        assert _evict(cache=make(), cfg=_ecfg(**kw)) == status
+
+
+def test_score_and_evict_null_structs_and_scales():
+    assert _score(cache=_cache8(k_scale=None)) == -1 and _evict(cache=_cache8(v_scale=FAKE + 4)) == -1
+    lib, s = binding.lib(), ctypes.byref(_seqs())
+    for c in (None, ctypes.byref(_cache8())):
+        assert lib.still_paged8_evict(c, s if c is None else None, ctypes.byref(_ecfg()), FAKE, FAKE, FAKE, None) == -1
+        assert lib.still_paged8_score(c, s if c is None else None, ctypes.byref(_acfg()), FAKE, None, FAKE, None, FAKE, None) == -1
+    assert lib.still_paged8_evict(ctypes.byref(_cache8()), s, None, FAKE, FAKE, FAKE, None) == -1
+    assert lib.still_paged_evict(None, s, ctypes.byref(_ecfg()), FAKE, FAKE, FAKE, None) == -1
+    assert lib.still_paged_score(None, s, ctypes.byref(_acfg()), FAKE, None, FAKE, None, FAKE, None) == -1
+
+
+def test_binding_refuses_scores_that_do_not_fit():
+    c = Paged8(4, [40, 7], 2, 64, 16)
+    k, v, ks, vs, table, lens = c.pages()
+    q, lse = c.rows(2, heads=4), torch.zeros(2, 4)
+    _raises(-1, binding.paged_score, q, lse, k, c.scores, table, lens, k_scales=ks)       # CPU tensors: a GPU is needed
+    _raises(-3, binding.paged_score, q, lse, k, c.scores, table, lens)
+    _raises(-1, binding.paged_score, q, lse, k.bfloat16(), c.scores, table, lens, k_scales=ks)
+    _raises(-1, binding.paged_evict, k, v, table, lens, c.scores, 8, k_scales=ks, v_scales=vs)
+    _raises(-1, binding.paged_evict, k, v, table, lens, c.scores, 8, k_scales=ks)
+    _raises(-1, binding.paged_evict, k.float(), v.float(), table, lens, c.scores, 8)
+    _raises(-1, binding.compact_paged, configs.get_workload(1).cfg, [None], [k], [v], table, lens, 0, 40, None, 1e6, 8,
+            scales=[None])
