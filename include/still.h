@@ -503,13 +503,18 @@ typedef struct {
  *   kept      [n_seqs][shared ? 1 : H][keep] int32: the entries that stay, rising,
  *             -1 behind them
  *   new_lens  [n_seqs] int32: the lengths behind the call; may be seqs->lens
+ *   workspace still_paged_evict_workspace_size bytes (16-byte aligned; NULL where that is 0), for
+ *             caches of 8 bits too (of the same dimensions); at most 64 MiB, nothing for tables
+ *             of up to 8192 entries
  * The pages that the sequences name must be distinct. */
+size_t still_paged_evict_workspace_size(const still_paged_cache *cache, const still_paged_seqs *seqs,
+                                        const still_paged_evict_config *cfg);
 still_status still_paged_evict(const still_paged_cache *cache, const still_paged_seqs *seqs,
                                const still_paged_evict_config *cfg, float *scores, int32_t *kept, int32_t *new_lens,
-                               void *stream);
+                               void *workspace, size_t workspace_bytes, void *stream);
 still_status still_paged8_evict(const still_paged8_cache *cache, const still_paged_seqs *seqs,
                                 const still_paged_evict_config *cfg, float *scores, int32_t *kept, int32_t *new_lens,
-                                void *stream);
+                                void *workspace, size_t workspace_bytes, void *stream);
 
 /* Human-readable name of a status code (static string). */
 const char *still_status_string(int32_t status);

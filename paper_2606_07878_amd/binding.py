@@ -172,8 +172,11 @@ def lib():
         for kind, score, evict in ((cache, L.still_paged_score, L.still_paged_evict),
                                    (cache8, L.still_paged8_score, L.still_paged8_evict)):
             score.argtypes = [kind, seqs, ctypes.POINTER(still_paged_attend_config), *[ctypes.c_void_p] * 6]
-            evict.argtypes = [kind, seqs, ctypes.POINTER(still_paged_evict_config), *[ctypes.c_void_p] * 4]
+            evict.argtypes = [kind, seqs, ctypes.POINTER(still_paged_evict_config), *[ctypes.c_void_p] * 4, ctypes.c_size_t,
+                              ctypes.c_void_p]
             score.restype = evict.restype = ctypes.c_int32
+        L.still_paged_evict_workspace_size.argtypes = [cache, seqs, ctypes.POINTER(still_paged_evict_config)]
+        L.still_paged_evict_workspace_size.restype = ctypes.c_size_t
         L.still_status_string.argtypes = [ctypes.c_int32]
         L.still_status_string.restype = ctypes.c_char_p
         L.still_last_error.argtypes = []
@@ -347,12 +350,17 @@ def still_paged_score(cache, seqs: still_paged_seqs, cfg: still_paged_attend_con
                 _ptr(known), _ptr(scores), _ptr(stream))
 
 
-def still_paged_evict(cache, seqs: still_paged_seqs, cfg: still_paged_evict_config, scores, kept, new_lens, stream) -> int:
+def still_paged_evict_workspace_size(cache: still_paged_cache, seqs: still_paged_seqs, cfg: still_paged_evict_config) -> int:
+    return int(lib().still_paged_evict_workspace_size(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(cfg)))
+
+
+def still_paged_evict(cache, seqs: still_paged_seqs, cfg: still_paged_evict_config, scores, kept, new_lens, workspace,
+                      workspace_bytes: int, stream) -> int:
     """Raw entry points still_paged_evict and, for a still_paged8_cache, still_paged8_evict (pointers or
     tensors); returns the status code."""
     call = lib().still_paged8_evict if isinstance(cache, still_paged8_cache) else lib().still_paged_evict
     return call(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(cfg), _ptr(scores), _ptr(kept), _ptr(new_lens),
-                _ptr(stream))
+                _ptr(workspace), workspace_bytes, _ptr(stream))
 
 
 STILL_PAGED_WORKSPACE_BYTES = 17 << 20
@@ -935,7 +943,7 @@ def paged_score(q, lse, k_pages, scores, table, lens, causal: bool = False, scal
 
 
 def paged_evict(k_pages, v_pages, table, lens, scores, keep: int, first: int = 0, recent: int = 0, shared: bool = False,
-                k_scales=None, v_scales=None, beta_pages=None, kept=None, new_lens=None):
+                k_scales=None, v_scales=None, beta_pages=None, kept=None, new_lens=None, workspace=None):
     """Cut every sequence to its ``keep`` entries of largest score inside its pages, on
     the current stream (still_paged_evict; still_paged8_evict with ``k_scales`` and
     ``v_scales``): the ``first`` and the ``recent`` ones always stay.  Each KV head
@@ -943,7 +951,8 @@ def paged_evict(k_pages, v_pages, table, lens, scores, keep: int, first: int = 0
     scores: then an entry still has one position, and compact_paged can take the
     sequence with ``positions[kept]``.  Returns (kept [n_seqs, H or 1, keep] int32: the entries that
     stay, rising, -1 behind them; new lengths [n_seqs] int32), into ``kept`` and
-    ``new_lens`` where given; ``new_lens`` may be ``lens``."""
+    ``new_lens`` where given; ``new_lens`` may be ``lens``.  ``workspace`` (64 MiB serve every
+    call, none is needed for tables of up to 8192 entries) may be given too."""
     torch = _torch()
     cache, seqs, dev = _cache(torch, k_pages, v_pages, k_scales, v_scales, beta_pages, table, lens, torch.bfloat16)
     keep, first, recent = int(keep), int(first), int(recent)
@@ -961,10 +970,20 @@ def paged_evict(k_pages, v_pages, table, lens, scores, keep: int, first: int = 0
         new_lens = torch.empty(seqs.n_seqs, dtype=torch.int32, device=k_pages.device)
     else:
         _want(new_lens, "new_lens", torch.int32, table.shape[:1], dev)
+    if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
+        _refuse(-1, f"workspace is on {workspace.device}, the pages on {k_pages.device}, or it is not contiguous")
+    cfg = still_paged_evict_config(keep, first, recent, bool(shared))
+    need, room = 0, 0 if workspace is None else workspace.numel() * workspace.element_size()
+    if seqs.max_pages * k_pages.shape[2] > 8192:
+        plain = cache if k_scales is None else still_paged_cache(cache.n_kv_heads, cache.head_dim, cache.page_size,
+                                                                        cache.n_pages, cache.mode, cache.k, cache.v)
+        need = still_paged_evict_workspace_size(plain, seqs, cfg)
+    if room < need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=k_pages.device)
+        room = need
     call = (_lib or lib()).still_paged_evict if k_scales is None else (_lib or lib()).still_paged8_evict
-    _on(torch, dev, call, ctypes.byref(cache), ctypes.byref(seqs),
-        ctypes.byref(still_paged_evict_config(keep, first, recent, bool(shared))), scores.data_ptr(), kept.data_ptr(),
-        new_lens.data_ptr())
+    _on(torch, dev, call, ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(cfg), scores.data_ptr(), kept.data_ptr(),
+        new_lens.data_ptr(), _ptr(workspace), room)
     return kept, new_lens
 
 

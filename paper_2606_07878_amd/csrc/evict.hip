@@ -52,27 +52,45 @@ static still_status paged_score_call(const still_paged_cache* cache, const float
     const dim3 grid(cache->n_kv_heads, seqs->n_seqs, z);
     const bool rot = a.qpos != nullptr;
     if (cfg->group * cfg->n_queries <= 16)
-      hipLaunchKernelGGL((paged_score_kernel<IT, D, 1, CT>), grid, dim3(256), (ScoreTile<IT, D, 1, CT>::lds_bytes(rot)), st, a);
+      hipLaunchKernelGGL((paged_score_kernel<IT, D, 1, CT>), grid, dim3(256), (ScoreTile<IT, D, 1, CT>::lds_bytes(rot, cfg->n_queries)), st, a);
     else
-      hipLaunchKernelGGL((paged_score_kernel<IT, D, 2, CT>), grid, dim3(256), (ScoreTile<IT, D, 2, CT>::lds_bytes(rot)), st, a);
+      hipLaunchKernelGGL((paged_score_kernel<IT, D, 2, CT>), grid, dim3(256), (ScoreTile<IT, D, 2, CT>::lds_bytes(rot, cfg->n_queries)), st, a);
   });
   HIP_TRY(hipGetLastError());
   return STILL_OK;
 }
 
-// ks, vs: scales of pages of 8 bits, else NULL.
-static still_status paged_evict_call(const still_paged_cache* cache, float* ks, float* vs, const still_paged_seqs* seqs,
-                                     const still_paged_evict_config* cfg, float* scores, int32_t* kept, int32_t* new_lens,
-                                     void* stream) {
+static still_status check_evict(const still_paged_cache* cache, const still_paged_seqs* seqs, const still_paged_evict_config* cfg) {
   still_status s;
   if ((s = check_cache(cache)) != STILL_OK || (s = check_seqs(cache, seqs)) != STILL_OK) return s;
   if (!cfg) return fail(STILL_E_INVAL, "paged evict config is NULL");
   if (cfg->keep < 1 || cfg->first < 0 || cfg->recent < 0 || (long)cfg->first + cfg->recent > cfg->keep)
     return fail(STILL_E_SHAPE, "keep %d must be >= 1 and hold first %d and recent %d", cfg->keep, cfg->first, cfg->recent);
   if (cfg->shared != 0 && cfg->shared != 1) return fail(STILL_E_INVAL, "shared must be 0 or 1");
+  return STILL_OK;
+}
+
+// Keys of a list in the workspace, where they are formed ahead; 0 where a list's workgroup
+// forms its own.
+static long evict_keys(const still_paged_cache* c, const still_paged_seqs* q, const still_paged_evict_config* f) {
+  const long cap = (long)q->max_pages * c->page_size, lists = (long)q->n_seqs * (f->shared ? 1 : c->n_kv_heads);
+  return cap > 8192 && lists <= 64 && lists * cap <= 1L << 24 ? cap : 0;
+}
+
+// ks, vs: scales of pages of 8 bits, else NULL.
+static still_status paged_evict_call(const still_paged_cache* cache, float* ks, float* vs, const still_paged_seqs* seqs,
+                                     const still_paged_evict_config* cfg, float* scores, int32_t* kept, int32_t* new_lens,
+                                     void* workspace, size_t workspace_bytes, void* stream) {
+  still_status s = check_evict(cache, seqs, cfg);
+  if (s != STILL_OK) return s;
   if ((s = check_pages(cache)) != STILL_OK || (s = check_ptr(scores, "scores", true)) != STILL_OK) return s;
   if (!kept || !new_lens || ((uintptr_t)kept & 3u) || ((uintptr_t)new_lens & 3u))
     return fail(STILL_E_INVAL, "kept or new_lens is NULL or not 4-byte aligned");
+  const int lists = seqs->n_seqs * (cfg->shared ? 1 : cache->n_kv_heads);
+  const size_t need = (size_t)lists * evict_keys(cache, seqs, cfg) * sizeof(uint32_t);
+  if (need && !workspace) return fail(STILL_E_WORKSPACE, "workspace is NULL");
+  if (need && (s = check_ptr(workspace, "workspace", true)) != STILL_OK) return s;
+  if (workspace_bytes < need) return fail(STILL_E_WORKSPACE, "workspace of %zu bytes, need %zu", workspace_bytes, need);
   PagedEvictArgs a;
   a.c = paged_args(cache, seqs);
   a.c.ks = ks;
@@ -89,9 +107,20 @@ static still_status paged_evict_call(const still_paged_cache* cache, float* ks, 
   TIMED(STILL_K_OTHER);
   const long cap = (long)seqs->max_pages * cache->page_size;
   const int H = cache->n_kv_heads, n_seqs = seqs->n_seqs;
-  const dim3 lists(cfg->shared ? 1 : H, n_seqs);
-  if (cap <= 4096) hipLaunchKernelGGL((paged_select_kernel<256>), lists, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((paged_select_kernel<1024>), lists, dim3(1024), 0, st, a);
+  const int per_seq = cfg->shared ? 1 : H;
+  const dim3 grid_of(per_seq, n_seqs);
+  a.keys = (uint32_t*)workspace;
+  a.kstride = evict_keys(cache, seqs, cfg);
+  if (a.kstride) {
+    hipLaunchKernelGGL(paged_keys_kernel, dim3(std::min(512L, (cap + 1023) / 1024), per_seq, n_seqs), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((paged_select_kernel<1024, 64, true>), grid_of, dim3(1024), 0, st, a);
+  } else if (cap <= 2048) {
+    hipLaunchKernelGGL((paged_select_kernel<256, 8, false>), grid_of, dim3(256), 0, st, a);
+  } else if (cap <= 8192) {
+    hipLaunchKernelGGL((paged_select_kernel<512, 16, false>), grid_of, dim3(512), 0, st, a);
+  } else {
+    hipLaunchKernelGGL((paged_select_kernel<1024, 32, false>), grid_of, dim3(1024), 0, st, a);
+  }
   HIP_TRY(hipGetLastError());
   const bool few = (long)H * n_seqs <= 64;
   const int pieces = ks || !few ? 1 : 4;
@@ -144,20 +173,31 @@ still_status still_paged8_score(const still_paged8_cache* cache, const still_pag
 
 still_status still_paged_evict(const still_paged_cache* cache, const still_paged_seqs* seqs,
                                const still_paged_evict_config* cfg, float* scores, int32_t* kept, int32_t* new_lens,
-                               void* stream) {
-  return paged_evict_call(cache, nullptr, nullptr, seqs, cfg, scores, kept, new_lens, stream);
+                               void* workspace, size_t workspace_bytes, void* stream) {
+  return paged_evict_call(cache, nullptr, nullptr, seqs, cfg, scores, kept, new_lens, workspace, workspace_bytes, stream);
+}
+
+size_t still_paged_evict_workspace_size(const still_paged_cache* cache, const still_paged_seqs* seqs,
+                                        const still_paged_evict_config* cfg) {
+  const std::string keep = g_last_error;
+  if (check_evict(cache, seqs, cfg) != STILL_OK) {
+    g_last_error = keep;
+    return 0;
+  }
+  return (size_t)seqs->n_seqs * (cfg->shared ? 1 : cache->n_kv_heads) * evict_keys(cache, seqs, cfg) * sizeof(uint32_t);
 }
 
 still_status still_paged8_evict(const still_paged8_cache* cache, const still_paged_seqs* seqs,
                                 const still_paged_evict_config* cfg, float* scores, int32_t* kept, int32_t* new_lens,
-                                void* stream) {
+                                void* workspace, size_t workspace_bytes, void* stream) {
   if (!cache) return fail(STILL_E_INVAL, "paged cache is NULL");
   const still_paged_cache c = plain_view(cache);
   still_status s;
   if ((s = check_cache(&c)) != STILL_OK || (s = check_ptr(cache->k_scale, "cache k_scale", true)) != STILL_OK ||
       (s = check_ptr(cache->v_scale, "cache v_scale", true)) != STILL_OK)
     return s;
-  return paged_evict_call(&c, cache->k_scale, cache->v_scale, seqs, cfg, scores, kept, new_lens, stream);
+  return paged_evict_call(&c, cache->k_scale, cache->v_scale, seqs, cfg, scores, kept, new_lens, workspace,
+                          workspace_bytes, stream);
 }
 
 }  // extern "C"

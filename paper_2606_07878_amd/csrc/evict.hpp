@@ -34,10 +34,10 @@ template <class IT, int D, int NR, class CT>
 struct ScoreTile {
   static constexpr bool C8 = sizeof(CT) == 1, B16 = C8 || sizeof(IT) == 2;
   static constexpr int ROWB = D * (int)sizeof(CT), NP = ROWB / 64;
-  static constexpr int NKT = std::max(1, std::min(8, 1024 / ROWB));   // tiles of a wave at a time: 16 KB of keys
+  static constexpr int NKT = std::max(1, std::min(4, 512 / ROWB));   // tiles of a wave at a time: 8 KB of keys
   static constexpr int QROW = D * (B16 ? 2 : 4) + 16, QPART = 16 * NR * QROW;
   static __host__ __device__ bool split(bool rot) { return B16 && (rot || sizeof(IT) == 4); }
-  static __host__ __device__ int lds_bytes(bool rot) { return (split(rot) ? 3 : 1) * QPART; }
+  static __host__ __device__ int lds_bytes(bool rot, int nq) { return (split(rot) ? 3 : 1) * QPART + (rot ? nq * D / 2 * (int)sizeof(float2) : 0); }
 };
 
 template <class IT, int D, int NR, class CT>
@@ -47,6 +47,7 @@ __global__ __launch_bounds__(256) void paged_score_kernel(PagedScoreArgs a) {
   constexpr int NKT = TL::NKT, NP = TL::NP, ROWB = TL::ROWB, QROW = TL::QROW, HD = D / 2, STEP = 16 * NKT;
   extern __shared__ float4 score_smem[];
   char* qs = (char*)score_smem;                  // [16 NR][QROW], where split three parts of that
+  float2* cs = (float2*)(qs + (TL::split(a.qpos != nullptr) ? 3 : 1) * TL::QPART);   // [nq][D / 2]
   __shared__ float row_lse[16 * NR];             // plus infinity: a row that takes no part
   const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), l = lane & 15, lg = lane >> 4;
   const int h = blockIdx.x, s = blockIdx.y, R = a.group * a.nq, Hq = a.c.H * a.group;
@@ -54,6 +55,57 @@ __global__ __launch_bounds__(256) void paged_score_kernel(PagedScoreArgs a) {
   if ((long)blockIdx.z * SCORE_CHUNK >= len) return;
   const int known = a.known ? a.known[s] : len;
   const bool rot = a.qpos != nullptr;
+  // ---- this wave's units of STEP entries, in rising order: page numbers a unit ahead of the keys
+  constexpr int UPC = SCORE_CHUNK / (4 * STEP);   // of a chunk
+  auto start_of = [&](int v) { return ((long)blockIdx.z + (long)(v / UPC) * gridDim.z) * SCORE_CHUNK + (v % UPC * 4 + w) * STEP; };
+  struct Unit {
+    long j0;
+    int p[NKT];
+  };
+  auto lookup = [&](int v) {
+    Unit u;
+    u.j0 = start_of(v);
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt)
+      u.p[kt] = a.c.table[s * a.c.tstride + min((u.j0 + 16 * kt) >> a.c.lp, (long)a.c.max_pages - 1)];
+    return u;
+  };
+  int nv[NKT];      // valid entries of each tile
+  long row[NKT];    // rows of the pages in front of it
+  u32x4 kp[NKT][NP];
+  f32x4 bias[NKT], old[NKT];
+  float ks[C8 ? NKT : 1];
+  auto load = [&](const Unit& u) {
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt) {
+      const long j = u.j0 + 16 * kt;
+      const int p = uniform(u.p[kt]);
+      const bool ok = j < len && (unsigned)p < (unsigned)a.c.n_pages;
+      nv[kt] = ok ? (int)min(16L, len - j) : 0;
+      row[kt] = (((long)(ok ? p : 0) * a.c.H + h) << a.c.lp) + (ok ? (int)j & ((1 << a.c.lp) - 1) : 0);
+    }
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt) {
+      const auto r = paged_rows(a.c.k + row[kt] * ROWB, nv[kt] * ROWB);
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+        kp[kt][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, l * ROWB + lg * 16 + 64 * i, 0, 0));
+      const int few = nv[kt] > 0 ? 64 : 0;
+      bias[kt] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                               paged_rows(a.c.beta + row[kt], a.c.beta ? few : 0), 16 * lg, 0, 0));
+      old[kt] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(paged_rows(a.scores + row[kt], few), 16 * lg, 0, 0));
+      if constexpr (C8)
+        ks[kt] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(
+                                               paged_rows(a.c.ks + row[kt] / PAGED_BLOCK, nv[kt] > 0 ? 4 : 0), 0, 0, 0));
+    }
+  };
+  Unit cur = lookup(0);
+  if (rot) {   // (cos, sin) of the queries' angles
+    for (int e = tid; e < a.nq * HD; e += 256)
+      cs[e] = rope_cs(a.qpos[(long)s * a.nq + e / HD], exp2(a.log2_theta * (-2.0 * (e % HD) / D)));
+    __syncthreads();
+  }
+  load(cur);
   // ---- the query rows into LDS: row g * nq + i is query i of head h * group + g
   constexpr int EPI = TL::B16 ? 8 : 4, NV = EPI * (int)sizeof(IT) / 16, HP = HD / EPI;
   for (int e = tid; e < 16 * NR * HP; e += 256) {
@@ -74,10 +126,10 @@ __global__ __launch_bounds__(256) void paged_score_kernel(PagedScoreArgs a) {
         unpack16<IT>(y[1][u], *(float(*)[EPI / NV])(x1 + u * (EPI / NV)));
       }
       if (rot) {
-        const double pos = a.qpos[token];
+        const float2* turn = cs + (i - g * a.nq) * HD + p * EPI;
 #pragma unroll
         for (int u = 0; u < EPI; ++u) {
-          const float2 c = rope_cs(pos, exp2(a.log2_theta * (-2.0 * (p * EPI + u) / D)));
+          const float2 c = turn[u];
           const float z = x0[u] * c.x - x1[u] * c.y;
           x1[u] = x1[u] * c.x + x0[u] * c.y;
           x0[u] = z;
@@ -118,35 +170,11 @@ __global__ __launch_bounds__(256) void paged_score_kernel(PagedScoreArgs a) {
     ref[rt] = row_lse[r];
     lim[rt] = ref[rt] == INFINITY ? -1 : a.causal ? len - a.nq + r % a.nq : len - 1;
   }
-  for (long z = (long)blockIdx.z * SCORE_CHUNK; z < len; z += (long)gridDim.z * SCORE_CHUNK)
-    for (int j0 = (int)z + w * STEP; j0 < min((long)len, z + SCORE_CHUNK); j0 += 4 * STEP) {
-      int nv[NKT];      // valid entries of each tile
-      long row[NKT];    // rows of the pages in front of it
-      u32x4 kp[NKT][NP];
-      f32x4 bias[NKT], old[NKT];
-      float ks[C8 ? NKT : 1];
-#pragma unroll
-      for (int kt = 0; kt < NKT; ++kt) {
-        const int j = j0 + 16 * kt;
-        const int p = uniform(a.c.table[s * a.c.tstride + min(j >> a.c.lp, a.c.max_pages - 1)]);
-        const bool ok = j < len && (unsigned)p < (unsigned)a.c.n_pages;
-        nv[kt] = ok ? min(16, len - j) : 0;
-        row[kt] = (((long)(ok ? p : 0) * a.c.H + h) << a.c.lp) + (ok ? j & ((1 << a.c.lp) - 1) : 0);
-      }
-#pragma unroll
-      for (int kt = 0; kt < NKT; ++kt) {
-        const auto r = paged_rows(a.c.k + row[kt] * ROWB, nv[kt] * ROWB);
-#pragma unroll
-        for (int i = 0; i < NP; ++i)
-          kp[kt][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, l * ROWB + lg * 16 + 64 * i, 0, 0));
-        const int few = nv[kt] > 0 ? 64 : 0;
-        bias[kt] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                                                 paged_rows(a.c.beta + row[kt], a.c.beta ? few : 0), 16 * lg, 0, 0));
-        old[kt] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(paged_rows(a.scores + row[kt], few), 16 * lg, 0, 0));
-        if constexpr (C8)
-          ks[kt] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(
-                                                 paged_rows(a.c.ks + row[kt] / PAGED_BLOCK, nv[kt] > 0 ? 4 : 0), 0, 0, 0));
-      }
+  const long open = a.causal ? (long)len - a.nq : len - 1L;   // every row sees the entries up to this one
+  for (int v = 0; cur.j0 < len; ++v) {
+      const long j0 = cur.j0;
+      const Unit next = lookup(v + 1);
+      __builtin_amdgcn_sched_barrier(0);
       f32x4 x[NR][NKT];
 #pragma unroll
       for (int rt = 0; rt < NR; ++rt)
@@ -190,45 +218,71 @@ __global__ __launch_bounds__(256) void paged_score_kernel(PagedScoreArgs a) {
             product(2, kv, at);
           }
         }
+      // the next unit's keys are on their way while this one's weights are summed
+      f32x4 bc[NKT], oc[NKT];
+      float sc[NKT];
+      int n[NKT];
+      float* to[NKT];
 #pragma unroll
       for (int kt = 0; kt < NKT; ++kt) {
-        if (nv[kt] == 0) continue;
-        const float sc = C8 ? a.scale * ks[C8 ? kt : 0] : a.scale;
-        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        bc[kt] = bias[kt];
+        oc[kt] = old[kt];
+        sc[kt] = C8 ? a.scale * ks[C8 ? kt : 0] : a.scale;
+        n[kt] = nv[kt];
+        to[kt] = a.scores + row[kt] + 4 * lg;
+      }
+      load(next);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt) {
+        if (n[kt] == 0) continue;
+        const int j1 = (int)j0 + 16 * kt;
+        float y[NR][4];
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[rt][j] = exp_of<float>(fmaf(x[rt][kt][j], sc[kt], bc[kt][j]) - ref[rt]);
+        // rows that take no part, entries that a row does not see (whatever they hold)
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            y[rt][j] = (j1 + 15 <= open ? ref[rt] != INFINITY : j1 + 4 * lg + j <= lim[rt]) ? y[rt][j] : 0.f;
+        f32x4 sum;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int at = j0 + 16 * kt + 4 * lg + j;
+          sum[j] = y[0][j];
 #pragma unroll
-          for (int rt = 0; rt < NR; ++rt) {
-            const float y = exp_of<float>(fmaf(x[rt][kt][j], sc, bias[kt][j]) - ref[rt]);
-            sum[j] += at <= lim[rt] ? y : 0.f;
-          }
+          for (int rt = 1; rt < NR; ++rt) sum[j] += y[rt][j];
           sum[j] += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(sum[j]), 0x128, 0xF, 0xF, true));   // row_ror 8, 4, 2, 1
           sum[j] += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(sum[j]), 0x124, 0xF, 0xF, true));
           sum[j] += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(sum[j]), 0x122, 0xF, 0xF, true));
           sum[j] += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(sum[j]), 0x121, 0xF, 0xF, true));
-          if (at < known) sum[j] += old[kt][j];
+          if (j1 + 4 * lg + j < known) sum[j] += oc[kt][j];
         }
         if (l == 0) {
-          float* to = a.scores + row[kt] + 4 * lg;
-          if (nv[kt] == 16) {
-            *(f32x4*)to = sum;
+          if (n[kt] == 16) {
+            *(f32x4*)to[kt] = sum;
           } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-              if (4 * lg + j < nv[kt]) to[j] = sum[j];
+              if (4 * lg + j < n[kt]) to[kt][j] = sum[j];
           }
         }
       }
-    }
+      cur = next;
+  }
 }
 
 // ---------------------------------------------------------------------------
 // Choice of the entries to keep.  Block (g, s): head g of sequence s, or all heads
 // together (their scores added in 64 bits, rounded to 32).  Of n > keep entries the
 // first and the recent ones stay and the m largest scores between them: the m-th
-// largest key is found 11, 11 and 10 bits at a time by counting, then every wave lists
-// its part of the entries in order, those equal to that key until there are enough.
+// largest key is found 11, 11 and 10 bits at a time by counting, then the entries
+// above it, and those equal to it until there are enough, are listed in order.
+// T threads hold K keys each, entry k T + t in thread t; a list that is longer is read
+// again for every step.  Counts are kept four times over (lane mod 4): most scores share
+// a few exponents, and a count that many lanes raise at once takes them one by one.
 // ---------------------------------------------------------------------------
 struct PagedEvictArgs {
   PagedArgs c;
@@ -236,6 +290,8 @@ struct PagedEvictArgs {
   int* kept;            // [n_seqs][shared ? 1 : H][keep]
   int* new_lens;
   int keep, first, recent, shared;
+  uint32_t* keys;       // [lists][kstride] or NULL
+  long kstride;
 };
 
 // the order of numbers as that of whole ones; NaN as minus infinity, -0 as 0
@@ -244,10 +300,42 @@ __device__ __forceinline__ uint32_t score_key(float x) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-template <int T>
+// Few long lists: their keys by the whole chip first, four entries a thread; 0 for those that
+// are not chosen from.
+__global__ __launch_bounds__(256) void paged_keys_kernel(PagedEvictArgs a) {
+  const int g = blockIdx.y, s = blockIdx.z, n = paged_len(a.c, s);
+  if (n <= a.keep) return;
+  uint32_t* keys = a.keys + ((long)s * gridDim.y + g) * a.kstride;
+  for (long j = ((long)blockIdx.x * 256 + threadIdx.x) * 4; j < n; j += (long)gridDim.x * 1024) {
+    const int p = paged_page(a.c, s, j);
+    f32x4 x = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    if (p >= 0 && !a.shared) x = *(const f32x4*)(a.scores + paged_row(a.c, p, g, j));
+    if (p >= 0 && a.shared) {
+      double sum[4] = {};
+#pragma unroll 8
+      for (int h = 0; h < a.c.H; ++h) {
+        const f32x4 y = *(const f32x4*)(a.scores + paged_row(a.c, p, h, j));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] += y[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = (float)sum[i];
+    }
+    u32x4 k;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) k[i] = j + i >= a.first && j + i < n - a.recent ? score_key(x[i]) : 0;
+    *(u32x4*)(keys + j) = k;
+  }
+}
+
+constexpr int SELECT_COPIES = 4;
+
+// DENSE: keys of paged_keys_kernel.
+template <int T, int K, bool DENSE>
 __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
-  constexpr int BINS = 2048, W = T / 64, PER = BINS / T;
-  __shared__ int hist[BINS], part[W], part_eq[W], found[2];
+  constexpr int BINS = 2048, W = T / 64, PER = BINS / T, CP = SELECT_COPIES;
+  static_assert(K * W <= BINS * CP / 2, "the counts of (step, wave) take the place of the bins'");
+  __shared__ int hist[BINS * CP], part[W], found[2];
   const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), g = blockIdx.x, s = blockIdx.y;
   const int n = paged_len(a.c, s);
   int* kept = a.kept + ((long)s * gridDim.x + g) * a.keep;
@@ -255,30 +343,77 @@ __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
     for (int i = tid; i < a.keep; i += T) kept[i] = i < n ? i : -1;
     return;
   }
-  const int lo = a.first, hi = n - a.recent, m = a.keep - a.first - a.recent;   // lo + m < hi
-  auto key = [&](int j) {
-    const int p = paged_page(a.c, s, j);
-    if (p < 0) return score_key(-INFINITY);
-    if (!a.shared) return score_key(a.scores[paged_row(a.c, p, g, j)]);
-    double x = 0.0;
-    for (int h = 0; h < a.c.H; ++h) x += a.scores[paged_row(a.c, p, h, j)];
-    return score_key((float)x);
+  const int m = a.keep - a.first - a.recent;
+  for (int i = tid; i < a.first; i += T) kept[i] = i;
+  for (int i = tid; i < a.recent; i += T) kept[a.first + m + i] = n - a.recent + i;
+  if (m == 0) return;
+  const int lo = DENSE ? 0 : a.first, hi = DENSE ? n : n - a.recent;
+  uint32_t key[K];              // of entries base + k T + tid (behind the last one: 0, below every key)
+  auto load = [&](int first) {
+    if constexpr (DENSE) {
+      const uint32_t* keys = a.keys + ((long)s * gridDim.x + g) * a.kstride;
+#pragma unroll
+      for (int k = 0; k < K; ++k) key[k] = first + k * T + tid < hi ? keys[first + k * T + tid] : 0;
+      return;
+    }
+    constexpr int B = K < 8 ? K : 8;   // at a time
+#pragma unroll
+    for (int k0 = 0; k0 < (DENSE ? 0 : K); k0 += B) {
+      const int base = first + k0 * T;
+      if (base >= hi) {
+#pragma unroll
+        for (int k = 0; k < B; ++k) key[k0 + k] = 0;
+        continue;
+      }
+      int page[B];
+#pragma unroll
+      for (int k = 0; k < B; ++k) page[k] = a.c.table[s * a.c.tstride + (min(base + k * T + tid, hi - 1) >> a.c.lp)];
+      auto row = [&](int k, int h) {
+        const bool ok = (unsigned)page[k] < (unsigned)a.c.n_pages;
+        return paged_row(a.c, ok ? page[k] : 0, h, min(base + k * T + tid, hi - 1));
+      };
+      float x[B];
+      if (!a.shared) {
+#pragma unroll
+        for (int k = 0; k < B; ++k) x[k] = a.scores[row(k, g)];
+      } else {
+        double sum[B] = {};
+        for (int h = 0; h < a.c.H; ++h)
+#pragma unroll
+          for (int k = 0; k < B; ++k) sum[k] += a.scores[row(k, h)];
+#pragma unroll
+        for (int k = 0; k < B; ++k) x[k] = (float)sum[k];
+      }
+#pragma unroll
+      for (int k = 0; k < B; ++k) {
+        const bool ok = (unsigned)page[k] < (unsigned)a.c.n_pages;
+        key[k0 + k] = base + k * T + tid < hi ? score_key(ok ? x[k] : -INFINITY) : 0;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
+  load(lo);
+  const bool once = hi - lo <= K * T;
   uint32_t top = 0, mask = 0;   // the bits of the m-th largest key that are known
   int left = m;                 // its rank among the keys that have them
-  for (int shift = 21; m > 0 && shift >= 0; shift = shift == 21 ? 10 : shift - 10) {
+  for (int shift = 21; shift >= 0; shift = shift == 21 ? 10 : shift - 10) {
     const int bins = shift ? 2048 : 1024;
-    for (int i = tid; i < BINS; i += T) hist[i] = 0;
+    for (int i = tid; i < BINS * CP / 4; i += T) ((int4*)hist)[i] = make_int4(0, 0, 0, 0);
     __syncthreads();
-    for (int j = lo + tid; j < hi; j += T) {
-      const uint32_t k = key(j);
-      if ((k & mask) == top) atomicAdd(&hist[k >> shift & (bins - 1)], 1);
+    for (int base = lo; base < hi; base += K * T) {
+      if (!once && (base != lo || shift != 21)) load(base);
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        if (key[k] && (key[k] & mask) == top) atomicAdd(&hist[(key[k] >> shift & (bins - 1)) * CP + lane % CP], 1);
     }
     __syncthreads();
     // thread t holds bins BINS - 1 - (PER t + i), so that sums run from the largest key down
     int c[PER], sum = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) sum += c[i] = hist[BINS - 1 - (PER * tid + i)];
+    for (int i = 0; i < PER; ++i) {
+      const int4 x = ((const int4*)hist)[BINS - 1 - (PER * tid + i)];
+      sum += c[i] = x.x + x.y + x.z + x.w;
+    }
     const int incl = lanes_scan(sum);
     if (lane == 63) part[w] = incl;
     __syncthreads();
@@ -296,36 +431,45 @@ __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
     top |= (uint32_t)found[0] << shift;
     mask |= (uint32_t)(bins - 1) << shift;
     left = found[1];
+  }
+  // ---- the list: (step, wave) by (step, wave), counts of the larger and of the equal keys
+  int* larger = hist;
+  int* equal = hist + BINS * CP / 2;
+  int more = 0, same = 0;       // in front of the keys held
+  for (int base = lo; base < hi; base += K * T) {
+    if (!once) load(base);
+    __syncthreads();            // the bins, or the counts before, have been read
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int x = __popcll(__ballot(key[k] > top)), y = __popcll(__ballot(key[k] == top));
+      if (lane == 0) {
+        larger[k * W + w] = x;
+        equal[k * W + w] = y;
+      }
+    }
     __syncthreads();
-  }
-  for (int i = tid; i < a.first; i += T) kept[i] = i;
-  for (int i = tid; i < a.recent; i += T) kept[a.first + m + i] = hi + i;
-  if (m == 0) return;
-  // ---- every wave's part of the entries: how many it takes, then which
-  const int each = ((hi - lo + W - 1) / W + 63) / 64 * 64, j0 = lo + w * each, j1 = min(hi, j0 + each);
-  int more = 0, equal = 0;
-  for (int j = j0; j < j1; j += 64) {
-    const uint32_t k = j + lane < j1 ? key(j + lane) : 0;
-    more += __popcll(__ballot(k > top));
-    equal += __popcll(__ballot(k == top));
-  }
-  if (lane == 0) {
-    part[w] = more;
-    part_eq[w] = equal;
-  }
-  __syncthreads();
-  more = equal = 0;
-  for (int i = 0; i < w; ++i) {
-    more += part[i];
-    equal += part_eq[i];
-  }
-  for (int j = j0; j < j1; j += 64) {
-    const uint32_t k = j + lane < j1 ? key(j + lane) : 0;
-    const unsigned long over = __ballot(k > top), same = __ballot(k == top), below = (1UL << lane) - 1;
-    const int e = equal + __popcll(same & below);
-    if (k > top || (k == top && e < left)) kept[a.first + more + __popcll(over & below) + min(e, left)] = j + lane;
-    more += __popcll(over);
-    equal += __popcll(same);
+    // sums in front of (k, w): wave w takes 64 counts at a time, all of them
+    if (w < 2) {
+      int* counts = w ? equal : larger;
+      int run = w ? same : more;
+      for (int i = lane; i < (K * W + 63) / 64 * 64; i += 64) {
+        const int x = i < K * W ? counts[i] : 0, incl = lanes_scan(x);
+        if (i < K * W) counts[i] = run + incl - x;
+        run += __builtin_amdgcn_readlane(incl, 63);
+      }
+      if (lane == 0) part[w] = run;
+    }
+    __syncthreads();
+    const unsigned long below = (1UL << lane) - 1;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const unsigned long over = __ballot(key[k] > top), eq = __ballot(key[k] == top);
+      const int e = equal[k * W + w] + __popcll(eq & below);
+      if (key[k] > top || (key[k] == top && e < left))
+        kept[a.first + larger[k * W + w] + __popcll(over & below) + min(e, left)] = base + k * T + tid;
+    }
+    more = part[0];
+    same = part[1];
   }
 }
 
@@ -347,52 +491,66 @@ __global__ __launch_bounds__(1024) void paged_move_kernel(PagedEvictArgs a, int 
   if (z == 2 * pieces && h == 0 && tid == 0) a.new_lens[s] = min(paged_len(a.c, s), a.keep);
   if (kept[a.keep - 1] < 0) return;   // all of fewer entries stay
   constexpr int U = EVICT_U;
-  if (z == 2 * pieces) {
-    for (int i0 = 0; i0 < a.keep; i0 += U * T) {
-      const int last = min(i0 + U * T, a.keep) - 1;
-      if (kept[last] == last) continue;   // (and so every one before it)
+  const bool rows = z < 2 * pieces;
+  // keys, values: a wave takes U * rpw entries in a row, rpw at a time; scores: U * 64
+  const int kv = z / pieces, lpr = rows ? ROWB / 16 / pieces : 1, rpw = 64 / lpr, c = z % pieces * lpr + lane % lpr;
+  char* pages = kv ? a.c.v : a.c.k;
+  float* scales = kv ? a.c.vs : a.c.ks;
+  const int chunk = (T >> 6) * U * rpw;
+  auto entry = [&](int i0, int u) { return i0 + (w * U + u) * rpw + lane / lpr; };
+  long from[U], to[U];                // rows of the pages that entry and place are, or -1
+  auto find = [&](int i0) {
+    int j[U], pf[U], pt[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) j[u] = entry(i0, u) < a.keep ? kept[entry(i0, u)] : -1;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      pf[u] = j[u] < 0 ? -1 : paged_page(a.c, s, j[u]);
+      pt[u] = j[u] < 0 ? -1 : paged_page(a.c, s, entry(i0, u));
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      from[u] = pf[u] < 0 ? -1 : paged_row(a.c, pf[u], h, j[u]);
+      to[u] = pt[u] < 0 ? -1 : paged_row(a.c, pt[u], h, entry(i0, u));
+    }
+  };
+  auto moves = [&](int i0) {          // (kept[i] == i: and so for every entry before it)
+    const int last = min(i0 + chunk, a.keep) - 1;
+    return kept[last] != last;
+  };
+  int i0 = 0;
+  while (i0 < a.keep && !moves(i0)) i0 += chunk;
+  if (i0 < a.keep) find(i0);
+  for (; i0 < a.keep; i0 += chunk) {
+    long at[U];
+    if (!rows) {
       float x[U], b[U];
-      int to[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int i = i0 + u * T + tid, j = i < a.keep ? kept[i] : -1, from = j < 0 ? -1 : paged_page(a.c, s, j);
-        to[u] = j < 0 ? -1 : paged_page(a.c, s, i);
-        const long row = paged_row(a.c, max(from, 0), h, max(j, 0));
-        x[u] = from < 0 ? 0.f : a.scores[row];
-        b[u] = from < 0 || !a.c.beta ? 0.f : a.c.beta[row];
+        x[u] = from[u] < 0 ? 0.f : a.scores[from[u]];
+        b[u] = from[u] < 0 || !a.c.beta ? 0.f : a.c.beta[from[u]];
+        at[u] = to[u];
       }
+      if (i0 + chunk < a.keep) find(i0 + chunk);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (to[u] >= 0) {
-          const long row = paged_row(a.c, to[u], h, i0 + u * T + tid);
-          a.scores[row] = x[u];
-          if (a.c.beta) a.c.beta[row] = b[u];
+        if (at[u] >= 0) {
+          a.scores[at[u]] = x[u];
+          if (a.c.beta) a.c.beta[at[u]] = b[u];
         }
+      continue;
     }
-    return;
-  }
-  // a wave takes U * RPW entries in a row, RPW at a time
-  const int kv = z / pieces, lpr = ROWB / 16 / pieces, rpw = 64 / lpr, c = z % pieces * lpr + lane % lpr;
-  char* pages = kv ? a.c.v : a.c.k;
-  float* scales = kv ? a.c.vs : a.c.ks;
-  const int chunk = (T >> 6) * U * rpw;
-  for (int i0 = 0; i0 < a.keep; i0 += chunk) {
-    const int last = min(i0 + chunk, a.keep) - 1;
-    if (kept[last] == last) continue;
     u32x4 x[U];
     float sc[U];
-    int to[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = i0 + (w * U + u) * rpw + lane / lpr, j = i < a.keep ? kept[i] : -1;
-      const int from = j < 0 ? -1 : paged_page(a.c, s, j);
-      to[u] = j < 0 ? -1 : paged_page(a.c, s, i);
-      const long row = paged_row(a.c, max(from, 0), h, max(j, 0));
-      x[u] = from < 0 ? u32x4{0, 0, 0, 0} : ((const u32x4*)(pages + row * ROWB))[c];
-      if (C8) sc[u] = from < 0 ? 0.f : scales[row / PAGED_BLOCK];
+      x[u] = from[u] < 0 ? u32x4{0, 0, 0, 0} : __builtin_nontemporal_load((const u32x4*)(pages + from[u] * ROWB) + c);
+      if (C8) sc[u] = from[u] < 0 ? 0.f : scales[from[u] / PAGED_BLOCK];
+      at[u] = to[u];
     }
+    if (i0 + chunk < a.keep) find(i0 + chunk);   // (places and list are not what this chunk writes)
     if constexpr (C8) {   // a block's largest scale: over its lanes, then over its steps
       constexpr int LPR = ROWB / 16, RPW = 64 / LPR, SPB = std::max(1, PAGED_BLOCK / RPW);   // steps of a block
 #pragma unroll
@@ -424,11 +582,9 @@ __global__ __launch_bounds__(1024) void paged_move_kernel(PagedEvictArgs a, int 
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (to[u] >= 0) {
-        const int i = i0 + (w * U + u) * rpw + lane / lpr;
-        const long row = paged_row(a.c, to[u], h, i);
-        ((u32x4*)(pages + row * ROWB))[c] = x[u];
-        if (C8 && lane % lpr == 0 && (i & (PAGED_BLOCK - 1)) == 0) scales[row / PAGED_BLOCK] = sc[u];
+      if (at[u] >= 0) {
+        __builtin_nontemporal_store(x[u], (u32x4*)(pages + at[u] * ROWB) + c);
+        if (C8 && lane % lpr == 0 && (at[u] & (PAGED_BLOCK - 1)) == 0) scales[at[u] / PAGED_BLOCK] = sc[u];
       }
   }
 }

@@ -175,8 +175,9 @@ def _score(cache=None, seqs=None, cfg=None, q=FAKE, pos=None, lse=FAKE, known=No
     return binding.still_paged_score(cache or _cache8(), seqs or _seqs(), cfg or _acfg(), q, pos, lse, known, scores, None)
 
 
-def _evict(cache=None, seqs=None, cfg=None, scores=FAKE, kept=FAKE, new_lens=FAKE):
-    return binding.still_paged_evict(cache or _cache8(), seqs or _seqs(), cfg or _ecfg(), scores, kept, new_lens, None)
+def _evict(cache=None, seqs=None, cfg=None, scores=FAKE, kept=FAKE, new_lens=FAKE, ws=None, ws_bytes=0):
+    return binding.still_paged_evict(cache or _cache8(), seqs or _seqs(), cfg or _ecfg(), scores, kept, new_lens, ws, ws_bytes,
+                                     None)
 
 
 @pytest.mark.parametrize("make", [_cache8, _plain])
@@ -204,11 +205,25 @@ def test_score_and_evict_null_structs_and_scales():
     assert _score(cache=_cache8(k_scale=None)) == -1 and _evict(cache=_cache8(v_scale=FAKE + 4)) == -1
     lib, s = binding.lib(), ctypes.byref(_seqs())
     for c in (None, ctypes.byref(_cache8())):
-        assert lib.still_paged8_evict(c, s if c is None else None, ctypes.byref(_ecfg()), FAKE, FAKE, FAKE, None) == -1
+        assert lib.still_paged8_evict(c, s if c is None else None, ctypes.byref(_ecfg()), FAKE, FAKE, FAKE, None, 0, None) == -1
         assert lib.still_paged8_score(c, s if c is None else None, ctypes.byref(_acfg()), FAKE, None, FAKE, None, FAKE, None) == -1
-    assert lib.still_paged8_evict(ctypes.byref(_cache8()), s, None, FAKE, FAKE, FAKE, None) == -1
-    assert lib.still_paged_evict(None, s, ctypes.byref(_ecfg()), FAKE, FAKE, FAKE, None) == -1
+    assert lib.still_paged8_evict(ctypes.byref(_cache8()), s, None, FAKE, FAKE, FAKE, None, 0, None) == -1
+    assert lib.still_paged_evict(None, s, ctypes.byref(_ecfg()), FAKE, FAKE, FAKE, None, 0, None) == -1
     assert lib.still_paged_score(None, s, ctypes.byref(_acfg()), FAKE, None, FAKE, None, FAKE, None) == -1
+
+
+def test_evict_workspace():
+    """The lists' keys where few long tables are given, 64 MiB at most; none for others."""
+    size = binding.still_paged_evict_workspace_size
+    assert size(_plain(), _seqs(max_pages=512, table_stride=512), _ecfg()) == 0
+    long = _seqs(max_pages=600, table_stride=600)
+    assert size(_plain(), long, _ecfg()) == 4 * 8 * 9600 * 4 and size(_plain(), long, _ecfg(shared=1)) == 4 * 9600 * 4
+    assert size(_plain(), _seqs(n_seqs=60, max_pages=600, table_stride=600), _ecfg()) == 0
+    for pages in (1 << 16, 1 << 20, 1 << 26):
+        assert size(_plain(), _seqs(max_pages=pages, table_stride=pages), _ecfg(shared=1)) <= 64 << 20
+    assert size(_plain(head_dim=96), long, _ecfg()) == 0 and size(_plain(), long, _ecfg(keep=0)) == 0
+    assert _evict(seqs=long) == -4 and _evict(seqs=long, ws=FAKE, ws_bytes=1000) == -4
+    assert _evict(seqs=long, ws=FAKE + 4, ws_bytes=1 << 30) == -1
 
 
 def test_binding_refuses_scores_that_do_not_fit():
