@@ -280,9 +280,9 @@ __global__ __launch_bounds__(256) void paged_score_kernel(PagedScoreArgs a) {
 // first and the recent ones stay and the m largest scores between them: the m-th
 // largest key is found 11, 11 and 10 bits at a time by counting, then the entries
 // above it, and those equal to it until there are enough, are listed in order.
-// T threads hold K keys each, entry k T + t in thread t; a list that is longer is read
-// again for every step.  Counts are kept four times over (lane mod 4): most scores share
-// a few exponents, and a count that many lanes raise at once takes them one by one.
+// T threads hold up to K keys each; a list that is longer is read again for every step.
+// Long lists' counts are kept four times over (lane mod 4): most scores share a few
+// exponents, and a count that many lanes raise at once takes them one by one.
 // ---------------------------------------------------------------------------
 struct PagedEvictArgs {
   PagedArgs c;
@@ -328,14 +328,11 @@ __global__ __launch_bounds__(256) void paged_keys_kernel(PagedEvictArgs a) {
   }
 }
 
-constexpr int SELECT_COPIES = 4;
-
 // DENSE: keys of paged_keys_kernel.
 template <int T, int K, bool DENSE>
 __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
-  constexpr int BINS = 2048, W = T / 64, PER = BINS / T, CP = SELECT_COPIES;
-  static_assert(K * W <= BINS * CP / 2, "the counts of (step, wave) take the place of the bins'");
-  __shared__ int hist[BINS * CP], part[W], found[2];
+  constexpr int BINS = 2048, W = T / 64, PER = BINS / T, CP = T == 1024 ? 4 : 1;
+  __shared__ int hist[BINS * CP], part[W], part_eq[W], found[3];
   const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), g = blockIdx.x, s = blockIdx.y;
   const int n = paged_len(a.c, s);
   int* kept = a.kept + ((long)s * gridDim.x + g) * a.keep;
@@ -348,29 +345,41 @@ __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
   for (int i = tid; i < a.recent; i += T) kept[a.first + m + i] = n - a.recent + i;
   if (m == 0) return;
   const int lo = DENSE ? 0 : a.first, hi = DENSE ? n : n - a.recent;
-  uint32_t key[K];              // of entries base + k T + tid (behind the last one: 0, below every key)
-  auto load = [&](int first) {
+  // a round: `steps` keys of every thread, those of a wave next to each other
+  const int steps = min(K, (hi - lo + T - 1) / T), span = steps * T;
+  uint32_t key[K];              // (of no entry: 0, below every key)
+  auto entry = [&](int base, int k) { return base + (w * steps + k) * 64 + lane; };
+  auto load = [&](int base) {
     if constexpr (DENSE) {
-      const uint32_t* keys = a.keys + ((long)s * gridDim.x + g) * a.kstride;
+      // (behind the last key: zeros; a list's keys are 64 MB at most)
+      const auto r = paged_rows(a.keys + ((long)s * gridDim.x + g) * a.kstride, hi * 4);
+      const int off = ((int)base + w * steps * 64 + lane) * 4;
 #pragma unroll
-      for (int k = 0; k < K; ++k) key[k] = first + k * T + tid < hi ? keys[first + k * T + tid] : 0;
+      for (int k0 = 0; k0 < K; k0 += 16) {
+        if (k0 < steps) {
+#pragma unroll
+          for (int k = k0; k < k0 + 16; ++k) key[k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_raw_buffer_load_b32(r, off, k * 256, 0));
+        }
+#pragma unroll
+        for (int k = k0; k < k0 + 16; ++k) key[k] = k < steps ? key[k] : 0;
+      }
       return;
     }
     constexpr int B = K < 8 ? K : 8;   // at a time
 #pragma unroll
     for (int k0 = 0; k0 < (DENSE ? 0 : K); k0 += B) {
-      const int base = first + k0 * T;
-      if (base >= hi) {
+      if (k0 >= steps) {
 #pragma unroll
-        for (int k = 0; k < B; ++k) key[k0 + k] = 0;
+        for (int k = k0; k < k0 + B; ++k) key[k] = 0;
         continue;
       }
       int page[B];
+      auto at = [&](int k) { return min(entry(base, k0 + k), hi - 1); };
 #pragma unroll
-      for (int k = 0; k < B; ++k) page[k] = a.c.table[s * a.c.tstride + (min(base + k * T + tid, hi - 1) >> a.c.lp)];
+      for (int k = 0; k < B; ++k) page[k] = a.c.table[s * a.c.tstride + (at(k) >> a.c.lp)];
       auto row = [&](int k, int h) {
         const bool ok = (unsigned)page[k] < (unsigned)a.c.n_pages;
-        return paged_row(a.c, ok ? page[k] : 0, h, min(base + k * T + tid, hi - 1));
+        return paged_row(a.c, ok ? page[k] : 0, h, at(k));
       };
       float x[B];
       if (!a.shared) {
@@ -387,32 +396,49 @@ __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
 #pragma unroll
       for (int k = 0; k < B; ++k) {
         const bool ok = (unsigned)page[k] < (unsigned)a.c.n_pages;
-        key[k0 + k] = base + k * T + tid < hi ? score_key(ok ? x[k] : -INFINITY) : 0;
+        key[k0 + k] = k0 + k < steps && entry(base, k0 + k) < hi ? score_key(ok ? x[k] : -INFINITY) : 0;
       }
       __builtin_amdgcn_sched_barrier(0);
     }
   };
+  // f(k) for the keys held; those from `steps` on are 0
+  auto each = [&](auto f) {
+    constexpr int B = K < 16 ? K : 16;
+#pragma unroll
+    for (int k0 = 0; k0 < K; k0 += B)
+      if (k0 < steps)
+#pragma unroll
+        for (int k = k0; k < k0 + B; ++k) f(k);
+  };
   load(lo);
-  const bool once = hi - lo <= K * T;
+  const bool once = hi - lo <= span;
   uint32_t top = 0, mask = 0;   // the bits of the m-th largest key that are known
   int left = m;                 // its rank among the keys that have them
+  bool all = false;             // that is the last one of them
   for (int shift = 21; shift >= 0; shift = shift == 21 ? 10 : shift - 10) {
     const int bins = shift ? 2048 : 1024;
     for (int i = tid; i < BINS * CP / 4; i += T) ((int4*)hist)[i] = make_int4(0, 0, 0, 0);
     __syncthreads();
-    for (int base = lo; base < hi; base += K * T) {
+    for (long base = lo; base < hi; base += span) {
       if (!once && (base != lo || shift != 21)) load(base);
-#pragma unroll
-      for (int k = 0; k < K; ++k)
-        if (key[k] && (key[k] & mask) == top) atomicAdd(&hist[(key[k] >> shift & (bins - 1)) * CP + lane % CP], 1);
+      each([&](int k) {   // (the known bits of a key of no entry are not those of `top`, once there are any)
+        if (shift == 21 ? key[k] != 0 : ((key[k] ^ top) & mask) == 0)
+          atomicAdd(&hist[(key[k] >> shift & (bins - 1)) * CP + lane % CP], 1);
+      });
     }
     __syncthreads();
     // thread t holds bins BINS - 1 - (PER t + i), so that sums run from the largest key down
     int c[PER], sum = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int4 x = ((const int4*)hist)[BINS - 1 - (PER * tid + i)];
-      sum += c[i] = x.x + x.y + x.z + x.w;
+      const int b = BINS - 1 - (PER * tid + i);
+      if constexpr (CP == 4) {
+        const int4 x = ((const int4*)hist)[b];
+        c[i] = x.x + x.y + x.z + x.w;
+      } else {
+        c[i] = hist[b];
+      }
+      sum += c[i];
     }
     const int incl = lanes_scan(sum);
     if (lane == 63) part[w] = incl;
@@ -424,6 +450,7 @@ __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
       if (before < left && left <= before + c[i]) {   // (one thread's)
         found[0] = BINS - 1 - (PER * tid + i);
         found[1] = left - before;
+        found[2] = left == before + c[i];
       }
       before += c[i];
     }
@@ -431,45 +458,51 @@ __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
     top |= (uint32_t)found[0] << shift;
     mask |= (uint32_t)(bins - 1) << shift;
     left = found[1];
+    all = found[2];
   }
-  // ---- the list: (step, wave) by (step, wave), counts of the larger and of the equal keys
-  int* larger = hist;
-  int* equal = hist + BINS * CP / 2;
-  int more = 0, same = 0;       // in front of the keys held
-  for (int base = lo; base < hi; base += K * T) {
+  if (all) {   // every key equal to the m-th stays too
+    top -= 1;  // (keys of entries are above 0)
+    left = 0;
+  }
+  // ---- the list, wave by wave: how many keys each has above `top` and equal to it, then which
+  int more = 0, same = 0;       // in front of the round
+  for (long base = lo; base < hi; base += span) {
     if (!once) load(base);
-    __syncthreads();            // the bins, or the counts before, have been read
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int x = __popcll(__ballot(key[k] > top)), y = __popcll(__ballot(key[k] == top));
-      if (lane == 0) {
-        larger[k * W + w] = x;
-        equal[k * W + w] = y;
-      }
+    int x = 0, y = 0;
+    each([&](int k) { x += __popcll(__ballot(key[k] > top)); });
+    if (left) each([&](int k) { y += __popcll(__ballot(key[k] == top)); });
+    __syncthreads();            // the counts before have been read
+    if (lane == 0) {
+      part[w] = x;
+      part_eq[w] = y;
     }
     __syncthreads();
-    // sums in front of (k, w): wave w takes 64 counts at a time, all of them
-    if (w < 2) {
-      int* counts = w ? equal : larger;
-      int run = w ? same : more;
-      for (int i = lane; i < (K * W + 63) / 64 * 64; i += 64) {
-        const int x = i < K * W ? counts[i] : 0, incl = lanes_scan(x);
-        if (i < K * W) counts[i] = run + incl - x;
-        run += __builtin_amdgcn_readlane(incl, 63);
+    int over = 0, eq = 0;
+    for (int i = 0; i < W; ++i) {
+      if (i == w) {
+        over = more;
+        eq = same;
       }
-      if (lane == 0) part[w] = run;
+      more += part[i];
+      same += part_eq[i];
     }
-    __syncthreads();
-    const unsigned long below = (1UL << lane) - 1;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const unsigned long over = __ballot(key[k] > top), eq = __ballot(key[k] == top);
-      const int e = equal[k * W + w] + __popcll(eq & below);
-      if (key[k] > top || (key[k] == top && e < left))
-        kept[a.first + larger[k * W + w] + __popcll(over & below) + min(e, left)] = base + k * T + tid;
+    auto lanes_below = [](unsigned long x) { return (int)__builtin_amdgcn_mbcnt_hi(x >> 32, __builtin_amdgcn_mbcnt_lo((uint32_t)x, 0)); };
+    int* to = kept + a.first;
+    if (left == 0) {
+      each([&](int k) {
+        const unsigned long o = __ballot(key[k] > top);
+        if (key[k] > top) to[over + lanes_below(o)] = entry((int)base, k);
+        over += __popcll(o);
+      });
+      continue;
     }
-    more = part[0];
-    same = part[1];
+    each([&](int k) {
+      const unsigned long o = __ballot(key[k] > top), e = __ballot(key[k] == top);
+      const int r = eq + lanes_below(e);
+      if (key[k] > top || (key[k] == top && r < left)) to[over + lanes_below(o) + min(r, left)] = entry((int)base, k);
+      over += __popcll(o);
+      eq += __popcll(e);
+    });
   }
 }
 
