@@ -51,10 +51,16 @@ static still_status paged_score_call(const still_paged_cache* cache, const float
     constexpr int D = decltype(d)::value;
     const dim3 grid(cache->n_kv_heads, seqs->n_seqs, z);
     const bool rot = a.qpos != nullptr;
-    if (cfg->group * cfg->n_queries <= 16)
-      hipLaunchKernelGGL((paged_score_kernel<IT, D, 1, CT>), grid, dim3(256), (ScoreTile<IT, D, 1, CT>::lds_bytes(rot, cfg->n_queries)), st, a);
-    else
-      hipLaunchKernelGGL((paged_score_kernel<IT, D, 2, CT>), grid, dim3(256), (ScoreTile<IT, D, 2, CT>::lds_bytes(rot, cfg->n_queries)), st, a);
+    auto launch = [&](auto rp) {
+      using TL = ScoreTile<IT, D, decltype(rp)::value, CT>;
+      hipLaunchKernelGGL((paged_score_kernel<IT, D, decltype(rp)::value, CT>), grid, dim3(256), TL::lds_bytes(rot, cfg->n_queries),
+                         st, a);
+    };
+    const int R = cfg->group * cfg->n_queries;
+    if (R <= 4) launch(std::integral_constant<int, 4>());
+    else if (R <= 8) launch(std::integral_constant<int, 8>());
+    else if (R <= 16) launch(std::integral_constant<int, 16>());
+    else launch(std::integral_constant<int, 32>());
   });
   HIP_TRY(hipGetLastError());
   return STILL_OK;

@@ -12,8 +12,10 @@ namespace still {
 // With the rows' lse from the attention before it the keys are read once more and
 // nothing has to be joined: block (h, s, z) takes the chunks z, z + gridDim.z, ... of
 // SCORE_CHUNK entries of sequence s, a wave NKT 16-entry tiles of one at a time.
-// S^T[entry][row] as in paged_attend_kernel (16 entries by 16 rows), so a lane holds row
-// l = lane % 16 of entries 4 lg + j, and the sum over the rows is one over 16 lanes.
+// S^T[entry][row] as in paged_attend_kernel (16 entries by 16 rows): lane group lg holds
+// entries 4 lg + j, lane l of it row l.  Where a KV head has 4 or 8 rows (a decode
+// step) the logits of 4 or 2 tiles are put next to each other in the 16 lanes, so that the
+// exponentials, of which there are more than products, are formed for rows that exist.
 // ---------------------------------------------------------------------------
 struct PagedScoreArgs {
   PagedArgs c;         // (v is not read)
@@ -30,21 +32,37 @@ struct PagedScoreArgs {
 
 constexpr int SCORE_CHUNK = 512;   // entries of a workgroup at a time
 
-template <class IT, int D, int NR, class CT>
+// RP: rows that fit a tile's lanes (4, 8, 16; 32: two tiles of rows).
+template <class IT, int D, int RP, class CT>
 struct ScoreTile {
   static constexpr bool C8 = sizeof(CT) == 1, B16 = C8 || sizeof(IT) == 2;
-  static constexpr int ROWB = D * (int)sizeof(CT), NP = ROWB / 64;
+  static constexpr int ROWB = D * (int)sizeof(CT), NP = ROWB / 64, NR = RP == 32 ? 2 : 1;
   static constexpr int NKT = std::max(1, std::min(4, 512 / ROWB));   // tiles of a wave at a time: 8 KB of keys
+  static constexpr int PK = std::min(NKT, RP < 16 ? 16 / RP : 1);    // of them side by side
   static constexpr int QROW = D * (B16 ? 2 : 4) + 16, QPART = 16 * NR * QROW;
   static __host__ __device__ bool split(bool rot) { return B16 && (rot || sizeof(IT) == 4); }
-  static __host__ __device__ int lds_bytes(bool rot, int nq) { return (split(rot) ? 3 : 1) * QPART + (rot ? nq * D / 2 * (int)sizeof(float2) : 0); }
+  static __host__ __device__ int lds_bytes(bool rot, int nq) {
+    return (split(rot) ? 3 : 1) * QPART + (rot ? nq * D / 2 * (int)sizeof(float2) : 0);
+  }
 };
 
-template <class IT, int D, int NR, class CT>
+// sum over the lanes of a group of RP
+template <int RP>
+__device__ __forceinline__ float rows_sum(float x) {
+  auto add = [](float x, auto c) { return x + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), decltype(c)::value, 0xF, 0xF, true)); };
+  x = add(x, std::integral_constant<int, 0xB1>());                 // lanes 1 0 3 2, 2 3 0 1, then those of the
+  x = add(x, std::integral_constant<int, 0x4E>());                 // other half of 8 and of 16
+  if (RP >= 8) x = add(x, std::integral_constant<int, 0x141>());
+  if (RP >= 16) x = add(x, std::integral_constant<int, 0x140>());
+  return x;
+}
+
+template <class IT, int D, int RP, class CT>
 __global__ __launch_bounds__(256) void paged_score_kernel(PagedScoreArgs a) {
-  using TL = ScoreTile<IT, D, NR, CT>;
+  using TL = ScoreTile<IT, D, RP, CT>;
   constexpr bool C8 = TL::C8;
-  constexpr int NKT = TL::NKT, NP = TL::NP, ROWB = TL::ROWB, QROW = TL::QROW, HD = D / 2, STEP = 16 * NKT;
+  constexpr int NKT = TL::NKT, NP = TL::NP, NR = TL::NR, ROWB = TL::ROWB, QROW = TL::QROW, HD = D / 2, STEP = 16 * NKT;
+  constexpr int PK = TL::PK, G = NKT / PK, LR = RP < 16 ? RP : 16;   // groups of PK tiles; lanes of a tile
   extern __shared__ float4 score_smem[];
   char* qs = (char*)score_smem;                  // [16 NR][QROW], where split three parts of that
   float2* cs = (float2*)(qs + (TL::split(a.qpos != nullptr) ? 3 : 1) * TL::QPART);   // [nq][D / 2]
@@ -55,48 +73,54 @@ __global__ __launch_bounds__(256) void paged_score_kernel(PagedScoreArgs a) {
   if ((long)blockIdx.z * SCORE_CHUNK >= len) return;
   const int known = a.known ? a.known[s] : len;
   const bool rot = a.qpos != nullptr;
-  // ---- this wave's units of STEP entries, in rising order: page numbers a unit ahead of the keys
-  constexpr int UPC = SCORE_CHUNK / (4 * STEP);   // of a chunk
+  // ---- this wave's units of STEP entries, in rising order.  A lane looks after one tile of
+  // each group: its page, its bias and scores.
+  constexpr int UPC = SCORE_CHUNK / (4 * STEP);   // units of a chunk
+  const int mine = min(l / LR, PK - 1);
   auto start_of = [&](int v) { return ((long)blockIdx.z + (long)(v / UPC) * gridDim.z) * SCORE_CHUNK + (v % UPC * 4 + w) * STEP; };
   struct Unit {
     long j0;
-    int p[NKT];
+    int p[G];
   };
   auto lookup = [&](int v) {
     Unit u;
     u.j0 = start_of(v);
 #pragma unroll
-    for (int kt = 0; kt < NKT; ++kt)
-      u.p[kt] = a.c.table[s * a.c.tstride + min((u.j0 + 16 * kt) >> a.c.lp, (long)a.c.max_pages - 1)];
+    for (int g = 0; g < G; ++g)
+      u.p[g] = a.c.table[s * a.c.tstride + min((u.j0 + 16 * (g * PK + mine)) >> a.c.lp, (long)a.c.max_pages - 1)];
     return u;
   };
-  int nv[NKT];      // valid entries of each tile
-  long row[NKT];    // rows of the pages in front of it
   u32x4 kp[NKT][NP];
-  f32x4 bias[NKT], old[NKT];
-  float ks[C8 ? NKT : 1];
+  f32x4 bias[G], old[G];
+  float ks[G];
+  int nv[G];        // valid entries of the lane's tile
+  float* to[G];     // their scores
   auto load = [&](const Unit& u) {
+    auto rows_of = [&](long j, int p, bool& ok) {   // row of the pages in front of the tile at entry j
+      ok = j < len && (unsigned)p < (unsigned)a.c.n_pages;
+      return (((long)(ok ? p : 0) * a.c.H + h) << a.c.lp) + (ok ? (int)j & ((1 << a.c.lp) - 1) : 0);
+    };
 #pragma unroll
-    for (int kt = 0; kt < NKT; ++kt) {
-      const long j = u.j0 + 16 * kt;
-      const int p = uniform(u.p[kt]);
-      const bool ok = j < len && (unsigned)p < (unsigned)a.c.n_pages;
-      nv[kt] = ok ? (int)min(16L, len - j) : 0;
-      row[kt] = (((long)(ok ? p : 0) * a.c.H + h) << a.c.lp) + (ok ? (int)j & ((1 << a.c.lp) - 1) : 0);
-    }
+    for (int g = 0; g < G; ++g)
 #pragma unroll
-    for (int kt = 0; kt < NKT; ++kt) {
-      const auto r = paged_rows(a.c.k + row[kt] * ROWB, nv[kt] * ROWB);
+      for (int t = 0; t < PK; ++t) {
+        const int kt = g * PK + t;
+        bool ok;
+        const long j = u.j0 + 16 * kt, row = rows_of(j, __builtin_amdgcn_readlane(u.p[g], t * LR), ok);
+        const auto r = paged_rows(a.c.k + row * ROWB, ok ? (int)min(16L, len - j) * ROWB : 0);
 #pragma unroll
-      for (int i = 0; i < NP; ++i)
-        kp[kt][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, l * ROWB + lg * 16 + 64 * i, 0, 0));
-      const int few = nv[kt] > 0 ? 64 : 0;
-      bias[kt] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                                               paged_rows(a.c.beta + row[kt], a.c.beta ? few : 0), 16 * lg, 0, 0));
-      old[kt] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(paged_rows(a.scores + row[kt], few), 16 * lg, 0, 0));
-      if constexpr (C8)
-        ks[kt] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(
-                                               paged_rows(a.c.ks + row[kt] / PAGED_BLOCK, nv[kt] > 0 ? 4 : 0), 0, 0, 0));
+        for (int i = 0; i < NP; ++i)
+          kp[kt][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, l * ROWB + lg * 16 + 64 * i, 0, 0));
+      }
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      bool ok;
+      const long j = u.j0 + 16 * (g * PK + mine), row = rows_of(j, u.p[g], ok);   // (not ok: of a page that is there)
+      nv[g] = ok ? (int)min(16L, len - j) : 0;
+      to[g] = a.scores + row + 4 * lg;
+      old[g] = *(const f32x4*)to[g];
+      bias[g] = a.c.beta ? *(const f32x4*)(a.c.beta + row + 4 * lg) : f32x4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (C8) ks[g] = a.c.ks[row / PAGED_BLOCK];
     }
   };
   Unit cur = lookup(0);
@@ -166,111 +190,107 @@ __global__ __launch_bounds__(256) void paged_score_kernel(PagedScoreArgs a) {
   int lim[NR];   // last entry that this lane's row sees
 #pragma unroll
   for (int rt = 0; rt < NR; ++rt) {
-    const int r = 16 * rt + l;
+    const int r = 16 * rt + l % LR;
     ref[rt] = row_lse[r];
     lim[rt] = ref[rt] == INFINITY ? -1 : a.causal ? len - a.nq + r % a.nq : len - 1;
   }
-  const long open = a.causal ? (long)len - a.nq : len - 1L;   // every row sees the entries up to this one
+  const bool writes = l % LR == 0 && l / LR < PK;
   for (int v = 0; cur.j0 < len; ++v) {
-      const long j0 = cur.j0;
-      const Unit next = lookup(v + 1);
-      __builtin_amdgcn_sched_barrier(0);
-      f32x4 x[NR][NKT];
+    const int j0 = (int)cur.j0;
+    const Unit next = lookup(v + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4 x[NR][NKT];
 #pragma unroll
-      for (int rt = 0; rt < NR; ++rt)
+    for (int rt = 0; rt < NR; ++rt)
 #pragma unroll
-        for (int kt = 0; kt < NKT; ++kt) x[rt][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-      auto product = [&](int part, const u32x4 (&kv)[NKT], int at) {
+      for (int kt = 0; kt < NKT; ++kt) x[rt][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto product = [&](int part, const u32x4 (&kv)[NKT], int at) {
 #pragma unroll
-        for (int rt = 0; rt < NR; ++rt) {
-          const u32x4 qv = *(const u32x4*)(qs + part * TL::QPART + (16 * rt + l) * QROW + at);
+      for (int rt = 0; rt < NR; ++rt) {
+        const u32x4 qv = *(const u32x4*)(qs + part * TL::QPART + (16 * rt + l) * QROW + at);
 #pragma unroll
-          for (int kt = 0; kt < NKT; ++kt) {
-            if constexpr (TL::B16) {
-              x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kv[kt]),
-                                                                  __builtin_bit_cast(bf16x8, qv), x[rt][kt], 0, 0, 0);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kv[kt][e]), __uint_as_float(qv[e]),
-                                                                 x[rt][kt], 0, 0, 0);
-            }
-          }
-        }
-      };
-#pragma unroll
-      for (int p = 0; p < NP; ++p)
-#pragma unroll
-        for (int half = 0; half < (C8 ? 2 : 1); ++half) {
-          u32x4 kv[NKT];
-#pragma unroll
-          for (int kt = 0; kt < NKT; ++kt) {
-            kv[kt] = kp[kt][p];
-            if constexpr (C8) {
-              const uint32_t w0 = kp[kt][p][2 * half], w1 = kp[kt][p][2 * half + 1];
-              kv[kt] = u32x4{e4m3_pair<false>(w0), e4m3_pair<true>(w0), e4m3_pair<false>(w1), e4m3_pair<true>(w1)};
-            }
-          }
-          const int at = C8 ? 128 * p + 32 * lg + 16 * half : 64 * p + 16 * lg;
-          product(0, kv, at);
-          if (TL::split(rot)) {
-            product(1, kv, at);
-            product(2, kv, at);
-          }
-        }
-      // the next unit's keys are on their way while this one's weights are summed
-      f32x4 bc[NKT], oc[NKT];
-      float sc[NKT];
-      int n[NKT];
-      float* to[NKT];
-#pragma unroll
-      for (int kt = 0; kt < NKT; ++kt) {
-        bc[kt] = bias[kt];
-        oc[kt] = old[kt];
-        sc[kt] = C8 ? a.scale * ks[C8 ? kt : 0] : a.scale;
-        n[kt] = nv[kt];
-        to[kt] = a.scores + row[kt] + 4 * lg;
-      }
-      load(next);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int kt = 0; kt < NKT; ++kt) {
-        if (n[kt] == 0) continue;
-        const int j1 = (int)j0 + 16 * kt;
-        float y[NR][4];
-#pragma unroll
-        for (int rt = 0; rt < NR; ++rt)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) y[rt][j] = exp_of<float>(fmaf(x[rt][kt][j], sc[kt], bc[kt][j]) - ref[rt]);
-        // rows that take no part, entries that a row does not see (whatever they hold)
-#pragma unroll
-        for (int rt = 0; rt < NR; ++rt)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            y[rt][j] = (j1 + 15 <= open ? ref[rt] != INFINITY : j1 + 4 * lg + j <= lim[rt]) ? y[rt][j] : 0.f;
-        f32x4 sum;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          sum[j] = y[0][j];
-#pragma unroll
-          for (int rt = 1; rt < NR; ++rt) sum[j] += y[rt][j];
-          sum[j] += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(sum[j]), 0x128, 0xF, 0xF, true));   // row_ror 8, 4, 2, 1
-          sum[j] += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(sum[j]), 0x124, 0xF, 0xF, true));
-          sum[j] += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(sum[j]), 0x122, 0xF, 0xF, true));
-          sum[j] += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(sum[j]), 0x121, 0xF, 0xF, true));
-          if (j1 + 4 * lg + j < known) sum[j] += oc[kt][j];
-        }
-        if (l == 0) {
-          if (n[kt] == 16) {
-            *(f32x4*)to[kt] = sum;
+        for (int kt = 0; kt < NKT; ++kt) {
+          if constexpr (TL::B16) {
+            x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kv[kt]),
+                                                                __builtin_bit_cast(bf16x8, qv), x[rt][kt], 0, 0, 0);
           } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (4 * lg + j < n[kt]) to[kt][j] = sum[j];
+            for (int e = 0; e < 4; ++e)
+              x[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kv[kt][e]), __uint_as_float(qv[e]),
+                                                               x[rt][kt], 0, 0, 0);
           }
         }
       }
-      cur = next;
+    };
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int half = 0; half < (C8 ? 2 : 1); ++half) {
+        u32x4 kv[NKT];
+#pragma unroll
+        for (int kt = 0; kt < NKT; ++kt) {
+          kv[kt] = kp[kt][p];
+          if constexpr (C8) {
+            const uint32_t w0 = kp[kt][p][2 * half], w1 = kp[kt][p][2 * half + 1];
+            kv[kt] = u32x4{e4m3_pair<false>(w0), e4m3_pair<true>(w0), e4m3_pair<false>(w1), e4m3_pair<true>(w1)};
+          }
+        }
+        const int at = C8 ? 128 * p + 32 * lg + 16 * half : 64 * p + 16 * lg;
+        product(0, kv, at);
+        if (TL::split(rot)) {
+          product(1, kv, at);
+          product(2, kv, at);
+        }
+      }
+    // the next unit's keys are on their way while this one's weights are summed
+    f32x4 bc[G], oc[G];
+    float sc[G], *dst[G];
+    int n[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      bc[g] = bias[g];
+      oc[g] = old[g];
+      sc[g] = C8 ? a.scale * ks[g] : a.scale;
+      n[g] = nv[g];
+      dst[g] = to[g];
+    }
+    load(next);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const int j1 = j0 + 16 * (g * PK + mine) + 4 * lg;   // the lane's first entry
+      f32x4 sum;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        sum[j] = 0.f;
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) {
+          uint32_t y = __float_as_uint(x[rt][g * PK][j]);
+          if constexpr (RP == 4) {   // lanes 0 .. 3 of a tile to those from 4, 8 and 12 on
+            if constexpr (PK >= 2) y = __builtin_amdgcn_update_dpp(y, __float_as_uint(x[rt][g * PK + 1][j]), 0x114, 0xF, 0x2, false);
+            if constexpr (PK >= 4) {
+              y = __builtin_amdgcn_update_dpp(y, __float_as_uint(x[rt][g * PK + 2][j]), 0x118, 0xF, 0x4, false);
+              y = __builtin_amdgcn_update_dpp(y, __float_as_uint(x[rt][g * PK + 3][j]), 0x11C, 0xF, 0x8, false);
+            }
+          }
+          if constexpr (RP == 8 && PK == 2) y = __builtin_amdgcn_update_dpp(y, __float_as_uint(x[rt][g * PK + 1][j]), 0x118, 0xF, 0xC, false);
+          const float e = exp_of<float>(fmaf(__uint_as_float(y), sc[g], bc[g][j]) - ref[rt]);
+          sum[j] += j1 + j <= lim[rt] ? e : 0.f;   // (whatever an entry holds that the row does not see)
+        }
+        sum[j] = rows_sum<LR>(sum[j]);
+        if (j1 + j < known) sum[j] += oc[g][j];
+      }
+      if (writes) {
+        if (n[g] == 16) {
+          *(f32x4*)dst[g] = sum;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (4 * lg + j < n[g]) dst[g][j] = sum[j];
+        }
+      }
+    }
+    cur = next;
   }
 }
 
