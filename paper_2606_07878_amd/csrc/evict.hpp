@@ -30,7 +30,7 @@ struct PagedScoreArgs {
   float scale;
 };
 
-constexpr int SCORE_CHUNK = 512;   // entries of a workgroup at a time
+constexpr int SCORE_CHUNK = 1024;   // entries of a workgroup at a time
 
 // RP: rows that fit a tile's lanes (4, 8, 16; 32: two tiles of rows).
 template <class IT, int D, int RP, class CT>

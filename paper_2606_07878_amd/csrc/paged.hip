@@ -57,7 +57,7 @@ size_t still_paged_attend_workspace_size(const still_paged_cache* cache, const s
     g_last_error = keep;
     return 0;
   }
-  return paged_plan(cache, cfg).total;
+  return paged_plan(cache, cfg, false).total;
 }
 
 still_status still_paged_attend(const still_paged_cache* cache, const still_paged_seqs* seqs,

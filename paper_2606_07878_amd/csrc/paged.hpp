@@ -304,10 +304,18 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // Parts of the line: waves per workgroup, workgroups resident on a CU, and
 // 16-entry tiles per chunk: 128 KB of keys and values in flight per CU (of width 64
 // half of that: its rate is the same, and short sequences take less).
+// 8 bits: a tile's arithmetic is that of 16 bits for half the bytes, so its waves wait
+// for each other more than for memory.  us of one sequence of 131136 entries, width 128,
+// with two waves per SIMD and 4 tiles 57 (the registers spill), 2 tiles 48, with three
+// waves and 2 tiles 51 (spilled); of width 256 with one wave and 4 tiles 107, 2 tiles 94, with
+// two and 2 tiles 85; 64 sequences of 5 to 16384 of width 64 with 2 tiles 44, 4 tiles 41.
 constexpr int paged_waves(int esize, int D, int NR) { return NR == 2 && D <= 128 && esize == 4 ? 8 : 4; }
-constexpr int paged_resident(int D, int NR) { return NR == 1 && D <= 128 ? 2 : 1; }
+constexpr int paged_resident(int esize, int D, int NR) {
+  return esize == 1 ? (NR == 1 || D <= 128 ? 2 : 1) : NR == 1 && D <= 128 ? 2 : 1;
+}
 constexpr int paged_tiles(int esize, int D, int NR) {
-  return std::min(8, (NR == 1 && D == 64 ? 64 : 128) * 1024 / (paged_waves(esize, D, NR) * paged_resident(D, NR) * 32 * D * esize));
+  if (esize == 1) return D == 64 ? 4 : 2;
+  return (NR == 1 && D == 64 ? 64 : 128) * 1024 / (paged_waves(esize, D, NR) * paged_resident(esize, D, NR) * 32 * D * esize);
 }
 // Whole sequences: waves per workgroup (two per SIMD, or as the registers allow).
 constexpr int paged_team(int D, int NR) { return NR == 1 && D <= 128 ? 8 : 4; }
@@ -324,7 +332,7 @@ template <class IT, int D, int NR, int SW, class CT = IT>
 struct PagedTile {
   static constexpr bool C8 = sizeof(CT) == 1, B16 = C8 || sizeof(IT) == 2;   // B16: products of bf16
   static constexpr int NW = SW > 0 ? SW : paged_waves(sizeof(CT), D, NR);
-  static constexpr int PER_SIMD = SW == 1 ? (D <= 128 ? 2 : 1) : NW * (SW > 0 ? 1 : paged_resident(D, NR)) / 4;
+  static constexpr int PER_SIMD = SW == 1 ? (D <= 128 ? 2 : 1) : NW * (SW > 0 ? 1 : paged_resident(sizeof(CT), D, NR)) / 4;
   static constexpr int NKT = SW > 0 ? (B16 ? 2 : 1) : paged_tiles(sizeof(CT), D, NR);   // 16-entry tiles per chunk
   static constexpr int CH = 16 * NKT;
   static constexpr int AUX = SW < 0 ? 2 : 0;            // cache policy of the entries' loads: 2 non-temporal
@@ -344,14 +352,14 @@ struct PagedTile {
 // waves' sums [waves][R][OROW] or, before there are any, the queries' angles
 // [nq][D / 2].  The sums take the rows' place where both do not fit 160 KB, and in
 // workgroups of one wave, many of which share a CU.
-constexpr bool paged_alias(int D, int NR, int SW) { return SW == 1 || D * NR > 256; }
+constexpr bool paged_alias(int esize, int D, int NR, int SW) { return SW == 1 || D * NR > (esize == 1 ? 128 : 256); }
 template <class TL>
 inline __host__ __device__ int paged_q_bytes(bool rot) { return (TL::split(rot) ? 3 : 1) * TL::QPART; }
-template <class TL, int D, int NR, int SW>
+template <class TL, int esize, int D, int NR, int SW>
 inline size_t paged_lds_bytes(int R, int nq, bool rot) {
   const size_t q = paged_q_bytes<TL>(rot), o = (size_t)TL::NW * R * TL::OROW * sizeof(float);
   const size_t angles = rot ? (size_t)nq * D / 2 * sizeof(float2) : 0;
-  return paged_alias(D, NR, SW) ? std::max(q + angles, o) : q + std::max(angles, o);
+  return paged_alias(esize, D, NR, SW) ? std::max(q + angles, o) : q + std::max(angles, o);
 }
 
 // x as the sum of three bf16: each takes the leading 8 bits of what the ones before
@@ -456,7 +464,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
   constexpr bool SINGLE = SW > 0, C8 = TL::C8;
   constexpr int NKT = TL::NKT, CH = TL::CH, NP = TL::NP, FPT = TL::FPT, VB = TL::VB, ROWB = TL::ROWB, NW = TL::NW;
   constexpr int QROW = TL::QROW, OROW = TL::OROW, NT = 64 * NW, HD = D / 2;
-  constexpr bool ALIAS = paged_alias(D, NR, SW);
+  constexpr bool ALIAS = paged_alias(sizeof(CT), D, NR, SW);
   extern __shared__ float4 paged_smem[];
   char* qs = (char*)paged_smem;                  // [16 NR][QROW], rotated bf16 rows: three parts of that
   __shared__ float wm[NW][16 * NR], wl[NW][16 * NR];
@@ -479,9 +487,16 @@ void paged_attend_kernel(PagedAttendArgs a) {
   // (of 8 values where they end up as bf16)
   constexpr int EPP = TL::B16 ? 8 : 4, NV = EPP * (int)sizeof(IT) / 16, HP = HD / EPP, QI = (16 * NR * HP + NT - 1) / NT;
   u32x4 qr[QI][2][NV];
+  // this thread, where it is wanted once a sequence (8 bits: no register is kept for what comes of it)
+  auto self = [&] {
+    int t = tid;
+    if constexpr (C8) asm volatile("" : "+v"(t));
+    return t;
+  };
   // a thread's angles belong to one pair where the threads are a multiple of the pairs
   const double inv_freq = rot ? exp2(a.log2_theta * (-2.0 * (tid % HD) / D)) : 0.0;
   auto load_q = [&](int s) {
+    const int tid = self();
 #pragma unroll
     for (int k = 0; k < QI; ++k) {
       const int e = k * NT + tid, r = min(e / HP, R - 1), hr = head_of(r);   // (rows past R repeat the last one)
@@ -494,6 +509,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
     }
   };
   auto stage_q = [&](int s) {   // rotated, in LDS; ends with a barrier
+    const int tid = self();
     if (rot) {
       for (int e = tid; e < a.nq * HD; e += NT)
         cs[e] = rope_cs(a.qpos[(long)s * a.nq + e / HD],
@@ -577,7 +593,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
     }
     cuts(__builtin_amdgcn_readlane(lanes_scan(n), 63), __builtin_amdgcn_readlane(lanes_scan(some), 63));
   }
-  int4 goes_on = make_int4(-1, 0, 0, 0);
+  if (!SINGLE && h == 0 && tid == 0 && !a.by_seq) a.plan[g] = make_int4(-1, 0, 0, 0);   // (overwritten by the same thread)
   int line = 0, padded = 0;   // chunks in front of the round, without and with pads
   for (int base = SINGLE ? blockIdx.y : 0; base < n_seqs; base += PAGED_ROUND) {
     const int cnt = SINGLE ? 1 : min(PAGED_ROUND, n_seqs - base);
@@ -681,8 +697,8 @@ void paged_attend_kernel(PagedAttendArgs a) {
     f32x4 bias[NKT];
     float ks[C8 ? NKT : 1], vs[C8 ? NKT : 1];   // scales of the tiles' keys and values
     auto scale_of = [&](const float* scales, const Tiles& k, int kt) {   // (of a tile without entries: 0)
-      return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(
-                                           paged_rows(scales + k.row[kt] / PAGED_BLOCK, k.nv[kt] > 0 ? 4 : 0), 0, 0, 0));
+      const float x = scalar_load(scales, k.row[kt] / PAGED_BLOCK);
+      return k.nv[kt] > 0 ? x : 0.f;
     };
     uint32_t vr[NKT * 4][VB / 4];
     // (the offsets are opaque to the compiler, which would keep every sum of one with
@@ -719,7 +735,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
         locate(cur_chunk, u);
         locate(nxt, u + NW);
       } else {
-        load_q(base + i);
+        if (!C8) load_q(base + i);   // (8 bits: behind the entries, which leave no registers for them)
         cur_chunk = lookup(u);
         nxt = lookup(u + NW);
       }
@@ -728,6 +744,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
       __builtin_amdgcn_sched_barrier(0);   // (loads stay in this order: their waits count the ones behind)
       load_v(cur);
       __builtin_amdgcn_sched_barrier(0);
+      if (C8 && !SINGLE) load_q(base + i);
       while (true) {   // the part's sequences that have entries
         const int len = len_of(i), s0 = SINGLE ? 0 : list_get(first, i), s1 = s0 + chunks(len);
         const int s = base + i, end = min(s1, hi);
@@ -789,6 +806,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
                   product(1, p, kv, 128 * p + 32 * lg + 16 * half);
                   product(2, p, kv, 128 * p + 32 * lg + 16 * half);
                 }
+                __builtin_amdgcn_sched_barrier(0);
               }
           } else {
             auto all = [&](int part) {
@@ -806,12 +824,20 @@ void paged_attend_kernel(PagedAttendArgs a) {
               all(2);
             }
           }
-          f32x4 bc[NKT];
+          f32x4 bc[C8 ? 1 : NKT];
+          if constexpr (C8) {   // (at once: registers for copies of bias and scales are short here)
 #pragma unroll
-          for (int kt = 0; kt < NKT; ++kt) bc[kt] = bias[kt];
-          float kc[NKT];   // a tile's logit scale
+            for (int kt = 0; kt < NKT; ++kt) {
+              const float kc = a.scale * ks[kt];
 #pragma unroll
-          for (int kt = 0; kt < NKT; ++kt) kc[kt] = C8 ? a.scale * ks[C8 ? kt : 0] : a.scale;
+              for (int rt = 0; rt < NR; ++rt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[rt][kt][j] = fmaf(x[rt][kt][j], kc, bias[kt][j]);
+            }
+          } else {
+#pragma unroll
+            for (int kt = 0; kt < NKT; ++kt) bc[kt] = bias[kt];
+          }
           const Tiles next = resolve(nxt);
           load_k(next);
           __builtin_amdgcn_sched_barrier(0);
@@ -824,10 +850,12 @@ void paged_attend_kernel(PagedAttendArgs a) {
           bool grows = false;
 #pragma unroll
           for (int rt = 0; rt < NR; ++rt) {
+            if constexpr (!C8) {
 #pragma unroll
-            for (int kt = 0; kt < NKT; ++kt)
+              for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) x[rt][kt][j] = fmaf(x[rt][kt][j], kc[kt], bc[kt][j]);
+                for (int j = 0; j < 4; ++j) x[rt][kt][j] = fmaf(x[rt][kt][j], a.scale, bc[kt][j]);
+            }
             if (!full) {
 #pragma unroll
               for (int kt = 0; kt < NKT; ++kt) {
@@ -903,6 +931,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
                   }
 #pragma unroll
                   for (int k = 0; k < 4; ++k) into(e + k, t[k]);
+                  __builtin_amdgcn_sched_barrier(0);   // (operands formed ahead would take registers that are not there)
                 }
                 continue;
               }
@@ -951,6 +980,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
           ls[rt] += __shfl_xor(ls[rt], 32);
         }
         if (ALIAS) __syncthreads();   // every wave has read the query rows
+        const int l = self() & 15, lg = self() >> 4 & 3;
 #pragma unroll
         for (int rt = 0; rt < NR; ++rt) {
           const int r = 16 * rt + l;
@@ -971,7 +1001,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
         __syncthreads();   // (also: every wave has read the query rows)
         const bool starts = at == s0, whole = SINGLE || (starts && end == s1);
         const long slot = ((long)h * a.G + g) * 2 + (starts ? 1 : 0);
-        for (int e = tid; e < R * (D / 4); e += NT) {
+        for (int e = self(); e < R * (D / 4); e += NT) {
           const int r = e / (D / 4), x = e % (D / 4) * 4;
           float M = wm[0][r];
 #pragma unroll
@@ -1006,12 +1036,7 @@ void paged_attend_kernel(PagedAttendArgs a) {
           const int v = list_get(padded_first, i) + pad + s1 - s0;   // behind its last chunk
           // the workgroup of place v - 1
           const int to = v <= more * (share + 1) ? (v - 1) / (share + 1) : more + (v - 1 - more * (share + 1)) / share;
-          const int4 p = whole ? make_int4(-1, 0, 0, 0) : make_int4(s, g, to, 0);
-          if (a.by_seq) {
-            if (h == 0 && tid == 0) a.plan[s] = p;
-          } else if (!whole) {
-            goes_on = p;
-          }
+          if (h == 0 && tid == 0 && (a.by_seq || !whole)) a.plan[a.by_seq ? s : g] = whole ? make_int4(-1, 0, 0, 0) : make_int4(s, g, to, 0);
         }
         if (last) break;
         i = ni;
@@ -1022,7 +1047,6 @@ void paged_attend_kernel(PagedAttendArgs a) {
     if (SINGLE) break;
     __syncthreads();   // the last sequence's sums have been read
   }
-  if (!SINGLE && h == 0 && tid == 0 && !a.by_seq) a.plan[g] = goes_on;
 }
 
 // Joins the partial sums of the sequences that lie in several parts: block

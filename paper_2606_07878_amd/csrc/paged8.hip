@@ -91,7 +91,12 @@ still_status still_paged8_gather(const still_paged8_cache* cache, const still_pa
 size_t still_paged8_attend_workspace_size(const still_paged8_cache* cache, const still_paged_attend_config* cfg) {
   if (!cache) return 0;
   const still_paged_cache c = plain_view(cache);
-  return still_paged_attend_workspace_size(&c, cfg);
+  const std::string keep = g_last_error;
+  if (check_attend(&c, cfg) != STILL_OK) {
+    g_last_error = keep;
+    return 0;
+  }
+  return paged_plan(&c, cfg, true).total;
 }
 
 still_status still_paged8_attend(const still_paged8_cache* cache, const still_paged_seqs* seqs,

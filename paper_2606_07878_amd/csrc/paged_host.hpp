@@ -137,10 +137,10 @@ struct PagedPlan {
   size_t opart, mpart, lpart, total;   // offsets behind the plan, bytes
 };
 
-inline PagedPlan paged_plan(const still_paged_cache* c, const still_paged_attend_config* f) {
+inline PagedPlan paged_plan(const still_paged_cache* c, const still_paged_attend_config* f, bool eight) {
   PagedPlan p;
   // workgroups per KV head: as many as are resident at once
-  p.G = std::max(1, 256 * paged_resident(c->head_dim, f->group * f->n_queries <= 16 ? 1 : 2) / c->n_kv_heads);
+  p.G = std::max(1, 256 * paged_resident(eight ? 1 : c->mode == STILL_MODE_FP32 ? 4 : 2, c->head_dim, f->group * f->n_queries <= 16 ? 1 : 2) / c->n_kv_heads);
   const size_t slots = p.G == 1 ? 0 : (size_t)c->n_kv_heads * p.G * 2 * f->group * f->n_queries;   // one part: no joins
   p.opart = (size_t)rup(p.G * (long)sizeof(int4), 256);
   p.mpart = p.opart + slots * c->head_dim * sizeof(float);
@@ -221,7 +221,7 @@ still_status paged_attend_call(const still_paged_cache* cache, const float* ks, 
     return s;
   if ((uintptr_t)lse & 3u) return fail(STILL_E_INVAL, "lse is not 4-byte aligned");
   if (!workspace) return fail(STILL_E_WORKSPACE, "workspace is NULL");
-  const PagedPlan p = paged_plan(cache, cfg);
+  const PagedPlan p = paged_plan(cache, cfg, C8);
   if (workspace_bytes < p.total)
     return fail(STILL_E_WORKSPACE, "workspace of %zu bytes, need %zu", workspace_bytes, p.total);
   char* ws = (char*)(((uintptr_t)workspace + 255) & ~(uintptr_t)255);
@@ -258,7 +258,7 @@ still_status paged_attend_call(const still_paged_cache* cache, const float* ks, 
       constexpr int NR = decltype(nr)::value, SW = decltype(sw)::value;
       using TL = PagedTile<IT, D, NR, SW, CT>;
       hipLaunchKernelGGL((paged_attend_kernel<IT, D, NR, SW, CT>), dim3(a.c.H, SW > 0 ? a.c.n_seqs : a.G), dim3(64 * TL::NW),
-                         (paged_lds_bytes<TL, D, NR, SW>(R, a.nq, a.qpos != nullptr)), st, a);
+                         (paged_lds_bytes<TL, sizeof(CT), D, NR, SW>(R, a.nq, a.qpos != nullptr)), st, a);
     };
     using One = std::integral_constant<int, 1>;
     using Two = std::integral_constant<int, 2>;
