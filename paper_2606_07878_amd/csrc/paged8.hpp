@@ -20,12 +20,10 @@ __device__ __forceinline__ float e4m3_scale(float top) {
   return __uint_as_float((uint32_t)max(e, 127 - 100) << 23);
 }
 
-// Four floats as codes, rounded to nearest even; infinities and NaN (e4m3 has no
-// infinity) as NaN.
+// Four floats of up to 448 as codes, rounded to nearest even; NaN as NaN.
 __device__ __forceinline__ uint32_t e4m3_codes(float a, float b, float c, float d) {
-  auto fine = [](float x) { return fabsf(x) < INFINITY ? x : NAN; };
-  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(fine(a), fine(b), 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(fine(c), fine(d), lo, true);
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
 }
 __device__ __forceinline__ void e4m3_floats(uint32_t w, float (&f)[4]) {
   const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
@@ -83,7 +81,7 @@ struct Append8Args {
 };
 
 template <class IT, int D, int TG>
-__global__ __launch_bounds__(256) void paged8_append_kernel(Append8Args p) {
+__global__ __launch_bounds__(256, 3) void paged8_append_kernel(Append8Args p) {
   constexpr int HD = D / 2, IPR = HD / 8, RPS = 64 / IPR, ST = PAGED_BLOCK / RPS, NV = sizeof(IT) / 2;
   const PagedAppendArgs& a = p.t;
   __shared__ double2 cs[PAGED_BLOCK][HD];
@@ -134,6 +132,7 @@ __global__ __launch_bounds__(256) void paged8_append_kernel(Append8Args p) {
       }
     }
   }
+  const double inv_freq = a.pos ? exp2(a.log2_theta * (-2.0 * (tid % HD) / D)) : 0.0;   // of this thread's angles
   unsigned long leaders = __ballot(count > 0);
   while (leaders) {
     const int t = __builtin_ctzll(leaders);
@@ -144,7 +143,7 @@ __global__ __launch_bounds__(256) void paged8_append_kernel(Append8Args p) {
     if (a.pos) {
       __syncthreads();   // the block before has been rotated
       for (int e = tid; e < n * HD; e += 256)
-        cs[e / HD][e % HD] = rope_cs64(a.pos[first + e / HD], exp2(a.log2_theta * (-2.0 * (e % HD) / D)));
+        cs[e / HD][e % HD] = rope_cs64(a.pos[first + e / HD], inv_freq);
       __syncthreads();
     }
     for (int u = 2 * h0 + w; u < 2 * h1; u += 4) {
@@ -186,14 +185,25 @@ __global__ __launch_bounds__(256) void paged8_append_kernel(Append8Args p) {
               x[k][8 + e] = (float)(x1 * z.x + x0 * z.y);
             }
         }
-      float top = 0.f;
+      auto largest = [&] {   // (a maximum leaves NaN out)
+        float top = 0.f;
 #pragma unroll
-      for (int k = 0; k < ST; ++k)
-        if (k * RPS + r0 < n)
+        for (int k = 0; k < ST; ++k)
+          if (k * RPS + r0 < n)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(x[k][e]) < INFINITY ? fabsf(x[k][e]) : 0.f);
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(x[k][e]));
 #pragma unroll
-      for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+        for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+        return top;
+      };
+      float top = largest();
+      if (uniform(__float_as_uint(top)) == 0x7f800000u) {   // infinities are held as NaN
+#pragma unroll
+        for (int k = 0; k < ST; ++k)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[k][e] = fabsf(x[k][e]) < INFINITY ? x[k][e] : NAN;
+        top = largest();
+      }
       const float need = e4m3_scale(top);
       const float now = old && !(need > before) ? before : need, inv = 1.f / now;
       char* codes = (kv ? a.c.v : a.c.k) + row * D;
@@ -222,7 +232,7 @@ __global__ __launch_bounds__(256) void paged8_append_kernel(Append8Args p) {
             u32x2 y;
             y.x = e4m3_codes(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
             y.y = e4m3_codes(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv);
-            *(u32x2*)(codes + r * D + half * HD + c * 8) = y;
+            __builtin_nontemporal_store(y, (u32x2*)(codes + r * D + half * HD + c * 8));
           }
         }
       }
