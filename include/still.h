@@ -422,7 +422,7 @@ still_status still_paged_attend_lse(const still_paged_cache *cache, const still_
  *
  * Entries are OCP e4m3 codes (4 exponent bits, 3 fraction bits, largest 448, no
  * infinity), and blocks of 16 entries (slots 16 b .. 16 b + 15 of a page) of a head
- * share a float scale: an entry's key stands for its codes times k_scale of its
+ * share a positive float scale: an entry's key stands for its codes times k_scale of its
  * block, its value for its codes times v_scale.  The append makes scales that are
  * powers of two; the calls that read take any.  Sequences, tables, lengths and
  * absent pages as above.
@@ -485,7 +485,7 @@ still_status still_paged8_score(const still_paged8_cache *cache, const still_pag
                                 const float *lse, const int32_t *known, float *scores, void *stream);
 
 typedef struct {
-  int32_t keep;     /* entries that a sequence keeps at most, >= 1                         */
+  int32_t keep;     /* entries that a sequence keeps at most, 1 .. 2^30                    */
   int32_t first;    /* of them: its first ones, whatever their scores, >= 0                */
   int32_t recent;   /* and its last ones, >= 0; first + recent <= keep                     */
   int32_t shared;   /* 0: every KV head keeps its own entries; 1: all heads the same, by
@@ -537,8 +537,9 @@ enum {
   STILL_K_REFINE = 3,       /* exact-logit refinement of the top keys         */
   STILL_K_LATENT = 4,       /* latent-side GEMMs (V/O proj, self-attn, FFN, heads) */
   STILL_K_OTHER = 5,        /* norms, softmax, merge, tables, conversions, beta,
-                               paged append and gather                         */
-  STILL_K_ATTEND = 6,       /* consumer attention (dense and paged), its merge   */
+                               paged append, gather and eviction               */
+  STILL_K_ATTEND = 6,       /* consumer attention (dense and paged), its merge,
+                               the entries' scores                             */
   STILL_K_STAGE = 7,        /* RoPE-fix staging of X, X^T: the KV-cache stream */
   STILL_K_COUNT = 8
 };

@@ -72,6 +72,7 @@ static still_status check_evict(const still_paged_cache* cache, const still_page
   if (!cfg) return fail(STILL_E_INVAL, "paged evict config is NULL");
   if (cfg->keep < 1 || cfg->first < 0 || cfg->recent < 0 || (long)cfg->first + cfg->recent > cfg->keep)
     return fail(STILL_E_SHAPE, "keep %d must be >= 1 and hold first %d and recent %d", cfg->keep, cfg->first, cfg->recent);
+  if (cfg->keep > 1 << 30) return fail(STILL_E_UNSUPPORTED, "keep above 2^30, more than a table holds");
   if (cfg->shared != 0 && cfg->shared != 1) return fail(STILL_E_INVAL, "shared must be 0 or 1");
   return STILL_OK;
 }

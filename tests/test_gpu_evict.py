@@ -70,7 +70,7 @@ def check_score(c, q, kind, causal=False, scale=0.0, qpos=None, theta=0.0, beta=
 
 @pytest.mark.parametrize("kind,mode", [(BF16, BF16), (FP32, FP32), (E8, BF16), (E8, FP32)])
 @pytest.mark.parametrize("d", [64, 128, 256])
-@pytest.mark.parametrize("group,nq", [(1, 1), (4, 1), (3, 5), (8, 4), (17, 1), (1, 32)])
+@pytest.mark.parametrize("group,nq", [(1, 1), (2, 1), (4, 1), (1, 3), (5, 1), (2, 4), (7, 1), (3, 3), (3, 5), (8, 4), (17, 1), (1, 32)])
 def test_score_rows_and_widths(kind, mode, d, group, nq):
     log(f"score kind={kind} mode={mode} d={d} group={group} nq={nq}")
     c = Paged8(50, [1200, 77, 0, 3], 2, d, 32)

@@ -112,6 +112,15 @@ def test_attend_pointers_workspace_and_nothing_to_do():
     assert binding.still_paged8_gather(_cache8(), _seqs(), 0, 0, 0, None, None, None, None) == 0
 
 
+@pytest.mark.parametrize("H", [1, 2, 3, 8, 64, 300, 65535])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_one_workspace_serves_every_call(H, d):
+    for mode in (configs.MODE_BF16, configs.MODE_FP32):
+        for rows in (1, 16, 17, 32):
+            need = binding.still_paged8_attend_workspace_size(_cache8(n_kv_heads=H, head_dim=d, mode=mode), _acfg(group=rows))
+            assert 0 < need <= binding.STILL_PAGED_WORKSPACE_BYTES
+
+
 def test_null_structs():
     lib, c, s = binding.lib(), ctypes.byref(_cache8()), ctypes.byref(_seqs())
     assert lib.still_paged8_append(None, s, ctypes.byref(_tokens()), None) == -1
@@ -197,7 +206,8 @@ def test_score_and_evict_refuse(make):
     for kw in (dict(scores=None), dict(scores=FAKE + 8), dict(kept=None), dict(kept=FAKE + 2), dict(new_lens=None), dict(new_lens=FAKE + 3)):
         assert _evict(cache=make(), **kw) == -1
     for kw, status in ((dict(keep=0), -2), (dict(keep=-5), -2), (dict(first=-1), -2), (dict(recent=-1), -2),
-                       (dict(first=50, recent=15), -2), (dict(first=2 ** 31 - 1, recent=2 ** 31 - 1), -2), (dict(shared=2), -1)):
+                       (dict(first=50, recent=15), -2), (dict(first=2 ** 31 - 1, recent=2 ** 31 - 1), -2), (dict(shared=2), -1),
+                       (dict(keep=2 ** 30 + 1), -5), (dict(keep=2 ** 31 - 1), -5)):
         assert _evict(cache=make(), cfg=_ecfg(**kw)) == status
 
 
