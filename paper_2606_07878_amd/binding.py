@@ -688,14 +688,18 @@ def _on(torch, dev: int, call, *args) -> None:
 
 def _tokens(torch, k, v, k_pages, dtype, cache, seqs, dev, offsets, positions, rope_theta, beta):
     """C view of rows k, v of this type to append, checked."""
-    if k.dim() != 3:
+    size = k.shape
+    if len(size) != 3:
         _refuse(-2, f"k has {k.dim()} dimensions, not [n_tokens, H, d]")
-    n = k.shape[0]
+    n = size[0]
     if n >= 1 << 31:
         _refuse(-2, f"{n} tokens given")
     shape = (n, cache.n_kv_heads, cache.head_dim)
-    _want_rows(k, "k", k_pages, shape, dtype)
-    _want_rows(v, "v", k_pages, shape, dtype)
+    # one expression, as before every call of a decode step
+    if not (size == shape and v.shape == size and k.dtype is dtype and v.dtype is dtype and k.stride(2) == 1
+            and v.stride(2) == 1 and k.get_device() == dev and v.get_device() == dev):
+        _want_rows(k, "k", k_pages, shape, dtype)
+        _want_rows(v, "v", k_pages, shape, dtype)
     off = pos = b = None
     if offsets is not None:
         _want(offsets, "offsets", torch.int32, (seqs.n_seqs + 1,), dev)
@@ -860,7 +864,7 @@ def _paged8(torch, k_pages, v_pages, k_scales, v_scales, beta_pages, table, lens
             and v_pages.dtype is dt and v_pages.shape == shape and k_pages.is_contiguous() and v_pages.is_contiguous()
             and v_pages.get_device() == dev and table.dtype is i32 and len(size) == 2 and lens.dtype is i32
             and k_scales.dtype is f32 and v_scales.dtype is f32
-            and k_scales.shape == v_scales.shape == (shape[0], shape[1], shape[2] // 16)
+            and k_scales.shape == v_scales.shape == (shape[0], shape[1], shape[2] >> 4)
             and k_scales.is_contiguous() and v_scales.is_contiguous()
             and k_scales.get_device() == dev and v_scales.get_device() == dev
             and lens.shape == size[:1] and lens.is_contiguous() and lens.get_device() == dev
