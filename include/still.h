@@ -504,7 +504,7 @@ typedef struct {
  *             -1 behind them
  *   new_lens  [n_seqs] int32: the lengths behind the call; may be seqs->lens
  *   workspace still_paged_evict_workspace_size bytes (16-byte aligned; NULL where that is 0), for
- *             caches of 8 bits too (of the same dimensions); at most 64 MiB, nothing for tables
+ *             caches of 8 bits too (of the same dimensions); at most 96 MiB, nothing for tables
  *             of up to 8192 entries
  * The pages that the sequences name must be distinct. */
 size_t still_paged_evict_workspace_size(const still_paged_cache *cache, const still_paged_seqs *seqs,

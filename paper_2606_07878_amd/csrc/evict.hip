@@ -77,11 +77,23 @@ static still_status check_evict(const still_paged_cache* cache, const still_page
   return STILL_OK;
 }
 
-// Keys of a list in the workspace, where they are formed ahead; 0 where a list's workgroup
-// forms its own.
-static long evict_keys(const still_paged_cache* c, const still_paged_seqs* q, const still_paged_evict_config* f) {
-  const long cap = (long)q->max_pages * c->page_size, lists = (long)q->n_seqs * (f->shared ? 1 : c->n_kv_heads);
-  return cap > 8192 && lists <= 64 && lists * cap <= 1L << 24 ? cap : 0;
+// The workspace: keys of lists that are formed ahead, and counts of their parts; none where
+// a list's workgroup forms its own.
+struct EvictPlan {
+  long lists, kstride = 0;
+  int kblocks = 0, kpart = 0;
+  size_t total = 0;
+};
+static EvictPlan evict_plan(const still_paged_cache* c, const still_paged_seqs* q, const still_paged_evict_config* f) {
+  EvictPlan p;
+  const long cap = (long)q->max_pages * c->page_size;
+  p.lists = (long)q->n_seqs * (f->shared ? 1 : c->n_kv_heads);
+  if (cap <= 8192 || p.lists > 64 || p.lists * cap > 1L << 24) return p;
+  p.kstride = cap;
+  p.kpart = (int)rup((cap + 63) / 64, 4096);   // 64 parts at most
+  p.kblocks = (int)((cap + p.kpart - 1) / p.kpart);
+  p.total = p.lists * (cap * sizeof(uint32_t) + p.kblocks * SELECT_BINS * sizeof(int));
+  return p;
 }
 
 // ks, vs: scales of pages of 8 bits, else NULL.
@@ -93,8 +105,8 @@ static still_status paged_evict_call(const still_paged_cache* cache, float* ks, 
   if ((s = check_pages(cache)) != STILL_OK || (s = check_ptr(scores, "scores", true)) != STILL_OK) return s;
   if (!kept || !new_lens || ((uintptr_t)kept & 3u) || ((uintptr_t)new_lens & 3u))
     return fail(STILL_E_INVAL, "kept or new_lens is NULL or not 4-byte aligned");
-  const int lists = seqs->n_seqs * (cfg->shared ? 1 : cache->n_kv_heads);
-  const size_t need = (size_t)lists * evict_keys(cache, seqs, cfg) * sizeof(uint32_t);
+  const EvictPlan plan = evict_plan(cache, seqs, cfg);
+  const size_t need = plan.total;
   if (need && !workspace) return fail(STILL_E_WORKSPACE, "workspace is NULL");
   if (need && (s = check_ptr(workspace, "workspace", true)) != STILL_OK) return s;
   if (workspace_bytes < need) return fail(STILL_E_WORKSPACE, "workspace of %zu bytes, need %zu", workspace_bytes, need);
@@ -117,16 +129,19 @@ static still_status paged_evict_call(const still_paged_cache* cache, float* ks, 
   const int per_seq = cfg->shared ? 1 : H;
   const dim3 grid_of(per_seq, n_seqs);
   a.keys = (uint32_t*)workspace;
-  a.kstride = evict_keys(cache, seqs, cfg);
+  a.kstride = plan.kstride;
+  a.bins = (int*)(a.keys + plan.lists * plan.kstride);
+  a.kblocks = plan.kblocks;
+  a.kpart = plan.kpart;
   if (a.kstride) {
-    hipLaunchKernelGGL(paged_keys_kernel, dim3(std::min(512L, (cap + 1023) / 1024), per_seq, n_seqs), dim3(256), 0, st, a);
-    hipLaunchKernelGGL((paged_select_kernel<1024, 64, true>), grid_of, dim3(1024), 0, st, a);
+    hipLaunchKernelGGL(paged_keys_kernel, dim3(a.kblocks, per_seq, n_seqs), dim3(1024), 0, st, a);
+    hipLaunchKernelGGL((paged_select_kernel<1024, 16, true>), grid_of, dim3(1024), 0, st, a);
   } else if (cap <= 2048) {
     hipLaunchKernelGGL((paged_select_kernel<256, 8, false>), grid_of, dim3(256), 0, st, a);
   } else if (cap <= 8192) {
     hipLaunchKernelGGL((paged_select_kernel<512, 16, false>), grid_of, dim3(512), 0, st, a);
   } else {
-    hipLaunchKernelGGL((paged_select_kernel<1024, 32, false>), grid_of, dim3(1024), 0, st, a);
+    hipLaunchKernelGGL((paged_select_kernel<1024, 16, false>), grid_of, dim3(1024), 0, st, a);
   }
   HIP_TRY(hipGetLastError());
   const bool few = (long)H * n_seqs <= 64;
@@ -191,7 +206,7 @@ size_t still_paged_evict_workspace_size(const still_paged_cache* cache, const st
     g_last_error = keep;
     return 0;
   }
-  return (size_t)seqs->n_seqs * (cfg->shared ? 1 : cache->n_kv_heads) * evict_keys(cache, seqs, cfg) * sizeof(uint32_t);
+  return evict_plan(cache, seqs, cfg).total;
 }
 
 still_status still_paged8_evict(const still_paged8_cache* cache, const still_paged_seqs* seqs,

@@ -300,7 +300,9 @@ __global__ __launch_bounds__(256) void paged_score_kernel(PagedScoreArgs a) {
 // first and the recent ones stay and the m largest scores between them: the m-th
 // largest key is found 11, 11 and 10 bits at a time by counting, then the entries
 // above it, and those equal to it until there are enough, are listed in order.
-// T threads hold up to K keys each; a list that is longer is read again for every step.
+// T threads hold up to K keys each; a list that is longer is read again for every step.  That
+// costs less than keys of 65536 entries in registers: code for 64 of them, run once, waits for
+// its instructions (34 us with 64 a thread, 27 with 16, 29 with 8).
 // Long lists' counts are kept four times over (lane mod 4): most scores share a few
 // exponents, and a count that many lanes raise at once takes them one by one.
 // ---------------------------------------------------------------------------
@@ -312,7 +314,10 @@ struct PagedEvictArgs {
   int keep, first, recent, shared;
   uint32_t* keys;       // [lists][kstride] or NULL
   long kstride;
+  int* bins;            // [lists][kblocks][SELECT_BINS]: how many keys of each part start with these bits
+  int kblocks, kpart;   // a list's parts, entries of one (a multiple of 4096)
 };
+constexpr int SELECT_BINS = 2048;
 
 // the order of numbers as that of whole ones; NaN as minus infinity, -0 as 0
 __device__ __forceinline__ uint32_t score_key(float x) {
@@ -320,13 +325,16 @@ __device__ __forceinline__ uint32_t score_key(float x) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// Few long lists: their keys by the whole chip first, four entries a thread; 0 for those that
-// are not chosen from.
-__global__ __launch_bounds__(256) void paged_keys_kernel(PagedEvictArgs a) {
-  const int g = blockIdx.y, s = blockIdx.z, n = paged_len(a.c, s);
-  if (n <= a.keep) return;
-  uint32_t* keys = a.keys + ((long)s * gridDim.y + g) * a.kstride;
-  for (long j = ((long)blockIdx.x * 256 + threadIdx.x) * 4; j < n; j += (long)gridDim.x * 1024) {
+// Few long lists: their keys by the whole chip first, four entries a thread, 0 for those that
+// are not chosen from; and the first counting step, part by part.
+__global__ __launch_bounds__(1024) void paged_keys_kernel(PagedEvictArgs a) {
+  __shared__ int count[4 * SELECT_BINS];
+  const int g = blockIdx.y, s = blockIdx.z, n = paged_len(a.c, s), tid = threadIdx.x;
+  const long j0 = (long)blockIdx.x * a.kpart, j1 = min((long)n, j0 + a.kpart), list = (long)s * gridDim.y + g;
+  if (n <= a.keep || j0 >= n) return;
+  for (int i = tid; i < SELECT_BINS; i += 1024) ((int4*)count)[i] = make_int4(0, 0, 0, 0);
+  __syncthreads();
+  for (long j = j0 + 4 * tid; j < j1; j += 4096) {
     const int p = paged_page(a.c, s, j);
     f32x4 x = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
     if (p >= 0 && !a.shared) x = *(const f32x4*)(a.scores + paged_row(a.c, p, g, j));
@@ -343,16 +351,28 @@ __global__ __launch_bounds__(256) void paged_keys_kernel(PagedEvictArgs a) {
     }
     u32x4 k;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) k[i] = j + i >= a.first && j + i < n - a.recent ? score_key(x[i]) : 0;
-    *(u32x4*)(keys + j) = k;
+    for (int i = 0; i < 4; ++i) {
+      k[i] = j + i >= a.first && j + i < n - a.recent ? score_key(x[i]) : 0;
+      if (k[i]) atomicAdd(&count[(k[i] >> 21) * 4 + tid % 4], 1);
+    }
+    *(u32x4*)(a.keys + list * a.kstride + j) = k;
+  }
+  __syncthreads();
+  int* out = a.bins + (list * a.kblocks + blockIdx.x) * SELECT_BINS;
+  for (int i = tid; i < SELECT_BINS; i += 1024) {
+    const int4 x = ((const int4*)count)[i];
+    out[i] = x.x + x.y + x.z + x.w;
   }
 }
 
-// DENSE: keys of paged_keys_kernel.
+// DENSE: keys and first counts of paged_keys_kernel; keys that share the first bits found are
+// put aside in the second step, so that the third one looks at them alone.
+constexpr int SELECT_ASIDE = 8192;
 template <int T, int K, bool DENSE>
 __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
-  constexpr int BINS = 2048, W = T / 64, PER = BINS / T, CP = T == 1024 ? 4 : 1;
-  __shared__ int hist[BINS * CP], part[W], part_eq[W], found[3];
+  constexpr int BINS = SELECT_BINS, W = T / 64, PER = BINS / T, CP = T == 1024 ? 4 : 1;
+  __shared__ int hist[BINS * CP], part[W], part_eq[W], found[4];
+  __shared__ uint32_t aside[DENSE ? SELECT_ASIDE : 1];
   const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), g = blockIdx.x, s = blockIdx.y;
   const int n = paged_len(a.c, s);
   int* kept = a.kept + ((long)s * gridDim.x + g) * a.keep;
@@ -375,13 +395,13 @@ __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
       const auto r = paged_rows(a.keys + ((long)s * gridDim.x + g) * a.kstride, hi * 4);
       const int off = ((int)base + w * steps * 64 + lane) * 4;
 #pragma unroll
-      for (int k0 = 0; k0 < K; k0 += 16) {
+      for (int k0 = 0; k0 < K; k0 += 8) {
         if (k0 < steps) {
 #pragma unroll
-          for (int k = k0; k < k0 + 16; ++k) key[k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_raw_buffer_load_b32(r, off, k * 256, 0));
+          for (int k = k0; k < k0 + 8; ++k) key[k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_raw_buffer_load_b32(r, off, k * 256, 0));
         }
 #pragma unroll
-        for (int k = k0; k < k0 + 16; ++k) key[k] = k < steps ? key[k] : 0;
+        for (int k = k0; k < k0 + 8; ++k) key[k] = k < steps ? key[k] : 0;
       }
       return;
     }
@@ -432,27 +452,49 @@ __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
   };
   load(lo);
   const bool once = hi - lo <= span;
+  auto in_front = [&](const int* x) {   // the sum of the waves' numbers in front of this one, and of all
+    const int v = lane < W ? x[lane] : 0, incl = lanes_scan(v);
+    return make_int2(__builtin_amdgcn_readlane(incl - v, w), __builtin_amdgcn_readlane(incl, 63));
+  };
   uint32_t top = 0, mask = 0;   // the bits of the m-th largest key that are known
   int left = m;                 // its rank among the keys that have them
   bool all = false;             // that is the last one of them
+  int cand = 0;                 // how many they are
   for (int shift = 21; shift >= 0; shift = shift == 21 ? 10 : shift - 10) {
     const int bins = shift ? 2048 : 1024;
-    for (int i = tid; i < BINS * CP / 4; i += T) ((int4*)hist)[i] = make_int4(0, 0, 0, 0);
-    __syncthreads();
-    for (long base = lo; base < hi; base += span) {
-      if (!once && (base != lo || shift != 21)) load(base);
-      each([&](int k) {   // (the known bits of a key of no entry are not those of `top`, once there are any)
-        if (shift == 21 ? key[k] != 0 : ((key[k] ^ top) & mask) == 0)
-          atomicAdd(&hist[(key[k] >> shift & (bins - 1)) * CP + lane % CP], 1);
-      });
+    const bool given = DENSE && shift == 21, few = DENSE && cand <= SELECT_ASIDE;
+    if (!given) {
+      for (int i = tid; i < BINS * CP / 4; i += T) ((int4*)hist)[i] = make_int4(0, 0, 0, 0);
+      if (tid == 0) found[3] = 0;
+      __syncthreads();
+      auto raise = [&](uint32_t k) { atomicAdd(&hist[(k >> shift & (bins - 1)) * CP + lane % CP], 1); };
+      if (few && shift == 0) {
+        for (int i = tid; i < cand; i += T)
+          if (((aside[i] ^ top) & mask) == 0) raise(aside[i]);
+      } else {
+        for (long base = lo; base < hi; base += span) {
+          if (!once && (base != lo || shift != 21)) load(base);
+          each([&](int k) {   // (the known bits of a key of no entry are not those of `top`, once there are any)
+            if (shift == 21 ? key[k] != 0 : ((key[k] ^ top) & mask) == 0) {
+              raise(key[k]);
+              if (few) aside[atomicAdd(&found[3], 1)] = key[k];   // (in any order: they are only counted)
+            }
+          });
+        }
+      }
+      __syncthreads();
     }
-    __syncthreads();
     // thread t holds bins BINS - 1 - (PER t + i), so that sums run from the largest key down
     int c[PER], sum = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int b = BINS - 1 - (PER * tid + i);
-      if constexpr (CP == 4) {
+      if (given) {
+        c[i] = 0;
+        const int* parts = a.bins + ((long)s * gridDim.x + g) * a.kblocks * BINS + b;
+#pragma unroll 8
+        for (int k = 0; k < (n + a.kpart - 1) / a.kpart; ++k) c[i] += parts[k * BINS];
+      } else if constexpr (CP == 4) {
         const int4 x = ((const int4*)hist)[b];
         c[i] = x.x + x.y + x.z + x.w;
       } else {
@@ -463,14 +505,14 @@ __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
     const int incl = lanes_scan(sum);
     if (lane == 63) part[w] = incl;
     __syncthreads();
-    int before = incl - sum;
-    for (int i = 0; i < w; ++i) before += part[i];
+    int before = incl - sum + in_front(part).x;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       if (before < left && left <= before + c[i]) {   // (one thread's)
         found[0] = BINS - 1 - (PER * tid + i);
         found[1] = left - before;
         found[2] = left == before + c[i];
+        if (shift == 21) found[3] = c[i];
       }
       before += c[i];
     }
@@ -479,6 +521,8 @@ __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
     mask |= (uint32_t)(bins - 1) << shift;
     left = found[1];
     all = found[2];
+    if (shift == 21) cand = found[3];
+    __syncthreads();
   }
   if (all) {   // every key equal to the m-th stays too
     top -= 1;  // (keys of entries are above 0)
@@ -497,15 +541,10 @@ __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
       part_eq[w] = y;
     }
     __syncthreads();
-    int over = 0, eq = 0;
-    for (int i = 0; i < W; ++i) {
-      if (i == w) {
-        over = more;
-        eq = same;
-      }
-      more += part[i];
-      same += part_eq[i];
-    }
+    const int2 a0 = in_front(part), e0 = in_front(part_eq);
+    int over = more + a0.x, eq = same + e0.x;
+    more += a0.y;
+    same += e0.y;
     auto lanes_below = [](unsigned long x) { return (int)__builtin_amdgcn_mbcnt_hi(x >> 32, __builtin_amdgcn_mbcnt_lo((uint32_t)x, 0)); };
     int* to = kept + a.first;
     if (left == 0) {

@@ -223,14 +223,15 @@ def test_score_and_evict_null_structs_and_scales():
 
 
 def test_evict_workspace():
-    """The lists' keys where few long tables are given, 64 MiB at most; none for others."""
+    """The lists' keys and counts where few long tables are given, 96 MiB at most; none for others."""
     size = binding.still_paged_evict_workspace_size
     assert size(_plain(), _seqs(max_pages=512, table_stride=512), _ecfg()) == 0
     long = _seqs(max_pages=600, table_stride=600)
-    assert size(_plain(), long, _ecfg()) == 4 * 8 * 9600 * 4 and size(_plain(), long, _ecfg(shared=1)) == 4 * 9600 * 4
+    each = 9600 * 4 + 3 * 2048 * 4
+    assert size(_plain(), long, _ecfg()) == 4 * 8 * each and size(_plain(), long, _ecfg(shared=1)) == 4 * each
     assert size(_plain(), _seqs(n_seqs=60, max_pages=600, table_stride=600), _ecfg()) == 0
     for pages in (1 << 16, 1 << 20, 1 << 26):
-        assert size(_plain(), _seqs(max_pages=pages, table_stride=pages), _ecfg(shared=1)) <= 64 << 20
+        assert size(_plain(), _seqs(max_pages=pages, table_stride=pages), _ecfg(shared=1)) <= 96 << 20
     assert size(_plain(head_dim=96), long, _ecfg()) == 0 and size(_plain(), long, _ecfg(keep=0)) == 0
     assert _evict(seqs=long) == -4 and _evict(seqs=long, ws=FAKE, ws_bytes=1000) == -4
     assert _evict(seqs=long, ws=FAKE + 4, ws_bytes=1 << 30) == -1
