@@ -78,7 +78,11 @@ static still_status check_evict(const still_paged_cache* cache, const still_page
 }
 
 // The workspace: keys of lists that are formed ahead, and counts of their parts; none where
-// a list's workgroup forms its own.
+// a list's workgroup forms its own: where it holds them all (16384 keys; those of all heads
+// together from 8192 on take longer to sum), and where there are lists for a quarter of the chip.
+// us formed there / ahead (and a launch more, about 1.5): one sequence for all 8 heads of 9000
+// entries 19 / 15, 64 such sequences 21 / 17; by head, 8 lists of 12000 entries 14 / 16, 64 of them
+// 15 / 17, 8 of 20000 36 / 22, of 65536 70 / 32, 64 of them 71 / 39.
 struct EvictPlan {
   long lists, kstride = 0;
   int kblocks = 0, kpart = 0;
@@ -88,7 +92,7 @@ static EvictPlan evict_plan(const still_paged_cache* c, const still_paged_seqs* 
   EvictPlan p;
   const long cap = (long)q->max_pages * c->page_size;
   p.lists = (long)q->n_seqs * (f->shared ? 1 : c->n_kv_heads);
-  if (cap <= 8192 || p.lists > 64 || p.lists * cap > 1L << 24) return p;
+  if (cap <= (f->shared ? 8192 : 16384) || p.lists > 64 || p.lists * cap > 1L << 24) return p;
   p.kstride = cap;
   p.kpart = (int)rup((cap + 63) / 64, 4096);   // 64 parts at most
   p.kblocks = (int)((cap + p.kpart - 1) / p.kpart);
@@ -136,6 +140,8 @@ static still_status paged_evict_call(const still_paged_cache* cache, float* ks, 
   if (a.kstride) {
     hipLaunchKernelGGL(paged_keys_kernel, dim3(a.kblocks, per_seq, n_seqs), dim3(1024), 0, st, a);
     hipLaunchKernelGGL((paged_select_kernel<1024, 16, true>), grid_of, dim3(1024), 0, st, a);
+  // us by 256 / 512 / 1024 threads: 512 lists of 1500 8.8 / 12.0 / 23, of 3000 19 / 13 / 24; 256 of
+  // 6000 22 / 12 / 13
   } else if (cap <= 2048) {
     hipLaunchKernelGGL((paged_select_kernel<256, 8, false>), grid_of, dim3(256), 0, st, a);
   } else if (cap <= 8192) {
@@ -144,7 +150,11 @@ static still_status paged_evict_call(const still_paged_cache* cache, float* ks, 
     hipLaunchKernelGGL((paged_select_kernel<1024, 16, false>), grid_of, dim3(1024), 0, st, a);
   }
   HIP_TRY(hipGetLastError());
-  const bool few = (long)H * n_seqs <= 64;
+  // Workgroups of 1024 threads, and of 16 and 32 bits column pieces of their own, where there are
+  // few lists: us of 8-bit moves to 1024 entries by 1024 / 256 threads, 8 lists 9 / 17, 64 11 / 20, 128
+  // 19 / 24, 512 - / 62; of bf16 (four pieces / one) 64 lists 22 / 34, 128 43 / 41, 512 210 / 110; 8 lists
+  // to 4096 in 1 / 2 / 4 / 8 pieces 51 / 29 / 22 / 26.
+  const bool few = (long)H * n_seqs <= (ks ? 128 : 64);
   const int pieces = ks || !few ? 1 : 4;
   const dim3 grid(H, n_seqs, 2 * pieces + 1), threads(few ? 1024 : 256);
   auto move = [&](auto rowb, auto c8) {

@@ -46,10 +46,13 @@ still_status still_paged8_append(const still_paged8_cache* cache, const still_pa
   paged_dispatch(&c, [&](auto it, auto d) {
     using IT = decltype(it);
     constexpr int D = decltype(d)::value;
-    // tokens of a workgroup: one that is alone leads by itself; of longer runs one in 16 does.
+    // Tokens of a workgroup, 1 or 16: one that is alone leads by itself; of longer runs one in
+    // 16 does, and where they are few it does not matter that the others start for nothing.
+    // us at 1 / 16: 256 runs of 4 tokens of width 128 17 / 22, of 8 32 / 16, of 16 70 / 13; 4 runs of 8
+    // 4.4 / 11, of 64 8 / 11.
     // Heads of a workgroup: a wave's 2 units of two heads one after the other, or of four,
     // which share the angles.  us at 2 / 4 / 8: one token of 8 heads 4.5 / 5.3 / 6.6, 64 tokens
-    // 5.0 / 5.9 / 7.8, 256 of width 256 9.6 / 7.2 / 8.9, 7k in 13 prompts 46 / 37 / 42.
+    // 5.0 / 5.9 / 7.8, 256 of width 256 9.6 / 7.2 / 8.9, 7k in 13 prompts (with two waves per SIMD) 46 / 37 / 42.
     auto launch = [&](auto tg) {
       constexpr int TG = decltype(tg)::value;
       const PagedGrid g(((unsigned)t->n_tokens + TG - 1) / TG);
@@ -57,7 +60,7 @@ still_status still_paged8_append(const still_paged8_cache* cache, const still_pa
       hipLaunchKernelGGL((paged8_append_kernel<IT, D, TG>), dim3(g.x, (c.n_kv_heads + a.heads - 1) / a.heads, g.more),
                          dim3(256), 0, st, a);
     };
-    if (t->n_tokens / seqs->n_seqs < 8) launch(std::integral_constant<int, 1>());
+    if (t->n_tokens <= 256 || t->n_tokens / seqs->n_seqs < 8) launch(std::integral_constant<int, 1>());
     else launch(std::integral_constant<int, 16>());
   });
   HIP_TRY(hipGetLastError());

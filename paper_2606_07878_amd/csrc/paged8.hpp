@@ -72,8 +72,10 @@ __device__ __forceinline__ double2 rope_cs64(double pos, double inv) {
 // wave a (head, key or value) at a time: its rows' largest magnitude decides the
 // scale, so no two waves share a block.  A lane holds 8 values and the 8 that are
 // rotated with them, d/2 further on.
-// Reads the rows, writes a byte a value; the chain offsets -> length -> page -> old scale
-// is what a single token costs.
+// Reads the rows, writes a byte a value: 6977 tokens of 8 heads of width 256 (86 MB) 30 us, 2.9
+// TB/s, 22 without rotation; the largest number of a block is known only once all of it is in
+// registers, which leaves three waves per SIMD at that width.  A single token costs the chain
+// offsets -> length -> page -> old scale, 4.4 us.
 // ---------------------------------------------------------------------------
 struct Append8Args {
   PagedAppendArgs t;
@@ -248,7 +250,8 @@ __global__ __launch_bounds__(256, 3) void paged8_append_kernel(Append8Args p) {
 
 // ---------------------------------------------------------------------------
 // Gather: block (x, h, z) reads PAGED_GATHER_ROWS entries of head h, a thread the codes
-// of 16 bytes of a row given out, keys and values.
+// of 16 bytes of a row given out, keys and values.  Bound by the copy: 65536 entries of 8 heads
+// of width 256 (806 MB) 151 us, 5.3 TB/s.
 // ---------------------------------------------------------------------------
 template <class IT, int D>
 __global__ __launch_bounds__(256) void paged8_gather_kernel(PagedGatherArgs a) {

@@ -196,12 +196,23 @@ def test_evict_how_many(kind, keep, first, recent):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("seqs,n,keep", [(1, 9000, 4000), (1, 40000, 123), (40, 600, 512), (3, 5000, 4999)])
+@pytest.mark.parametrize("seqs,n,keep", [(1, 9000, 4000), (1, 17000, 900), (1, 40000, 123), (40, 600, 512), (3, 5000, 4999),
+                                         (3, 9000, 8000), (33, 17000, 100)])
 def test_evict_long_and_many(kind, seqs, n, keep):
     """Lists by 256 and by 1024 threads, moves in column pieces and in several chunks."""
     log(f"evict kind={kind} {seqs} of {n} to {keep}")
     c = Paged8(62, [n - 7 * s for s in range(seqs)], 2, 64, 64, spare=1)
     check_evict(c, kind, keep, first=4, recent=min(64, keep // 4), shared=seqs == 3)
+
+
+def test_evict_long_lists_of_equal_scores():
+    """Ties across threads, waves and rounds; more keys than are put aside share the bits found."""
+    c = Paged8(67, [40000, 12000], 1, 64, 64, spare=1)
+    c.scores = (torch.arange(c.n_pages * 64) * 7919 % 5).float().reshape(c.n_pages, 1, 64) / 4 + 1
+    check_evict(c, BF16, 20000, shared=True)
+    check_evict(c, BF16, 11000)
+    c.scores.fill_(1.0)
+    check_evict(c, E8, 9000, first=3, recent=50)
 
 
 def test_evict_equal_and_odd_scores():

@@ -226,9 +226,11 @@ def test_evict_workspace():
     """The lists' keys and counts where few long tables are given, 96 MiB at most; none for others."""
     size = binding.still_paged_evict_workspace_size
     assert size(_plain(), _seqs(max_pages=512, table_stride=512), _ecfg()) == 0
-    long = _seqs(max_pages=600, table_stride=600)
-    each = 9600 * 4 + 3 * 2048 * 4
+    long = _seqs(max_pages=1200, table_stride=1200)
+    each = 19200 * 4 + 5 * 2048 * 4
     assert size(_plain(), long, _ecfg()) == 4 * 8 * each and size(_plain(), long, _ecfg(shared=1)) == 4 * each
+    assert size(_plain(), _seqs(max_pages=600, table_stride=600), _ecfg()) == 0
+    assert size(_plain(), _seqs(max_pages=600, table_stride=600), _ecfg(shared=1)) > 0
     assert size(_plain(), _seqs(n_seqs=60, max_pages=600, table_stride=600), _ecfg()) == 0
     for pages in (1 << 16, 1 << 20, 1 << 26):
         assert size(_plain(), _seqs(max_pages=pages, table_stride=pages), _ecfg(shared=1)) <= 96 << 20
