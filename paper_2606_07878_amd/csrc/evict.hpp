@@ -481,7 +481,10 @@ __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
           each([&](int k) {   // (the known bits of a key of no entry are not those of `top`, once there are any)
             if (shift == 21 ? key[k] != 0 : ((key[k] ^ top) & mask) == 0) {
               raise(key[k]);
-              if (few) aside[atomicAdd(&found[3], 1)] = key[k];   // (in any order: they are only counted)
+              if (few) {   // (in any order: they are only counted)
+                const int at = atomicAdd(&found[3], 1);
+                if (at < SELECT_ASIDE) aside[at] = key[k];
+              }
             }
           });
         }
@@ -532,7 +535,8 @@ __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
     top -= 1;  // (keys of entries are above 0)
     left = 0;
   }
-  // ---- the list, wave by wave: how many keys each has above `top` and equal to it, then which
+  // ---- the list, wave by wave: how many keys each has above `top` and equal to it, then which.
+  // (They are m, unless scores or workspace change meanwhile, which must not write past the list.)
   int more = 0, same = 0;       // in front of the round
   for (long base = lo; base < hi; base += span) {
     if (!once) load(base);
@@ -554,7 +558,8 @@ __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
     if (left == 0) {
       each([&](int k) {
         const unsigned long o = __ballot(key[k] > top);
-        if (key[k] > top) to[over + lanes_below(o)] = entry((int)base, k);
+        const int at = over + lanes_below(o);
+        if (key[k] > top && at < m) to[at] = entry((int)base, k);
         over += __popcll(o);
       });
       continue;
@@ -562,7 +567,8 @@ __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
     each([&](int k) {
       const unsigned long o = __ballot(key[k] > top), e = __ballot(key[k] == top);
       const int r = eq + lanes_below(e);
-      if (key[k] > top || (key[k] == top && r < left)) to[over + lanes_below(o) + min(r, left)] = entry((int)base, k);
+      const int at = over + lanes_below(o) + min(r, left);
+      if ((key[k] > top || (key[k] == top && r < left)) && at < m) to[at] = entry((int)base, k);
       over += __popcll(o);
       eq += __popcll(e);
     });
@@ -600,7 +606,10 @@ __global__ __launch_bounds__(1024) void paged_move_kernel(PagedEvictArgs a, int 
   auto find = [&](int i0) {
     int j[U], pf[U], pt[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) j[u] = entry(i0, u) < a.keep ? kept[entry(i0, u)] : -1;
+    for (int u = 0; u < U; ++u) {
+      j[u] = entry(i0, u) < a.keep ? kept[entry(i0, u)] : -1;
+      if (j[u] >= paged_cap(a.c)) j[u] = -1;   // (no entry: the list was written to meanwhile)
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       pf[u] = j[u] < 0 ? -1 : paged_page(a.c, s, j[u]);
