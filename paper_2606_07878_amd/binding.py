@@ -784,8 +784,9 @@ def _queries(torch, q, k_pages, dtype, cache, seqs, dev, causal, scale, q_positi
     H, n = cache.n_kv_heads, seqs.n_seqs
     if n < 1 or H < 1 or d != cache.head_dim or Hq < H or Hq % H or tokens < n or tokens % n:
         _refuse(-2, f"q {tuple(shape)} does not fit {n} sequences and pages {tuple(k_pages.shape)}")
-    _want_rows(q, "q", k_pages, shape, dtype)
     qs = q.stride()
+    if not (q.dtype is dtype and qs[2] == 1 and q.get_device() == dev):
+        _want_rows(q, "q", k_pages, shape, dtype)
     if (qs[1] != d and Hq > 1) or (qs[0] == 0 and tokens > 1):   # (a stride of 0 means dense tokens to the C call)
         _refuse(-1, "q's tokens are not contiguous, or the same one")
     pos = None
@@ -803,7 +804,7 @@ def _attend(torch, q, k_pages, cache, seqs, dev, causal, scale, q_positions, rop
     shape = q.shape
     if out is None:
         out = torch.empty(shape, dtype=q.dtype, device=q.device)
-    else:
+    elif not (out.dtype is q.dtype and out.shape == shape and out.is_contiguous() and out.get_device() == dev):
         _want(out, "out", q.dtype, shape, dev)
     if lse is not None:
         _want(lse, "lse", torch.float32, shape[:2], dev)
