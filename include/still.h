@@ -453,7 +453,8 @@ still_status still_paged8_gather(const still_paged8_cache *cache, const still_pa
                                  int32_t start, int32_t n, void *K, void *V, float *beta, void *stream);
 
 /* still_paged_attend_lse over such a cache (`lse` may be NULL): queries and outputs
- * are of the cache's mode, products and sums of 32 bits as there. */
+ * are of the cache's mode, products and sums of 32 bits as there.  The workspace is
+ * never above STILL_PAGED_WORKSPACE_BYTES either. */
 size_t still_paged8_attend_workspace_size(const still_paged8_cache *cache, const still_paged_attend_config *cfg);
 still_status still_paged8_attend(const still_paged8_cache *cache, const still_paged_seqs *seqs,
                                  const still_paged_attend_config *cfg, const void *q, const double *q_positions,

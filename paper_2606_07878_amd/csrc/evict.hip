@@ -5,10 +5,6 @@
 
 namespace still {
 
-static still_paged_cache plain_view(const still_paged8_cache* c) {
-  return {c->n_kv_heads, c->head_dim, c->page_size, c->n_pages, c->mode, c->k, c->v, c->beta};
-}
-
 // C8: keys of 8 bits, with scales ks.
 template <bool C8>
 static still_status paged_score_call(const still_paged_cache* cache, const float* ks, const still_paged_seqs* seqs,

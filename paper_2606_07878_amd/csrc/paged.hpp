@@ -256,6 +256,9 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(PagedGatherArgs a) {
 //   parts would round each by 2^-17: 45.0 us instead of 48.0 for 8 causal rows of 5
 //   sequences, 87 instead of 97 for 16 sequences of width 64 and 32 rows, no difference
 //   above 1 % to 16 rows.  fp32: one v_mfma_f32_16x16x4_f32 per entry.
+//   8 bits: e4m3 codes become bf16, which holds them, two at a time; a piece of a key is
+//   two operands.  A tile is a block of entries that share a scale: the keys' goes into
+//   the logits' factor, the values' into the weights.  fp32 queries go in as three parts too.
 // Keys of the next chunk are loaded once the logits have used this one's, values
 // once P.V has; page numbers are read two chunks ahead, before the keys of the
 // next one, so that they are there with them (loads return in order).  A tile is

@@ -5,12 +5,6 @@
 
 namespace still {
 
-// The cache's dimensions, pointers and rows' type, which the checks of the other paged
-// caches cover.
-static still_paged_cache plain_view(const still_paged8_cache* c) {
-  return {c->n_kv_heads, c->head_dim, c->page_size, c->n_pages, c->mode, c->k, c->v, c->beta};
-}
-
 static still_status check_scales(const still_paged8_cache* c) {
   still_status s;
   if ((s = check_ptr(c->k_scale, "cache k_scale", true)) != STILL_OK) return s;

@@ -18,6 +18,12 @@ inline still_status check_cache(const still_paged_cache* c) {
   return STILL_OK;
 }
 
+// The dimensions, pointers and rows' type of a cache in 8 bits, which the checks of the
+// others cover.
+inline still_paged_cache plain_view(const still_paged8_cache* c) {
+  return {c->n_kv_heads, c->head_dim, c->page_size, c->n_pages, c->mode, c->k, c->v, c->beta};
+}
+
 inline still_status check_pages(const still_paged_cache* c) {
   still_status s;
   if ((s = check_ptr(c->k, "cache k", true)) != STILL_OK || (s = check_ptr(c->v, "cache v", true)) != STILL_OK) return s;
