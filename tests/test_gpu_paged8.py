@@ -426,3 +426,15 @@ def test_steps_captured_in_a_graph_follow_the_lengths():
         q.copy_(c.rows(S, heads=H * group))
         eager = step(other, None, eager_lse).clone()
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("mode,bits", [(BF16, [0x7F81, -127, 0x7FC0, 0x7FFF]), (FP32, [0x7F800001, -8388607, 0x7FC00000, 0x7FFFFFFF])])
+def test_append_every_nan(mode, bits):
+    """Signalling and quiet ones of both signs leave the scale alone, whatever holds the largest number."""
+    c = Paged8(19, [32], 1, 64, 16, beta=False)
+    x = torch.randn(32, 1, 64, generator=c.g).to(DT[mode])
+    raw = x.view(torch.int16 if mode == BF16 else torch.int32)
+    raw[torch.arange(0, 32, 2), 0, torch.arange(16) * 3] = torch.tensor(bits * 4, dtype=raw.dtype)
+    assert x.isnan().sum() == 16
+    check_append(c, x.cuda(), x.flip(0).contiguous().cuda())
+    check_append(c, x.cuda(), x.flip(0).contiguous().cuda(), positions=torch.arange(32, dtype=torch.float64), theta=1e4)
