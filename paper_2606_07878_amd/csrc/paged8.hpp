@@ -103,13 +103,14 @@ __global__ __launch_bounds__(256, 3) void paged8_append_kernel(Append8Args p) {
       const int x0 = (lane + 1) * ((n_seqs + 63) / 64);
       int base = uniform(paged_seq_of(a.offsets, n_seqs, (int)t0, x0 < n_seqs ? a.offsets[x0] : 0));
       s = base;
-      // sequences that start behind the first token, 64 at a time
+      // sequences that start behind the first token, 64 at a time: a token is as many further on as
+      // start up to it, in whichever 64
       while (true) {
         const int x = base + 1 + lane, o = x < n_seqs ? a.offsets[x] : INT32_MAX;
 #pragma unroll
         for (int t = 0; t < TG; ++t) {
           const int n = __popcll(__ballot(o <= (int)t0 + t));
-          if (lane == t) s = base + n;
+          if (lane == t) s += n;
         }
         const int last = __builtin_amdgcn_readlane(o, 63);
         if ((long)last > t0 + TG - 1) break;

@@ -99,6 +99,25 @@ def test_append_finds_the_sequence_among_many(seqs):
     check_append(c, c.rows(int(off[-1])).cuda(), c.rows(int(off[-1])).cuda(), offsets=off)
 
 
+@pytest.mark.parametrize("mode", [BF16, FP32])
+@pytest.mark.parametrize("seqs", [80, 128, 200])
+@pytest.mark.parametrize("busy", [(0,), (5,), (-1,), (40, 41), (0, -1), (3, 70)])
+def test_append_to_a_batch_of_idle_sequences(mode, seqs, busy):
+    """Prompts in a table of which all other sequences get nothing: 64 and more start within one
+    workgroup's 16 tokens, in front of, between and behind the ones that have some."""
+    log(f"append8 mode={mode} {len(busy)} of {seqs} have tokens")
+    rng = np.random.default_rng(seqs)
+    new, held = np.zeros(seqs, int), rng.integers(0, 30, seqs)
+    for i, s in enumerate(busy):
+        new[s] = (8 * seqs + 5) // len(busy) + 3 * i + 1
+    assert new.sum() % 16 and new.sum() > 256 and new.sum() >= 8 * seqs
+    c = Paged8(19, held + new, 1, 64, 16)
+    n = int(new.sum())
+    off = torch.tensor(np.concatenate([[0], np.cumsum(new)]), dtype=torch.int32)
+    check_append(c, c.rows(n, mode).cuda(), c.rows(n, mode).cuda(), offsets=off, positions=torch.arange(n, dtype=torch.float64),
+                 theta=1e4, beta=torch.randn(n, 1, generator=c.g).cuda())
+
+
 def test_append_strided_rows_and_no_bias_given():
     c = Paged8(14, [40, 33], 3, 128, 16)
     qkv = torch.randn(9, 12 * 128, generator=c.g).bfloat16().cuda()
