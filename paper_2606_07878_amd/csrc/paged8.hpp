@@ -95,26 +95,26 @@ __global__ __launch_bounds__(256, 3) void paged8_append_kernel(Append8Args p) {
   long j = -1;
   int count = 0, page = -1;
   {
-    const int i = (int)t0 + lane, n_seqs = a.c.n_seqs;
-    const bool mine = lane < TG && i < a.n_tokens;
+    const bool mine = lane < TG && t0 + lane < a.n_tokens;
+    const int i = mine ? (int)t0 + lane : 0, n_seqs = a.c.n_seqs;
     int s = 0;
     long start = 0, end = -1;
     if (a.offsets) {
       const int x0 = (lane + 1) * ((n_seqs + 63) / 64);
-      int base = uniform(paged_seq_of(a.offsets, n_seqs, (int)t0, x0 < n_seqs ? a.offsets[x0] : 0));
-      s = base;
+      const int from = uniform(paged_seq_of(a.offsets, n_seqs, (int)t0, x0 < n_seqs ? a.offsets[x0] : 0));
+      s = from;
       // sequences that start behind the first token, 64 at a time: a token is as many further on as
-      // start up to it, in whichever 64
-      while (true) {
-        const int x = base + 1 + lane, o = x < n_seqs ? a.offsets[x] : INT32_MAX;
+      // start up to it, in whichever 64.  (Tokens and offsets may be as many as an int counts: that
+      // there are no more sequences is known from n_seqs alone.)
+      for (int next = from + 1; next < n_seqs; next += 64) {
+        const bool there = next + lane < n_seqs;
+        const int o = there ? a.offsets[next + lane] : 0;
 #pragma unroll
         for (int t = 0; t < TG; ++t) {
-          const int n = __popcll(__ballot(o <= (int)t0 + t));
+          const int n = __popcll(__ballot(there && o <= (int)t0 + t));
           if (lane == t) s += n;
         }
-        const int last = __builtin_amdgcn_readlane(o, 63);
-        if ((long)last > t0 + TG - 1) break;
-        base += 64;
+        if (next + 64 <= n_seqs && __builtin_amdgcn_readlane(o, 63) > (int)t0 + (TG - 1)) break;
       }
       if (mine) {
         start = a.offsets[s];

@@ -118,6 +118,24 @@ def test_append_to_a_batch_of_idle_sequences(mode, seqs, busy):
                  theta=1e4, beta=torch.randn(n, 1, generator=c.g).cuda())
 
 
+def test_append_of_as_many_tokens_as_an_int_counts():
+    """2^31 - 1 tokens, one row over and over; the last entries have a place, those in front of the tables do not."""
+    n = (1 << 31) - 1
+    for lens, last in (([40], []), ([5, 23, 17], [n - 40, n - 17]), ([7] + [0] * 70 + [20], [n - 9] * 70 + [n - 9])):
+        c = Paged8(49, lens, 1, 64, 16, beta=False)
+        off = torch.tensor([0, *last, n], dtype=torch.int32)
+        row = c.rows(1).cuda()
+        want = [x.clone() for x in c.cuda().pools()]
+        new = np.minimum(lens, np.diff(off.numpy()))      # of them with a place
+        few = torch.from_numpy(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)).cuda()
+        binding.paged8_append(row.expand(int(few[-1]), 1, 64), row.expand(int(few[-1]), 1, 64), *want, c.table, c.lens, offsets=few)
+        torch.cuda.synchronize()
+        log(f"append8 of 2^31 - 1 tokens to {len(lens)} sequences")
+        binding.paged8_append(row.expand(n, 1, 64), row.expand(n, 1, 64), *c.pages(), offsets=off.cuda())
+        torch.cuda.synchronize()
+        assert all(equal(a, b) if a.dtype == E4M3 else torch.equal(a, b) for a, b in zip(c.pools(), want))
+
+
 def test_append_strided_rows_and_no_bias_given():
     c = Paged8(14, [40, 33], 3, 128, 16)
     qkv = torch.randn(9, 12 * 128, generator=c.g).bfloat16().cuda()
