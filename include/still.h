@@ -424,8 +424,8 @@ still_status still_paged_attend_lse(const still_paged_cache *cache, const still_
  * infinity), and blocks of 16 entries (slots 16 b .. 16 b + 15 of a page) of a head
  * share a positive float scale: an entry's key stands for its codes times k_scale of its
  * block, its value for its codes times v_scale.  The append makes scales that are
- * powers of two; the calls that read take any.  Sequences, tables, lengths and
- * absent pages as above.
+ * powers of two, 2^-100 at least; the calls that read take any from there on.
+ * Sequences, tables, lengths and absent pages as above.
  * ------------------------------------------------------------------------- */
 typedef struct {
   int32_t n_kv_heads, head_dim, page_size, n_pages;   /* as still_paged_cache                 */
@@ -497,8 +497,8 @@ typedef struct {
  * the first and the recent ones, then those of the largest scores (ties: the
  * earlier entry; NaN counts as minus infinity) move to the front in their order,
  * with their bias and scores.  In 8 bits, a block of 16 new places takes the
- * largest scale that its entries had, and their codes are rescaled to it (exact but
- * for what falls below the smallest code).  Places behind the new length stay as
+ * largest scale that its entries had (2^-100 where all of them lay on absent pages), and
+ * their codes are rescaled to it (exact but for what falls below the smallest code).  Places behind the new length stay as
  * they were.  An entry on an absent page counts as one of score minus infinity and
  * moves as zeros; an absent place is not written.
  *   kept      [n_seqs][shared ? 1 : H][keep] int32: the entries that stay, rising,

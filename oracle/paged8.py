@@ -190,7 +190,8 @@ def move(pages, table, kept) -> np.ndarray:
 
 
 def move8(pages, scales, table, kept):
-    """(pages, scales) of 8 bits after the same: a block's scale is the largest of those that its entries had."""
+    """(pages, scales) of 8 bits after the same: a block's scale is the largest of those that its entries had,
+    LEAST where none was there."""
     n_pages, H, P, _ = pages.shape
     out, new = pages.copy(), np.array(scales, np.float64)
     for s in range(table.shape[0]):
@@ -202,9 +203,9 @@ def move8(pages, scales, table, kept):
                 if dst is None:
                     continue
                 src = [slot(table, s, int(j), P, n_pages) for j in ids[b:b + BLOCK]]
-                had = [scales[x[0], h, x[1] // BLOCK] if x is not None else 0.0 for x in src]
+                had = [scales[x[0], h, x[1] // BLOCK] if x is not None else LEAST for x in src]
                 top = max(had)
                 for i, x in enumerate(src):
-                    out[dst[0], h, dst[1] + i] = e4m3(pages[x[0], h, x[1]] * (had[i] / top)) if x is not None and top > 0 else 0.0
+                    out[dst[0], h, dst[1] + i] = e4m3(pages[x[0], h, x[1]] * (had[i] / top)) if x is not None else 0.0
                 new[dst[0], h, dst[1] // BLOCK] = top
     return out, new

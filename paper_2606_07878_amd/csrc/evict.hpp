@@ -581,8 +581,8 @@ __global__ __launch_bounds__(T) void paged_select_kernel(PagedEvictArgs a) {
 // so a workgroup that takes the entries in order, a chunk loaded as a whole before any
 // of it is stored, needs no other memory.  Block (h, s, z): z counts the keys' and the
 // values' column pieces (of 8 bits one each, for their scales), the last z the scores
-// and bias.  In 8 bits a block of 16 places takes the largest scale of its new entries,
-// and their codes are rescaled to it.
+// and bias.  In 8 bits a block of 16 places takes the largest scale of its new entries
+// (E4M3_LEAST where they were all absent), and their codes are rescaled to it.
 // 512 lists of 1088 entries to 1024, 8 bits of width 128 (272 MB) 62 us, 4.5 TB/s; 8 lists of 65536 to
 // 4096, bf16 (34 MB) 22: two chunks one after the other, each three loads deep.
 // ---------------------------------------------------------------------------
@@ -662,7 +662,7 @@ __global__ __launch_bounds__(1024) void paged_move_kernel(PagedEvictArgs a, int 
       constexpr int LPR = ROWB / 16, RPW = 64 / LPR, SPB = std::max(1, PAGED_BLOCK / RPW);   // steps of a block
 #pragma unroll
       for (int u0 = 0; u0 < U; u0 += SPB) {
-        float top = 0.f;
+        float top = E4M3_LEAST;   // (of a block whose entries were all absent, too)
 #pragma unroll
         for (int u = u0; u < u0 + SPB; ++u) {
           float t = sc[u];
@@ -670,7 +670,7 @@ __global__ __launch_bounds__(1024) void paged_move_kernel(PagedEvictArgs a, int 
           for (int d = LPR; d < LPR * std::min(PAGED_BLOCK, RPW); d <<= 1) t = fmaxf(t, __shfl_xor(t, d));
           top = fmaxf(top, t);
         }
-        const float inv = top > 0.f ? 1.f / top : 0.f;
+        const float inv = 1.f / top;
 #pragma unroll
         for (int u = u0; u < u0 + SPB; ++u) {
           const float ratio = sc[u] * inv;

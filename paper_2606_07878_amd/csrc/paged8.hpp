@@ -11,9 +11,11 @@
 
 namespace still {
 
+constexpr float E4M3_LEAST = 0x1p-100f;   // the smallest scale: no product of a code with it is a subnormal float
+
 // The smallest power of two whose 448-fold (the largest code) reaches top, at least
-// 2^-100, so that no product of a code with it is a subnormal float.  With top =
-// m 2^e, 1 <= m < 2, and 448 = 1.75 2^8 it is 2^(e - 8), twice that where m > 1.75.
+// E4M3_LEAST.  With top = m 2^e, 1 <= m < 2, and 448 = 1.75 2^8 it is 2^(e - 8), twice that
+// where m > 1.75.
 __device__ __forceinline__ float e4m3_scale(float top) {
   const uint32_t b = __float_as_uint(top);
   const int e = (int)(b >> 23) - 8 + ((b & 0x7fffffu) > 0x600000u);

@@ -239,6 +239,27 @@ def test_evict_absent_pages():
         check_evict(c, kind, 140)
 
 
+def test_evict_of_absent_entries_leaves_positive_scales():
+    """A block whose entries all lay on absent pages: zeros, of the smallest scale, to which a later append adds."""
+    c = Paged8(68, [320, 200], 2, 64, 16, spare=4)
+    c.table[0, 17:20] = -1
+    kept, new = check_evict(c, E8, 100, recent=64)
+    c.cuda()
+    binding.paged_evict(c.k, c.v, c.table, c.lens, c.scores, 100, recent=64, k_scales=c.ks, v_scales=c.vs, beta_pages=c.beta,
+                        new_lens=c.lens)
+    of = c.table[0, :7].long()
+    assert (c.ks > 0).all() and (c.vs > 0).all()
+    assert (c.ks[of[4:]] == 2.0 ** -100).all() and (c.vs[of[4:]] == 2.0 ** -100).all()
+    K, V = binding.paged8_gather(*c.pages(), 0, 100)
+    assert K[:, :52].any() and not K[:, 52:].any() and not V[:, 52:].any()
+    was = f64(c.ks), f64(c.k)
+    lens, row = (c.lens + 5)[:1], c.rows(5).cuda()
+    binding.paged8_append(row, row, *c.pools(), c.table[:1], lens, beta_pages=c.beta)
+    want = O8.append(f64(row), f64(row), was[1], was[1], was[0], was[0], c.table[:1].cpu().numpy(), lens.cpu().numpy())
+    np.testing.assert_array_equal(f64(c.k), want[0])
+    np.testing.assert_array_equal(f64(c.ks), want[2])
+
+
 def test_evict_lengths_outside_the_table_and_in_place():
     c = Paged8(65, [100, 50], 2, 64, 16, width=8)
     lens = torch.tensor([10 ** 6, -4], dtype=torch.int32)
