@@ -498,9 +498,12 @@ typedef struct {
  * earlier entry; NaN counts as minus infinity) move to the front in their order,
  * with their bias and scores.  In 8 bits, a block of 16 new places takes the
  * largest scale that its entries had (2^-100 where all of them lay on absent pages), and
- * their codes are rescaled to it (exact but for what falls below the smallest code).  Places behind the new length stay as
- * they were.  An entry on an absent page counts as one of score minus infinity and
- * moves as zeros; an absent place is not written.
+ * their codes are rescaled to it (exact but for what falls below the smallest code).
+ * Places behind the new length are not written.  In 8 bits those that share a block with
+ * the last kept entry keep their codes, but stand for other values where the block's scale
+ * has changed: an entry wanted there again is to be appended anew.  An entry on an absent
+ * page counts as one of score minus infinity and moves as zeros; an absent place is not
+ * written.
  *   kept      [n_seqs][shared ? 1 : H][keep] int32: the entries that stay, rising,
  *             -1 behind them
  *   new_lens  [n_seqs] int32: the lengths behind the call; may be seqs->lens

@@ -956,7 +956,8 @@ def paged_evict(k_pages, v_pages, table, lens, scores, keep: int, first: int = 0
     scores: then an entry still has one position, and compact_paged can take the
     sequence with ``positions[kept]``.  Returns (kept [n_seqs, H or 1, keep] int32: the entries that
     stay, rising, -1 behind them; new lengths [n_seqs] int32), into ``kept`` and
-    ``new_lens`` where given; ``new_lens`` may be ``lens``.  ``workspace`` (96 MiB serve every
+    ``new_lens`` where given; ``new_lens`` may be ``lens``.  The dropped entries are lost, those
+    behind the new lengths too: of 8 bits, their block's scale may have changed.  ``workspace`` (96 MiB serve every
     call, none is needed for tables of up to 8192 entries) may be given too."""
     torch = _torch()
     cache, seqs, dev = _cache(torch, k_pages, v_pages, k_scales, v_scales, beta_pages, table, lens, torch.bfloat16)
