@@ -473,7 +473,9 @@ still_status still_paged8_attend(const still_paged8_cache *cache, const still_pa
  * sum in place of what their score was: new entries, whose slot another sequence
  * may have left (known NULL: there are none).  Entries behind the
  * lengths and on absent pages keep theirs.  A row whose lse is minus infinity
- * adds nothing.  The pages that a call's sequences name must be distinct.
+ * adds nothing.  The pages that a call's sequences name must be distinct.  More tokens than
+ * fit 32 rows of a KV head (the last ones of a prompt) go in several calls, the oldest
+ * first: `lens` ends at a call's last token, `known` is the lengths of the call before.
  *   lse     [n_seqs * n_queries][H*group] float32
  *   known   [n_seqs] int32 or NULL
  *   scores  [n_pages][H][page_size] float32 (16-byte aligned)
