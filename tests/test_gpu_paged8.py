@@ -321,6 +321,54 @@ def test_attend_streaming_loads(nq):
     check_attend(c, c.rows(2 * nq, heads=8), causal=True)
 
 
+ROWS = [(1, 1), (4, 1), (3, 5), (8, 4), (1, 32)]
+
+
+@pytest.mark.parametrize("mode", [BF16, FP32])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("group,nq", ROWS)
+@pytest.mark.parametrize("theta", [0.0, 1e6])
+def test_attend_short_tables(mode, d, group, nq, theta):
+    """Up to 1024 entries: a workgroup takes all of a sequence."""
+    log(f"attend8 short mode={mode} d={d} group={group} nq={nq} theta={theta}")
+    c = Paged8(45, [1000, 77, 0, 512, 3], 2, d, 32)
+    check_attend(c, c.rows(5 * nq, mode, heads=2 * group), causal=nq > 1, theta=theta,
+                 qpos=131000.0 + torch.arange(5 * nq, dtype=torch.float64) if theta else None)
+
+
+@pytest.mark.parametrize("mode", [BF16, FP32])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("group,nq,theta", [(1, 1, 0.0), (4, 1, 1e6), (8, 4, 1e6), (1, 32, 0.0)])
+def test_attend_many_short_tables(mode, d, group, nq, theta):
+    """Up to 512 entries and more than 256 sequences and heads: a wave takes all of one."""
+    log(f"attend8 many short mode={mode} d={d} group={group} nq={nq} theta={theta}")
+    lens = np.random.default_rng(d).integers(0, 60, 65)
+    lens[7] = 500
+    c = Paged8(46, lens, 4, d, 16)
+    check_attend(c, c.rows(65 * nq, mode, heads=4 * group), causal=nq > 1, theta=theta,
+                 qpos=131000.0 + torch.arange(65 * nq, dtype=torch.float64) if theta else None)
+
+
+@pytest.mark.parametrize("mode", [BF16, FP32])
+@pytest.mark.parametrize("d", [64, 256])
+@pytest.mark.parametrize("group,nq,theta", [(4, 1, 0.0), (8, 4, 1e6), (1, 32, 0.0)])
+def test_attend_streaming_loads_of_other_widths(mode, d, group, nq, theta):
+    log(f"attend8 streaming mode={mode} d={d} group={group} nq={nq} theta={theta}")
+    c = Paged8(47, [3000, 5], 2, d, 64)
+    c.table = torch.cat([c.table, torch.zeros(2, 9000 * 128 // d, dtype=torch.int32)], dim=1)
+    check_attend(c, c.rows(2 * nq, mode, heads=2 * group), causal=nq > 1, theta=theta,
+                 qpos=131000.0 + torch.arange(2 * nq, dtype=torch.float64) if theta else None)
+
+
+def test_attend_the_smallest_scales():
+    """2^-100, which blocks of zeros and of numbers near them have."""
+    c = Paged8(48, [700, 90], 2, 128, 16)
+    c.ks, c.vs = c.ks * 2.0 ** -94, c.vs * 2.0 ** -94
+    assert float(c.vs.min()) == 2.0 ** -100
+    check_attend(c, c.rows(2, FP32, heads=4) * 2.0 ** 90)
+    check_attend(c, c.rows(2, heads=4))
+
+
 def test_attend_any_scales():
     """Scales need not be powers of two to be read."""
     c = Paged8(35, [700, 90], 2, 128, 16)
