@@ -933,7 +933,8 @@ def paged_score(q, lse, k_pages, scores, table, lens, causal: bool = False, scal
     (still_paged_score; still_paged8_score for pages of 8 bits, with ``k_scales``).
     Arguments as in paged_attend, whose ``lse`` of the same rows the call takes.
     Entries from ``known`` on (int32 [n_seqs]: the lengths at the call before) get the
-    weights in place of their slots' old scores."""
+    weights in place of their slots' old scores.  More than 32 rows of a KV head (a prompt's
+    last tokens) go in several calls, the oldest first, with ``lens`` up to each call's last token."""
     torch = _torch()
     cache, seqs, dev = _cache(torch, k_pages, k_pages, k_scales, k_scales, beta_pages, table, lens, q.dtype)
     cfg, pos = _queries(torch, q, k_pages, k_pages.dtype if k_scales is None else q.dtype, cache, seqs, dev, causal, scale,

@@ -19,7 +19,9 @@ namespace still {
 // over 64 sequences of 5 to 16384 entries of 8 heads in 8 bits 69 -> 46 us).
 // Bound by the keys where sequences are long: 65536 entries of 8 heads of width 128, 4 rows: in 8
 // bits (67 MB) 16 us, 4.2 TB/s, bf16 31; 32 rows 33.  A workgroup's start takes about 5 us beside:
-// 64 sequences of 2000 (131 MB) 31, of 5 to 16384 43 (with chunks of 512 46, of 256 48).
+// 64 sequences of 2000 (131 MB) 31, of 5 to 16384 43 (with chunks of 512 46, of 256 48).  More
+// workgroups for a long sequence do not help: 65536 entries of bf16 and 32 rows 33.5, with chunks of
+// 512 31.9, of 256 33.2; 4 rows 30.5, 29.4, 30.6; 8 bits and 4 rows 16.0, 15.4, 17.8, 32 rows 23.6, 25.4, 30.1.
 // ---------------------------------------------------------------------------
 struct PagedScoreArgs {
   PagedArgs c;         // (v is not read)

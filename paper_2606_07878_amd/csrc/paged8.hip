@@ -42,8 +42,10 @@ still_status still_paged8_append(const still_paged8_cache* cache, const still_pa
     constexpr int D = decltype(d)::value;
     // Tokens of a workgroup, 1 or 16: one that is alone leads by itself; of longer runs one in
     // 16 does, and where they are few it does not matter that the others start for nothing.
-    // us at 1 / 16: 256 runs of 4 tokens of width 128 17 / 22, of 8 32 / 16, of 16 70 / 13; 4 runs of 8
-    // 4.4 / 11, of 64 8 / 11.
+    // us at 1 / 16, width 128, runs that start at any slot: 256 of 4 tokens 16 / 23, of 8 34 / 15, of 16 77 / 12; 64 of
+    // 4 6 / 23; 4 of 8 5 / 14, of 64 8 / 11.  The host knows the mean run only: one of 2000 beside 255 sequences without
+    // tokens, whose mean is 7.8, takes the first form, 47 / 12 (of width 256 75 / 19), beside 255 of one token each, whose
+    // mean is 8.8, the second, 32 / 46 (47 / 56).
     // Heads of a workgroup: a wave's 2 units of two heads one after the other, or of four,
     // which share the angles.  us at 2 / 4 / 8: one token of 8 heads 4.5 / 5.3 / 6.6, 64 tokens
     // 5.0 / 5.9 / 7.8, 256 of width 256 9.6 / 7.2 / 8.9, 7k in 13 prompts (with two waves per SIMD) 46 / 37 / 42.

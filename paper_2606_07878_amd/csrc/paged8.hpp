@@ -76,7 +76,8 @@ __device__ __forceinline__ double2 rope_cs64(double pos, double inv) {
 // rotated with them, d/2 further on.
 // Reads the rows, writes a byte a value: 6977 tokens of 8 heads of width 256 (86 MB) 30 us, 2.9
 // TB/s, 22 without rotation; the largest number of a block is known only once all of it is in
-// registers, which leaves three waves per SIMD at that width.  A single token costs the chain
+// registers, which leaves three waves per SIMD at that width, with three registers of 168 spilled to 16 bytes
+// of scratch.  A single token costs the chain
 // offsets -> length -> page -> old scale, 4.4 us.
 // ---------------------------------------------------------------------------
 struct Append8Args {

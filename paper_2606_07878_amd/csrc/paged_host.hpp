@@ -129,6 +129,15 @@ inline still_status check_attend(const still_paged_cache* c, const still_paged_a
 // MB): us with ordinary / streaming loads, one sequence of 131136 99 / 89, 64 of up to
 // 16384 108 / 98, 5 of up to 20011 and 32 rows (410 MB) 48.8 / 47.6; below it the entries
 // may still be there from the step before: 4 sequences of up to 9000 (147 MB) 23.6 / 25.8.
+// 8 bits take the same lines.  us at widths 64, 128, 256 (4 rows unless said).  Team / parts (capacity
+// 1024): one sequence of 256 4.8, 5.8, 7.3 / 9.6, 10.0, 11.4; 719 7.5, 8.9, 13.5 / 11.1, 10.2, 11.9; 1024 8.7,
+// 10.2, 16.9 / 11.1, 10.2, 11.9; 32 rows of 719 11.6, 15.0, 21.5 / 12.3, 12.4, 17.2; 64 of 1000 15.6, 24.2, 45.5 /
+// 23.3, 29.3, 49.0; 70 of 1 to 1024 10.9, 13.9, 20.8 / 19.4, 18.7, 24.3: parts are the faster ones for a few
+// sequences of more than 512 of width 256, or of 32 rows, only.  Wave / team (capacity 512): 40 sequences
+// of 30 4.1, 4.9, 6.5 / 5.4, 6.4, 6.3, of 128 6.7, 8.1, 11.1 / 5.8, 7.1, 8.3, of 512 17, 23, 32 / 8.8, 13.6, 19.9; 256 of
+// 30 5.4, 6.9, 11.9 / 15.7, 19.6, 22.2, of 256 16.7, 24.9, 44 / 21.3, 31.5, 49; wave / parts 256 of 30 5.4, 6.9, 11.9 /
+// 27, 23, 31.  Ordinary / streaming loads, one sequence of 131136 (134, 269, 537 MB) 37, 51, 111 / 36, 55, 96; 64 of
+// 16000 (1.0, 2.1, 4.2 GB) 228, 357, 702 / 222, 353, 615; 4 of up to 9000 13.5, 12.4, 14.5 / 13.5, 13.0, 15.3.
 enum PagedKernel { PAGED_PARTS, PAGED_STREAM, PAGED_TEAM, PAGED_WAVE };
 inline PagedKernel paged_kernel(const still_paged_cache* c, const still_paged_seqs* q, int esize) {
   const long cap = (long)q->max_pages * c->page_size, pairs = (long)q->n_seqs * c->n_kv_heads;
