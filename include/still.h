@@ -508,7 +508,8 @@ typedef struct {
  * written.
  *   kept      [n_seqs][shared ? 1 : H][keep] int32: the entries that stay, rising,
  *             -1 behind them
- *   new_lens  [n_seqs] int32: the lengths behind the call; may be seqs->lens
+ *   new_lens  [n_seqs] int32: the lengths behind the call; may be seqs->lens, where no other
+ *             layer is still to be cut from these lengths
  *   workspace still_paged_evict_workspace_size bytes (16-byte aligned; NULL where that is 0), for
  *             caches of 8 bits too (of the same dimensions); at most 96 MiB, nothing for tables
  *             of up to 8192 entries

@@ -957,7 +957,8 @@ def paged_evict(k_pages, v_pages, table, lens, scores, keep: int, first: int = 0
     scores: then an entry still has one position, and compact_paged can take the
     sequence with ``positions[kept]``.  Returns (kept [n_seqs, H or 1, keep] int32: the entries that
     stay, rising, -1 behind them; new lengths [n_seqs] int32), into ``kept`` and
-    ``new_lens`` where given; ``new_lens`` may be ``lens``.  The dropped entries are lost, those
+    ``new_lens`` where given; ``new_lens`` may be ``lens`` (of several layers that share it, in the
+    last one's call).  The dropped entries are lost, those
     behind the new lengths too: of 8 bits, their block's scale may have changed.  ``workspace`` (96 MiB serve every
     call, none is needed for tables of up to 8192 entries) may be given too."""
     torch = _torch()

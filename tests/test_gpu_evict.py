@@ -386,6 +386,55 @@ def test_step_with_eviction_captured_in_a_graph():
         q.copy_(c.rows(S, heads=H * group))
 
 
+def test_evict_of_long_lists_captured_with_one_workspace():
+    """Few long lists, whose keys and counts lie in the caller's workspace: captured for two layers that share
+    it and the lengths, replayed with new scores, whatever it holds, eager calls between."""
+    H, d, P, keep = 2, 64, 64, 1500
+    layers = [Paged8(74 + i, [30000, 900, 21000], H, d, P, spare=1).cuda() for i in range(2)]
+    table, lens = layers[0].table, layers[0].lens
+    size = binding.still_paged_evict_workspace_size(
+        binding.still_paged_cache(H, d, P, layers[0].n_pages, BF16, 16, 16, None),
+        binding.still_paged_seqs(3, table.shape[1], table.shape[1], table.data_ptr(), lens.data_ptr()),
+        binding.still_paged_evict_config(keep, 4, 100, 0))
+    assert size > 0
+    ws = torch.full((size,), 0xA5, dtype=torch.uint8, device="cuda")
+    kept = [torch.empty(3, H, keep, dtype=torch.int32, device="cuda") for _ in layers]
+    new = [torch.empty(3, dtype=torch.int32, device="cuda") for _ in layers]
+
+    def step(caches, kept, new, ws):
+        for x, ids, n in zip(caches, kept, new):
+            binding.paged_evict(x[0], x[1], table, lens, x[4], keep, first=4, recent=100, k_scales=x[2], v_scales=x[3], kept=ids,
+                                new_lens=n, workspace=ws)
+
+    state = [[*x.pools(), x.scores] for x in layers]
+    start = [[y.clone() for y in x] for x in state]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(g, stream=side):
+            step(state, kept, new, ws)
+    torch.cuda.current_stream().wait_stream(side)
+    for rep in range(4):
+        for x, y in zip(state, start):
+            y[4].copy_(torch.rand(y[4].shape, generator=layers[0].g) ** (2 * rep + 1))
+            for a, b in zip(x, y):
+                a.view(torch.uint8).copy_(b.view(torch.uint8))
+        lens.copy_(torch.tensor([30000 - 9000 * rep, 900 + rep * 500, 21000], dtype=torch.int32))
+        other = [[y.clone() for y in x] for x in start]
+        ids, n = [torch.empty_like(x) for x in kept], [torch.empty_like(x) for x in new]
+        step(other, ids, n, None)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert torch.equal(kept[i], ids[i]) and torch.equal(new[i], n[i]), f"replay {rep}"
+            assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(state[i], other[i])), f"replay {rep}"
+        want = O8.evict(table.cpu().numpy(), lens.cpu().numpy(), start[1][4].cpu().numpy(), keep, 4, 100)
+        np.testing.assert_array_equal(kept[1].cpu().numpy(), want[0])
+        ws.fill_(rep)
+
+
 def test_evict_on_another_stream_and_two_at_once():
     c = [Paged8(72 + i, [900, 300], 2, 64, 16).cuda() for i in range(2)]
     want = []
